@@ -567,6 +567,61 @@ nna_status nna_plan_cqt_lengths(const nna_plan* plan, long long* host_out, size_
  * (host array; k itself for a plan from nna_plan_stft). */
 nna_status nna_plan_sigma(const nna_plan* plan, double* host_out, size_t cap);
 
+/*
+ * Operators of networks on top of the transforms: their frames as a sequence.  No plan: `device` is the HIP device of every pointer
+ * (-1 is refused).  Elements are of an nna_dtype; sums, statistics and states are float32 throughout.
+ */
+typedef enum { NNA_F32 = 0, NNA_BF16 = 1, NNA_F16 = 2 } nna_dtype;
+
+/*
+ * Layer norm of `rows` rows of `width` values (1..16384):  y = h w + b,  h = (x - m) r,  m the row's mean, r = 1 / sqrt(mean((x - m)^2) + eps).
+ *   x_dev        of x_type, consecutive values of a row next to each other, rows row_stride elements apart (0: all the same row)
+ *   weight_dev, bias_dev  [width] float32, or NULL: ones, zeros
+ *   y_dev        [rows, width] of y_type: x_type, or NNA_BF16 / NNA_F16 where x_type is NNA_F32.  May be x_dev where the types and strides are equal.
+ *   stats_dev    NULL, or [rows, 2] float32 for the backward call: m and r
+ *   codes_dev, scales_dev  both NULL, or x in 8 bits for the backward call (y_type = x_type): as nna_pack8 writes it
+ * nna_layer_norm_frames normalises the frames of the library's own outputs: x_dev[B, width, T] float32, T fastest (width 1..2112);
+ *   y_dev[B, T, width]: the frames as a network's tokens, turned on the way.
+ * Zero rows are no error.  Errors: NNA_ERR_INVALID_ARG (NULL, types, eps negative or NaN), NNA_ERR_UNSUPPORTED (a width above the limit),
+ * NNA_ERR_SHAPE.  A value that is not finite makes its own row's outputs NaN and no other row's.
+ */
+nna_status nna_layer_norm(const void* x_dev, nna_dtype x_type, long long rows, long long width, long long row_stride, const float* weight_dev,
+                          const float* bias_dev, double eps, void* y_dev, nna_dtype y_type, float* stats_dev, signed char* codes_dev,
+                          float* scales_dev, int device, void* hip_stream);
+nna_status nna_layer_norm_frames(const float* x_dev, long long B, long long width, long long T, const float* weight_dev, const float* bias_dev,
+                                 double eps, void* y_dev, nna_dtype y_type, float* stats_dev, int device, void* hip_stream);
+/*
+ * Gradients of a layer norm, from gout_dev[rows, width] ([B, T, width]) = dLoss/dy of y's type:
+ *   gx = r (g - mean(g) - h mean(g h)), g = gout w;   gw = sum over rows of gout h;   gb = sum over rows of gout.
+ * x comes as it went into the forward call, or as the codes and scales that call wrote (x_dev NULL); stats_dev from that call.
+ *   gx_dev       [rows, width] of x_type ([B, width, T] float32 for frames), or NULL; not x_dev
+ *   gw_dev, gb_dev  [width] float32, or NULL
+ *   workspace_dev  16-byte aligned, nna_layer_norm_backward_workspace bytes (for frames with B and T; rows B = 0); not read where gw_dev and gb_dev are NULL.
+ * The sums over rows are taken in an order that depends on the shape alone: the same inputs give the same bits.
+ */
+nna_status nna_layer_norm_backward_workspace(long long rows, long long width, long long B, long long T, size_t* bytes);
+nna_status nna_layer_norm_backward(const void* gout_dev, nna_dtype gout_type, const void* x_dev, nna_dtype x_type, long long rows, long long width,
+                                   long long row_stride, const signed char* codes_dev, const float* scales_dev, const float* stats_dev,
+                                   const float* weight_dev, void* gx_dev, float* gw_dev, float* gb_dev, void* workspace_dev,
+                                   size_t workspace_bytes, int device, void* hip_stream);
+nna_status nna_layer_norm_frames_backward(const void* gout_dev, nna_dtype gout_type, const float* x_dev, long long B, long long width, long long T,
+                                          const float* stats_dev, const float* weight_dev, float* gx_dev, float* gw_dev, float* gb_dev,
+                                          void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream);
+
+/*
+ * Values kept in 8 bits, e.g. from a forward pass to its backward pass: 1 + 1/32 bytes a value in place of 2 or 4.  Blocks of
+ * NNA_BLOCK8 neighbours of a row (the last of a row may be shorter) share a scale: with a = the block's largest magnitude,
+ *   scale = a fl(1/127),  code = rint(x (127 / a)),  and a code stands for code * scale, all in float32: off by at most a / 254 and four roundings of a.
+ * A block with a < 2^-100 is zero (scale 0).  A block with a value that is not finite stands for NaN throughout (scale NaN, codes 0).
+ *   x_dev        [rows, width] of any nna_dtype, rows row_stride elements apart;  out_dev [rows, width], contiguous
+ *   codes_dev    [rows, width];  scales_dev [rows, ceil(width / NNA_BLOCK8)]
+ */
+#define NNA_BLOCK8 128
+nna_status nna_pack8(const void* x_dev, nna_dtype type, long long rows, long long width, long long row_stride, signed char* codes_dev,
+                     float* scales_dev, int device, void* hip_stream);
+nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, long long rows, long long width, void* out_dev, nna_dtype type,
+                       int device, void* hip_stream);
+
 void nna_plan_destroy(nna_plan* plan); /* NULL is allowed */
 
 const char* nna_status_str(nna_status s);

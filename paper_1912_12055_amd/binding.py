@@ -38,6 +38,8 @@ EXPORTS = [
     "nna_plan_destroy",
     "nna_status_str", "nna_last_error",
     "nna_cqt_workspace", "nna_cqt_in_workspace",
+    "nna_layer_norm", "nna_layer_norm_frames", "nna_layer_norm_backward_workspace", "nna_layer_norm_backward",
+    "nna_layer_norm_frames_backward", "nna_pack8", "nna_unpack8",
 ]
 
 _c = ctypes
@@ -114,6 +116,14 @@ def lib():
             getattr(L, name + "_backward_workspace").argtypes = [_VP, _LL, _LL, _c.POINTER(_c.c_size_t)]
             getattr(L, name + "_backward").argtypes = [_VP, _VP, _LL, _LL, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _VP]
         L.nna_mel_with_stft.argtypes = [_VP, _VP, _LL, _LL, _VP, _VP, _VP]
+        _I, _D = _c.c_int, _c.c_double
+        L.nna_layer_norm.argtypes = [_VP, _I, _LL, _LL, _LL, _VP, _VP, _D, _VP, _I, _VP, _VP, _VP, _I, _VP]
+        L.nna_layer_norm_frames.argtypes = [_VP, _LL, _LL, _LL, _VP, _VP, _D, _VP, _I, _VP, _I, _VP]
+        L.nna_layer_norm_backward_workspace.argtypes = [_LL, _LL, _LL, _LL, _c.POINTER(_c.c_size_t)]
+        L.nna_layer_norm_backward.argtypes = [_VP, _I, _VP, _I, _LL, _LL, _LL, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
+        L.nna_layer_norm_frames_backward.argtypes = [_VP, _I, _VP, _LL, _LL, _LL, _VP, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
+        L.nna_pack8.argtypes = [_VP, _I, _LL, _LL, _LL, _VP, _VP, _I, _VP]
+        L.nna_unpack8.argtypes = [_VP, _VP, _LL, _LL, _VP, _I, _I, _VP]
         L.nna_out_shape.argtypes = [_VP, _LL, _LL, _c.POINTER(_LL), _c.POINTER(_LL)]
         for name in ("nna_stft", "nna_mel", "nna_cqt", "nna_cqt1992", "nna_cqt2010v2_static"):
             getattr(L, name).argtypes = [_VP, _VP, _LL, _LL, _VP, _VP]
@@ -798,3 +808,197 @@ def nna_backward_kept(plan: Plan, x, gout, kept, want_gmelw=False, want_gw=True,
                                    gm.data_ptr() if want_gmelw else None, gw.data_ptr() if want_gw else None,
                                    gx.data_ptr() if want_gx else None, workspace.data_ptr(), need, _stream_of(x, stream)))
     return gm, gw, gx
+
+
+# ---- operators of networks on the transforms' frames ------------------------------------------------------------------
+NNA_F32, NNA_BF16, NNA_F16 = 0, 1, 2
+NNA_BLOCK8 = 128
+_types = {}
+
+
+def _type_of(t, name, allowed=("float32", "bfloat16", "float16")):
+    """The nna_dtype of a CUDA tensor, which is refused if it is none or of a type not `allowed`."""
+    import torch
+
+    if not _types:
+        _types.update({torch.float32: (NNA_F32, "float32"), torch.bfloat16: (NNA_BF16, "bfloat16"), torch.float16: (NNA_F16, "float16")})
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError(f"{name} must be a CUDA tensor")
+    known = _types.get(t.dtype)
+    if known is None or known[1] not in allowed:
+        raise TypeError(f"{name} must be of {' or '.join(allowed)}, not {t.dtype}")
+    return known[0]
+
+
+def _vector(t, name, shape, device, none=False):
+    """The pointer of a contiguous float32 tensor of `shape` on `device` (None where that is allowed)."""
+    import torch
+
+    if t is None and none:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == tuple(shape) and t.device == device):
+        raise TypeError(f"{name} must be a contiguous float32 tensor of shape {tuple(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _row_stride(x):
+    """Elements between the rows of x[..., width] if its rows are at one distance from each other, or None."""
+    shape, strides = x.shape, x.stride()
+    if not x.numel():
+        return shape[-1]
+    if shape[-1] != 1 and strides[-1] != 1:
+        return None
+    step = far = None
+    for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if n == 1:
+            continue
+        if step is None:
+            step, far = s, s * n
+        elif s != far:
+            return None
+        else:
+            far = s * n
+    return shape[-1] if step is None else step
+
+
+def _workspace_on(stream, need, workspace, device):
+    import torch
+
+    if workspace is None:
+        workspace = _memory_on(stream, need, device)
+        if workspace is None:
+            raise ValueError("torch has no allocator for this stream, or knows nothing of its capture: pass `workspace`")
+    elif not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous() and workspace.device == device):
+        raise TypeError("workspace must be a contiguous CUDA tensor on the inputs' device")
+    return workspace
+
+
+class NormKept:
+    """What nna_layer_norm keeps for nna_layer_norm_backward: every row's mean and 1 / sqrt(variance + eps) (`stats`), and the input
+    itself (`x`) or its 8 bits (`codes`, `scales`)."""
+
+    __slots__ = ("shape", "dtype", "out_dtype", "rows", "row_stride", "x", "stats", "codes", "scales")
+
+    def tensors(self):
+        return tuple(t for t in (self.x, self.stats, self.codes, self.scales) if t is not None)
+
+
+def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, out=None, stream=None):
+    """Layer norm over the last axis of x[..., width]: (x - mean) / sqrt(variance + eps) * weight + bias, contiguous, of x's type (float32 input:
+    also of `out_dtype` bfloat16 or float16).  x's rows lie at one distance from each other, or x is frames as the transforms write
+    them, ``spec.transpose(1, 2)`` of a contiguous float32 spec[B, bins, T].  weight, bias: float32 [width].
+    keep: 0, or what is kept for nna_layer_norm_backward, returned behind y as a NormKept: 32 the input as it is, 8 the input in 8 bits
+    (nna_pack8's; rows only, y of x's type)."""
+    import torch
+
+    xt = _type_of(x, "x")
+    if x.dim() < 1:
+        raise TypeError("x must have an axis to normalise")
+    if keep not in (0, 8, 32):
+        raise ValueError("keep: 0, 8 or 32")
+    shape, width, device = x.shape, x.shape[-1], x.device
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=device)
+    elif not (isinstance(out, torch.Tensor) and out.device == device and out.dtype == out_dtype and out.is_contiguous() and out.shape == shape):
+        raise TypeError(f"out must be a contiguous {out_dtype} CUDA tensor of shape {tuple(shape)}")
+    yt = _type_of(out, "out")
+    w, b = _vector(weight, "weight", (width,), device, none=True), _vector(bias, "bias", (width,), device, none=True)
+    rows = x.numel() // width if width else 0
+    step = _row_stride(x)
+    kept = stats = codes = scales = None
+    if keep:
+        stats = torch.empty((rows, 2), dtype=torch.float32, device=device)
+        if keep == 8:
+            codes = torch.empty((rows, width), dtype=torch.int8, device=device)
+            scales = torch.empty((rows, -(-width // NNA_BLOCK8)), dtype=torch.float32, device=device)
+        kept = NormKept()
+        kept.shape, kept.dtype, kept.out_dtype, kept.rows, kept.row_stride = shape, x.dtype, out_dtype, rows, step
+        kept.x, kept.stats, kept.codes, kept.scales = x if keep == 32 else None, stats, codes, scales
+    sp, st = stats.data_ptr() if keep else None, _stream_of(x, stream)
+    if step is not None:
+        _check(lib().nna_layer_norm(x.data_ptr(), xt, rows, width, step, w, b, eps, out.data_ptr(), yt, sp,
+                                    codes.data_ptr() if keep == 8 else None, scales.data_ptr() if keep == 8 else None, device.index, st))
+    elif x.dim() == 3 and xt == NNA_F32 and x.transpose(1, 2).is_contiguous():
+        if keep == 8:
+            raise TypeError("keep=8: x must be rows (consecutive values next to each other)")
+        _check(lib().nna_layer_norm_frames(x.data_ptr(), shape[0], width, shape[1], w, b, eps, out.data_ptr(), yt, sp, device.index, st))
+    else:
+        raise TypeError("x must be rows at one distance from each other, or the transpose of a contiguous float32 [B, bins, T]")
+    return (out, kept) if keep else out
+
+
+def nna_layer_norm_backward(gout, kept, weight=None, want_gx=True, want_gw=True, workspace=None, stream=None):
+    """(gx, gweight, gbias), None where not wanted: the gradients of a loss through nna_layer_norm(x, weight, bias, keep=...), given gout =
+    dLoss/dy of y's shape and type and what that call kept.  gx is of x's type, laid out as x was read (rows contiguous).
+    `workspace`: a CUDA tensor of nna_layer_norm_backward_workspace bytes (taken here if None)."""
+    import torch
+
+    gt = _type_of(gout, "gout")
+    if gout.dtype != kept.out_dtype or gout.shape != kept.shape or not gout.is_contiguous() or gout.device != kept.stats.device:
+        raise TypeError(f"gout must be a contiguous {kept.out_dtype} CUDA tensor of shape {tuple(kept.shape)}")
+    shape, width, device, rows = kept.shape, kept.shape[-1], gout.device, kept.rows
+    w = _vector(weight, "weight", (width,), device, none=True)
+    frames = kept.row_stride is None
+    B, T = (shape[0], shape[1]) if frames else (0, 0)
+    gx = gw = gb = None
+    if want_gx:
+        gx = torch.empty((B, width, T), dtype=kept.dtype, device=device).transpose(1, 2) if frames else torch.empty(shape, dtype=kept.dtype, device=device)
+    need = 0
+    if want_gw:
+        gw, gb = torch.empty((2, width), dtype=torch.float32, device=device).unbind(0)
+        need = nna_layer_norm_backward_workspace(rows, width, B, T)
+        workspace = _workspace_on(stream, need, workspace, device)
+    ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if want_gw else (None, 0)
+    grads = (gx.data_ptr() if want_gx else None, gw.data_ptr() if want_gw else None, gb.data_ptr() if want_gw else None)
+    sp, st = kept.stats.data_ptr(), _stream_of(gout, stream)
+    if frames:
+        _check(lib().nna_layer_norm_frames_backward(gout.data_ptr(), gt, kept.x.data_ptr(), B, width, T, sp, w, *grads, *ws, device.index, st))
+    else:
+        xt = {torch.float32: NNA_F32, torch.bfloat16: NNA_BF16, torch.float16: NNA_F16}[kept.dtype]
+        codes, scales = kept.codes, kept.scales
+        _check(lib().nna_layer_norm_backward(gout.data_ptr(), gt, None if kept.x is None else kept.x.data_ptr(), xt, rows, width, kept.row_stride,
+                                             None if codes is None else codes.data_ptr(), None if scales is None else scales.data_ptr(), sp, w,
+                                             *grads, *ws, device.index, st))
+    return gx, gw, gb
+
+
+def nna_layer_norm_backward_workspace(rows: int, width: int, B: int = 0, T: int = 0) -> int:
+    """Bytes for `rows` rows, or for the frames of [B, width, T] (rows = B T)."""
+    n = _c.c_size_t()
+    _check(lib().nna_layer_norm_backward_workspace(rows, width, B, T, _c.byref(n)))
+    return n.value
+
+
+def nna_pack8(x, stream=None):
+    """(codes int8 [..., width], scales float32 [..., ceil(width / 128)]): x[..., width] in 8 bits, 128 neighbours to a scale."""
+    import torch
+
+    xt = _type_of(x, "x")
+    step = _row_stride(x) if x.dim() else None
+    if step is None:
+        raise TypeError("x must be rows at one distance from each other")
+    width = x.shape[-1]
+    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scales = torch.empty((*x.shape[:-1], -(-width // NNA_BLOCK8)), dtype=torch.float32, device=x.device)
+    _check(lib().nna_pack8(x.data_ptr(), xt, x.numel() // width if width else 0, width, step, codes.data_ptr(), scales.data_ptr(), x.device.index,
+                           _stream_of(x, stream)))
+    return codes, scales
+
+
+def nna_unpack8(codes, scales, dtype=None, out=None, stream=None):
+    """The values that nna_pack8's codes stand for, codes * scales, in `dtype` (float32 if None), contiguous."""
+    import torch
+
+    if not (isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dtype == torch.int8 and codes.is_contiguous() and codes.dim()):
+        raise TypeError("codes must be a contiguous int8 CUDA tensor")
+    width = codes.shape[-1]
+    sp = _vector(scales, "scales", (*codes.shape[:-1], -(-width // NNA_BLOCK8)), codes.device)
+    if out is None:
+        out = torch.empty(codes.shape, dtype=torch.float32 if dtype is None else dtype, device=codes.device)
+    elif not (out.is_contiguous() and out.shape == codes.shape and out.device == codes.device and dtype in (None, out.dtype)):
+        raise TypeError(f"out must be a contiguous CUDA tensor of shape {tuple(codes.shape)}")
+    ot = _type_of(out, "out")
+    _check(lib().nna_unpack8(codes.data_ptr(), sp, codes.numel() // width if width else 0, width, out.data_ptr(), ot, codes.device.index,
+                             _stream_of(codes, stream)))
+    return out

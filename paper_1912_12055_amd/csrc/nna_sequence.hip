@@ -1,0 +1,198 @@
+// The operators of networks on top of the transforms (C ABI): argument checks, shapes, launches.
+#include "nna_host.h"
+#include "nna_norm.h"
+
+using namespace nna;
+using namespace nna::host;
+
+namespace {
+
+// enters the device for a call without a plan, its kernels set up
+nna_status enter_device(DeviceGuard& guard, int device) {
+  if (device < 0) return fail(NNA_ERR_INVALID_ARG, "device must be the HIP device of the arrays");
+  nna_status s = check_device(device);
+  if (s != NNA_OK) return s;
+  hipError_t e = guard.enter(device);
+  if (e != hipSuccess) return fail_hip(e, "hipSetDevice");
+  e = ensure_kernels_init(device);
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "kernel set-up");
+}
+
+bool known_type(int t) { return t == NNA_F32 || t == NNA_BF16 || t == NNA_F16; }
+
+// rows (B x T frames) of `width` values
+nna_status check_rows(long long rows, long long width, long long width_max) {
+  if (rows < 0 || width < 1) return fail(NNA_ERR_SHAPE, "rows must not be negative, and width at least 1");
+  if (width > width_max) return fail(NNA_ERR_UNSUPPORTED, "width " + std::to_string(width) + " is above " + std::to_string(width_max));
+  if (rows > (1LL << 60) / width) return fail(NNA_ERR_SHAPE, "too many values");
+  return NNA_OK;
+}
+
+nna_status check_frames(long long B, long long width, long long T) {
+  if (B < 0 || T < 0) return fail(NNA_ERR_SHAPE, "B and T must not be negative");
+  if (T && B > INT_MAX / ((T + 7) / 8)) return fail(NNA_ERR_SHAPE, "B T is too large");
+  return check_rows(B * T, width, NORM_FRAMES_WIDTH_MAX);
+}
+
+nna_status check_norm_types(int x_type, int y_type) {
+  if (!known_type(x_type) || !known_type(y_type)) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
+  if (x_type != y_type && x_type != NNA_F32) return fail(NNA_ERR_INVALID_ARG, "the outputs' type must be the inputs', or narrower than float32");
+  return NNA_OK;
+}
+
+size_t norm_workspace(long long rows, int width, bool frames, long long B, long long T) {
+  return (size_t)norm_backward_groups(rows, width, frames, B, T) * 2 * width * sizeof(float);
+}
+
+nna_status run_norm(NormParams& P, int x_type, int y_type, double eps, bool frames, int device, void* stream) {
+  if (!(eps >= 0.0) || eps > 3.0e38) return fail(NNA_ERR_INVALID_ARG, "eps must be finite and not negative");
+  if (P.rows && (!P.x || !P.y)) return fail(NNA_ERR_INVALID_ARG, "x_dev / y_dev is NULL");
+  if (P.rows && !P.codes != !P.scales) return fail(NNA_ERR_INVALID_ARG, "codes_dev and scales_dev come together");
+  if (P.codes && x_type != y_type) return fail(NNA_ERR_UNSUPPORTED, "8-bit codes need outputs of the inputs' type");
+  P.eps = (float)eps;
+  DeviceGuard guard;
+  nna_status s = enter_device(guard, device);
+  if (s != NNA_OK || !P.rows) return s;
+  const hipError_t e = launch_norm(P, x_type, y_type, frames, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "layer norm");
+}
+
+nna_status run_norm_backward(NormParams& P, int x_type, int g_type, bool frames, float* gw, float* gb, void* workspace, size_t bytes, int device, void* stream) {
+  if (!P.gx && !gw && !gb) return fail(NNA_ERR_INVALID_ARG, "no gradient is asked for");
+  if (P.rows && (!P.gout || !P.stats)) return fail(NNA_ERR_INVALID_ARG, "gout_dev / stats_dev is NULL");
+  if (P.rows && !P.codes != !P.scales) return fail(NNA_ERR_INVALID_ARG, "codes_dev and scales_dev come together");
+  if (P.rows && !P.x == !P.codes) return fail(NNA_ERR_INVALID_ARG, "either x_dev or its codes");
+  if (P.rows && P.gx && P.gx == P.x) return fail(NNA_ERR_INVALID_ARG, "gx_dev must not be x_dev");
+  if (P.codes && x_type != g_type) return fail(NNA_ERR_UNSUPPORTED, "8-bit codes need outputs of the inputs' type");
+  if (gw || gb) {
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15) || bytes < norm_workspace(P.rows, P.width, frames, P.batch, P.T))
+      return fail(NNA_ERR_INVALID_ARG, "workspace_dev is NULL, misaligned or smaller than nna_layer_norm_backward_workspace asks for");
+    P.partial = static_cast<float*>(workspace);
+  }
+  DeviceGuard guard;
+  nna_status s = enter_device(guard, device);
+  if (s != NNA_OK || (!P.rows && !P.partial)) return s;
+  const hipError_t e = launch_norm_backward(P, x_type, g_type, frames, gw, gb, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "layer norm, backward");
+}
+
+nna_status check_pack(int type, long long rows, long long width) {
+  if (!known_type(type)) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
+  return check_rows(rows, width, 1LL << 60);
+}
+
+}  // namespace
+
+extern "C" {
+
+nna_status nna_layer_norm(const void* x_dev, nna_dtype x_type, long long rows, long long width, long long row_stride, const float* weight_dev,
+                          const float* bias_dev, double eps, void* y_dev, nna_dtype y_type, float* stats_dev, signed char* codes_dev,
+                          float* scales_dev, int device, void* hip_stream) {
+  nna_status s = check_norm_types(x_type, y_type);
+  if (s == NNA_OK) s = check_rows(rows, width, NORM_WIDTH_MAX);
+  if (s != NNA_OK) return s;
+  NormParams P = {};
+  P.x = x_dev;
+  P.rows = rows;
+  P.row_stride = row_stride;
+  P.width = (int)width;
+  P.weight = weight_dev;
+  P.bias = bias_dev;
+  P.y = y_dev;
+  P.stats = stats_dev;
+  P.codes = codes_dev;
+  P.scales = scales_dev;
+  return run_norm(P, x_type, y_type, eps, false, device, hip_stream);
+}
+
+nna_status nna_layer_norm_frames(const float* x_dev, long long B, long long width, long long T, const float* weight_dev, const float* bias_dev,
+                                 double eps, void* y_dev, nna_dtype y_type, float* stats_dev, int device, void* hip_stream) {
+  nna_status s = check_norm_types(NNA_F32, y_type);
+  if (s == NNA_OK) s = check_frames(B, width, T);
+  if (s != NNA_OK) return s;
+  NormParams P = {};
+  P.x = x_dev;
+  P.rows = B * T;
+  P.batch = B;
+  P.T = T;
+  P.width = (int)width;
+  P.weight = weight_dev;
+  P.bias = bias_dev;
+  P.y = y_dev;
+  P.stats = stats_dev;
+  return run_norm(P, NNA_F32, y_type, eps, true, device, hip_stream);
+}
+
+nna_status nna_layer_norm_backward_workspace(long long rows, long long width, long long B, long long T, size_t* bytes) {
+  if (!bytes) return fail(NNA_ERR_INVALID_ARG, "bytes is NULL");
+  nna_status s = B ? check_frames(B, width, T) : check_rows(rows, width, NORM_WIDTH_MAX);
+  if (s != NNA_OK) return s;
+  *bytes = norm_workspace(rows, (int)width, B != 0, B, T);
+  return NNA_OK;
+}
+
+nna_status nna_layer_norm_backward(const void* gout_dev, nna_dtype gout_type, const void* x_dev, nna_dtype x_type, long long rows, long long width,
+                                   long long row_stride, const signed char* codes_dev, const float* scales_dev, const float* stats_dev,
+                                   const float* weight_dev, void* gx_dev, float* gw_dev, float* gb_dev, void* workspace_dev,
+                                   size_t workspace_bytes, int device, void* hip_stream) {
+  nna_status s = check_norm_types(x_type, gout_type);
+  if (s == NNA_OK) s = check_rows(rows, width, NORM_WIDTH_MAX);
+  if (s != NNA_OK) return s;
+  NormParams P = {};
+  P.x = x_dev;
+  P.gout = gout_dev;
+  P.rows = rows;
+  P.row_stride = row_stride;
+  P.width = (int)width;
+  P.weight = weight_dev;
+  P.gx = gx_dev;
+  P.stats = const_cast<float*>(stats_dev);
+  P.codes = const_cast<signed char*>(codes_dev);
+  P.scales = const_cast<float*>(scales_dev);
+  return run_norm_backward(P, x_type, gout_type, false, gw_dev, gb_dev, workspace_dev, workspace_bytes, device, hip_stream);
+}
+
+nna_status nna_layer_norm_frames_backward(const void* gout_dev, nna_dtype gout_type, const float* x_dev, long long B, long long width, long long T,
+                                          const float* stats_dev, const float* weight_dev, float* gx_dev, float* gw_dev, float* gb_dev,
+                                          void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream) {
+  nna_status s = check_norm_types(NNA_F32, gout_type);
+  if (s == NNA_OK) s = check_frames(B, width, T);
+  if (s != NNA_OK) return s;
+  NormParams P = {};
+  P.x = x_dev;
+  P.gout = gout_dev;
+  P.rows = B * T;
+  P.batch = B;
+  P.T = T;
+  P.width = (int)width;
+  P.weight = weight_dev;
+  P.gx = gx_dev;
+  P.stats = const_cast<float*>(stats_dev);
+  return run_norm_backward(P, NNA_F32, gout_type, true, gw_dev, gb_dev, workspace_dev, workspace_bytes, device, hip_stream);
+}
+
+nna_status nna_pack8(const void* x_dev, nna_dtype type, long long rows, long long width, long long row_stride, signed char* codes_dev,
+                     float* scales_dev, int device, void* hip_stream) {
+  nna_status s = check_pack(type, rows, width);
+  if (s != NNA_OK) return s;
+  if (rows && (!x_dev || !codes_dev || !scales_dev)) return fail(NNA_ERR_INVALID_ARG, "x_dev / codes_dev / scales_dev is NULL");
+  DeviceGuard guard;
+  s = enter_device(guard, device);
+  if (s != NNA_OK || !rows) return s;
+  const hipError_t e = launch_pack8(x_dev, type, rows, width, row_stride, codes_dev, scales_dev, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_pack8");
+}
+
+nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, long long rows, long long width, void* out_dev, nna_dtype type,
+                       int device, void* hip_stream) {
+  nna_status s = check_pack(type, rows, width);
+  if (s != NNA_OK) return s;
+  if (rows && (!out_dev || !codes_dev || !scales_dev)) return fail(NNA_ERR_INVALID_ARG, "out_dev / codes_dev / scales_dev is NULL");
+  DeviceGuard guard;
+  s = enter_device(guard, device);
+  if (s != NNA_OK || !rows) return s;
+  const hipError_t e = launch_unpack8(codes_dev, scales_dev, rows, width, out_dev, type, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_unpack8");
+}
+
+}  // extern "C"
