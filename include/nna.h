@@ -622,6 +622,44 @@ nna_status nna_pack8(const void* x_dev, nna_dtype type, long long rows, long lon
 nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, long long rows, long long width, void* out_dev, nna_dtype type,
                        int device, void* hip_stream);
 
+/*
+ * Linear attention with a decay l for each head (the state of a head is a matrix S[dk, dv]):
+ *   S_t = l S_{t-1} + k_t^T v_t,   o_t = scale q_t S_t = scale (sum_{s <= t} l^(t-s) (q_t . k_s) v_s + l^(t+1) q_t S_first).
+ * nna_decay_attention takes whole sequences, nna_decay_attention_step one new frame of each.
+ *   q_dev, k_dev [B, T, H, dk], v_dev [B, T, H, dv]   of `type`, NNA_F32 or NNA_BF16 (float16 has no range for the weights l^(t-s) q . k); a head's
+ *                values next to each other, strides[3] = elements between batches, frames, heads (0 where they are shared).  dk, dv 1..128
+ *   decay_dev    [H] float32, in [0, 1]: a constant of the head (no gradient is taken)
+ *   scale        finite, not 0
+ *   lengths_dev  [B] int32 in device memory, or NULL: T.  Frames from a sequence's length on (below 0: 0, above T: T) take no part: their values are not
+ *                used, their outputs and gradients are 0, and the last state is that after the length
+ *   first_dev, last_dev  [B, H, dk, dv] float32 or NULL: the state before the first frame (NULL: 0), and after the last.  They may be the same
+ *   out_dev      [B, T, H, dv] of `type`, contiguous
+ *   workspace_dev  256-byte aligned, nna_decay_attention_workspace bytes (0: may be NULL)
+ * States are float32, and sums of products of inputs are exact to float32; for NNA_BF16 the weights l^(t-s) (q . k) and the state are rounded to
+ * bfloat16 where they are multiplied with v and q (an error like that of the rounded output).  A value of v that is not finite makes the
+ * outputs of its head NaN from its frame on, and the last state; one of k likewise by the rules of arithmetic; one of q its own frame's.
+ *
+ * nna_decay_attention_backward: given gout_dev [B, T, H, dv] (contiguous) and glast_dev (or NULL: 0), the gradients of a loss with respect to out and
+ * the last state: gq_dev, gk_dev [B, T, H, dk], gv_dev [B, T, H, dv] (each or NULL; contiguous, of `type`) and gfirst_dev [B, H, dk, dv] (or NULL; with gk_dev
+ * or gv_dev).  The same inputs give the same bits.
+ * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_UNSUPPORTED (type, dk or dv above 128), NNA_ERR_SHAPE.  T = 0 or B = 0 is no error.
+ */
+nna_status nna_decay_attention_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes);
+nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, const void* k_dev, const long long* k_strides, const void* v_dev,
+                               const long long* v_strides, nna_dtype type, long long B, long long T, long long H, long long dk, long long dv,
+                               const float* decay_dev, double scale, const int* lengths_dev, const float* first_dev, float* last_dev,
+                               void* out_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream);
+nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev, const long long* q_strides, const void* k_dev,
+                                        const long long* k_strides, const void* v_dev, const long long* v_strides, nna_dtype type, long long B,
+                                        long long T, long long H, long long dk, long long dv, const float* decay_dev, double scale,
+                                        const int* lengths_dev, const float* first_dev, const float* glast_dev, void* gq_dev, void* gk_dev,
+                                        void* gv_dev, float* gfirst_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream);
+/* One new frame of B sequences: q_dev, k_dev [B, H, dk], v_dev [B, H, dv] (strides[2]: batches, heads), state_dev [B, H, dk, dv] updated in place,
+ * out_dev [B, H, dv] of `type`, contiguous: scale q S with the updated S. */
+nna_status nna_decay_attention_step(const void* q_dev, const long long* q_strides, const void* k_dev, const long long* k_strides, const void* v_dev,
+                                    const long long* v_strides, nna_dtype type, long long B, long long H, long long dk, long long dv,
+                                    const float* decay_dev, double scale, float* state_dev, void* out_dev, int device, void* hip_stream);
+
 void nna_plan_destroy(nna_plan* plan); /* NULL is allowed */
 
 const char* nna_status_str(nna_status s);

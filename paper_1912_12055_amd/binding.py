@@ -40,6 +40,7 @@ EXPORTS = [
     "nna_cqt_workspace", "nna_cqt_in_workspace",
     "nna_layer_norm", "nna_layer_norm_frames", "nna_layer_norm_backward_workspace", "nna_layer_norm_backward",
     "nna_layer_norm_frames_backward", "nna_pack8", "nna_unpack8",
+    "nna_decay_attention_workspace", "nna_decay_attention", "nna_decay_attention_backward", "nna_decay_attention_step",
 ]
 
 _c = ctypes
@@ -124,6 +125,11 @@ def lib():
         L.nna_layer_norm_frames_backward.argtypes = [_VP, _I, _VP, _LL, _LL, _LL, _VP, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
         L.nna_pack8.argtypes = [_VP, _I, _LL, _LL, _LL, _VP, _VP, _I, _VP]
         L.nna_unpack8.argtypes = [_VP, _VP, _LL, _LL, _VP, _I, _I, _VP]
+        qkv, shape = 3 * [_VP, _c.POINTER(_LL)], 5 * [_LL]
+        L.nna_decay_attention_workspace.argtypes = [*shape, _c.POINTER(_c.c_size_t)]
+        L.nna_decay_attention.argtypes = [*qkv, _I, *shape, _VP, _D, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
+        L.nna_decay_attention_backward.argtypes = [_VP, *qkv, _I, *shape, _VP, _D, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
+        L.nna_decay_attention_step.argtypes = [*qkv, _I, _LL, _LL, _LL, _LL, _VP, _D, _VP, _VP, _I, _VP]
         L.nna_out_shape.argtypes = [_VP, _LL, _LL, _c.POINTER(_LL), _c.POINTER(_LL)]
         for name in ("nna_stft", "nna_mel", "nna_cqt", "nna_cqt1992", "nna_cqt2010v2_static"):
             getattr(L, name).argtypes = [_VP, _VP, _LL, _LL, _VP, _VP]
@@ -1001,4 +1007,104 @@ def nna_unpack8(codes, scales, dtype=None, out=None, stream=None):
     ot = _type_of(out, "out")
     _check(lib().nna_unpack8(codes.data_ptr(), sp, codes.numel() // width if width else 0, width, out.data_ptr(), ot, codes.device.index,
                              _stream_of(codes, stream)))
+    return out
+
+
+def _heads(q, k, v, axes):
+    """(nna_dtype, sizes, the arguments q, k, v stand for) of [B, (T,) H, d] tensors; their strides but for the last are their own."""
+    t = _type_of(q, "q", ("float32", "bfloat16"))
+    for name, x in (("k", k), ("v", v)):
+        if _type_of(x, name, ("float32", "bfloat16")) != t or x.device != q.device:
+            raise TypeError("q, k and v must be of one type, on one device")
+    if q.dim() != axes or k.shape != q.shape or v.dim() != axes or v.shape[:-1] != q.shape[:-1]:
+        raise TypeError("q and k must be " + ("[B, T, H, dk] and v [B, T, H, dv]" if axes == 4 else "[B, H, dk] and v [B, H, dv]"))
+    args = []
+    for x in (q, k, v):
+        s = x.stride()
+        if x.shape[-1] != 1 and s[-1] != 1:
+            raise TypeError("a head's values must lie next to each other")
+        args += [x.data_ptr(), (_LL * (axes - 1))(*s[:-1])]
+    return t, (*q.shape, v.shape[-1]), args
+
+
+def _lengths(lengths, B, device):
+    import torch
+
+    if lengths is None:
+        return None
+    if not (isinstance(lengths, torch.Tensor) and lengths.dtype == torch.int32 and lengths.is_contiguous() and tuple(lengths.shape) == (B,) and lengths.device == device):
+        raise TypeError(f"lengths must be a contiguous int32 tensor of shape {(B,)} on {device}")
+    return lengths.data_ptr()
+
+
+def nna_decay_attention_workspace(B: int, T: int, H: int, dk: int, dv: int) -> int:
+    """Bytes that nna_decay_attention and its backward call need; 0 where there are sequences and heads enough to fill the card."""
+    n = _c.c_size_t()
+    _check(lib().nna_decay_attention_workspace(B, T, H, dk, dv, _c.byref(n)))
+    return n.value
+
+
+def nna_decay_attention(q, k, v, decay, scale=None, state=None, lengths=None, want_state=False, out=None, workspace=None, stream=None):
+    """o[B, T, H, dv] of linear attention with a decay for each head, S_t = decay S_{t-1} + k_t^T v_t, o_t = scale q_t S_t; with `want_state`
+    (o, S after the last frame [B, H, dk, dv]).  q, k [B, T, H, dk], v [B, T, H, dv]: float32 or bfloat16, any strides but the last.  decay: float32 [H], in
+    [0, 1].  scale: dk**-0.5 if None.  state: float32 [B, H, dk, dv] before the first frame (None: zero).  lengths: int32 [B] on the GPU; frames
+    from there on take no part, and their outputs are zero.  `workspace`: nna_decay_attention_workspace bytes, 256-byte aligned (taken here if None)."""
+    import torch
+
+    t, (B, T, H, dk, dv), args = _heads(q, k, v, 4)
+    device = q.device
+    dp, sp, lp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device, none=True), _lengths(lengths, B, device)
+    if out is None:
+        out = torch.empty((B, T, H, dv), dtype=q.dtype, device=device)
+    elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == (B, T, H, dv) and out.device == device):
+        raise TypeError(f"out must be a contiguous {q.dtype} tensor of shape {(B, T, H, dv)}")
+    last = torch.empty((B, H, dk, dv), dtype=torch.float32, device=device) if want_state else None
+    need = nna_decay_attention_workspace(B, T, H, dk, dv)
+    ws = (None, 0)
+    if need:
+        workspace = _workspace_on(stream, need, workspace, device)
+        ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(lib().nna_decay_attention(*args, t, B, T, H, dk, dv, dp, dk**-0.5 if scale is None else scale, lp, sp, last.data_ptr() if want_state else None,
+                                     out.data_ptr(), *ws, device.index, _stream_of(q, stream)))
+    return (out, last) if want_state else out
+
+
+def nna_decay_attention_backward(gout, q, k, v, decay, scale=None, state=None, lengths=None, gstate=None, want_gstate=False, workspace=None, stream=None):
+    """(gq, gk, gv, gradient of the first state or None): the gradients of a loss through nna_decay_attention, given gout = dLoss/do (contiguous)
+    and gstate = dLoss/d(last state) (None: zero)."""
+    import torch
+
+    t, (B, T, H, dk, dv), args = _heads(q, k, v, 4)
+    device = q.device
+    dp, sp, lp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device, none=True), _lengths(lengths, B, device)
+    lastp = _vector(gstate, "gstate", (B, H, dk, dv), device, none=True)
+    if not (isinstance(gout, torch.Tensor) and gout.dtype == q.dtype and gout.is_contiguous() and tuple(gout.shape) == (B, T, H, dv) and gout.device == device):
+        raise TypeError(f"gout must be a contiguous {q.dtype} tensor of shape {(B, T, H, dv)}")
+    gq, gk = (torch.empty((B, T, H, dk), dtype=q.dtype, device=device) for _ in range(2))
+    gv = torch.empty((B, T, H, dv), dtype=q.dtype, device=device)
+    first = torch.empty((B, H, dk, dv), dtype=torch.float32, device=device) if want_gstate else None
+    need = nna_decay_attention_workspace(B, T, H, dk, dv)
+    ws = (None, 0)
+    if need:
+        workspace = _workspace_on(stream, need, workspace, device)
+        ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(lib().nna_decay_attention_backward(gout.data_ptr(), *args, t, B, T, H, dk, dv, dp, dk**-0.5 if scale is None else scale, lp, sp, lastp,
+                                              gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), first.data_ptr() if want_gstate else None, *ws,
+                                              device.index, _stream_of(q, stream)))
+    return gq, gk, gv, first
+
+
+def nna_decay_attention_step(q, k, v, decay, state, scale=None, out=None, stream=None):
+    """o[B, H, dv] of one new frame q, k [B, H, dk], v [B, H, dv] of each sequence; state float32 [B, H, dk, dv] is updated in place."""
+    import torch
+
+    t, (B, H, dk, dv), args = _heads(q, k, v, 3)
+    device = q.device
+    dp, sp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device)
+    if out is None:
+        out = torch.empty((B, H, dv), dtype=q.dtype, device=device)
+    elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == (B, H, dv) and out.device == device):
+        raise TypeError(f"out must be a contiguous {q.dtype} tensor of shape {(B, H, dv)}")
+    _check(lib().nna_decay_attention_step(*args, t, B, H, dk, dv, dp, dk**-0.5 if scale is None else scale, sp, out.data_ptr(), device.index,
+                                          _stream_of(q, stream)))
     return out

@@ -1,5 +1,6 @@
 // Running a plan: shape checks, launch parameters and the transform calls of the C ABI, the per-device
 // set-up, and the library's static workspace with the entry point that uses it.
+#include "nna_decay.h"
 #include "nna_host.h"
 #include "nna_norm.h"
 
@@ -30,6 +31,7 @@ hipError_t ensure_kernels_init(int device) {
     if (e == hipSuccess) e = nna::short_kernels_init();
     if (e == hipSuccess) e = nna::fft_kernels_init();
     if (e == hipSuccess) e = nna::norm_kernels_init();
+    if (e == hipSuccess) e = nna::decay_kernels_init();
     if (e != hipSuccess) return e;
     void* ptr = nullptr;
     e = hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch));

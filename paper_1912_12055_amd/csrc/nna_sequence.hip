@@ -1,4 +1,5 @@
 // The operators of networks on top of the transforms (C ABI): argument checks, shapes, launches.
+#include "nna_decay.h"
 #include "nna_host.h"
 #include "nna_norm.h"
 
@@ -79,6 +80,50 @@ nna_status run_norm_backward(NormParams& P, int x_type, int g_type, bool frames,
 nna_status check_pack(int type, long long rows, long long width) {
   if (!known_type(type)) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
   return check_rows(rows, width, 1LL << 60);
+}
+
+nna_status check_heads(int type, long long B, long long T, long long H, long long dk, long long dv) {
+  if (!known_type(type)) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
+  if (type == NNA_F16) return fail(NNA_ERR_UNSUPPORTED, "float16 has no range for the weights: float32 or bfloat16");
+  if (B < 0 || T < 0 || H < 1 || dk < 1 || dv < 1) return fail(NNA_ERR_SHAPE, "B and T must not be negative, H, dk and dv at least 1");
+  if (dk > DECAY_HEAD_MAX || dv > DECAY_HEAD_MAX) return fail(NNA_ERR_UNSUPPORTED, "heads of more than " + std::to_string(DECAY_HEAD_MAX) + " values");
+  // a workgroup for each (sequence, head), its segments and its blocks of 1,024 values of a state
+  if (H > (1LL << 24) || B > (1LL << 24) / H) return fail(NNA_ERR_SHAPE, "B H is too large");
+  if (T > (1LL << 36)) return fail(NNA_ERR_SHAPE, "T is too large");
+  return NNA_OK;
+}
+
+nna_status check_decay_args(const void* decay, double scale, const void* workspace, size_t bytes, size_t need) {
+  if (!decay) return fail(NNA_ERR_INVALID_ARG, "decay_dev is NULL");
+  if (!(scale != 0.0) || !(std::fabs(scale) < 1e30) || !(std::fabs(scale) > 1e-30)) return fail(NNA_ERR_INVALID_ARG, "scale must be finite and not 0");
+  if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || bytes < need))
+    return fail(NNA_ERR_INVALID_ARG, "workspace_dev is NULL, misaligned or smaller than nna_decay_attention_workspace asks for");
+  return NNA_OK;
+}
+
+// which array a mix reads in which place
+struct Heads {
+  const void* at;
+  long long strides[3];
+  int width;
+};
+Heads heads_of(const void* at, const long long* strides, long long width) { return {at, {strides[0], strides[1], strides[2]}, (int)width}; }
+
+void set_mix(DecayMix& P, const Heads& a, const Heads& b, const Heads& c) {
+  P.a = a.at;
+  P.a_b = a.strides[0];
+  P.a_t = a.strides[1];
+  P.a_h = a.strides[2];
+  P.b = b.at;
+  P.b_b = b.strides[0];
+  P.b_t = b.strides[1];
+  P.b_h = b.strides[2];
+  P.c = c.at;
+  P.c_b = c.strides[0];
+  P.c_t = c.strides[1];
+  P.c_h = c.strides[2];
+  P.da = a.width;
+  P.dc = c.width;
 }
 
 }  // namespace
@@ -193,6 +238,136 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
   if (s != NNA_OK || !rows) return s;
   const hipError_t e = launch_unpack8(codes_dev, scales_dev, rows, width, out_dev, type, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_unpack8");
+}
+
+nna_status nna_decay_attention_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes) {
+  if (!bytes) return fail(NNA_ERR_INVALID_ARG, "bytes is NULL");
+  nna_status s = check_heads(NNA_F32, B, T, H, dk, dv);
+  if (s != NNA_OK) return s;
+  int segments, chunks;
+  *bytes = decay_segments(B, T, (int)H, (int)dk, (int)dv, &segments, &chunks);
+  return NNA_OK;
+}
+
+nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, const void* k_dev, const long long* k_strides, const void* v_dev,
+                               const long long* v_strides, nna_dtype type, long long B, long long T, long long H, long long dk, long long dv,
+                               const float* decay_dev, double scale, const int* lengths_dev, const float* first_dev, float* last_dev,
+                               void* out_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream) {
+  nna_status s = check_heads(type, B, T, H, dk, dv);
+  if (s != NNA_OK) return s;
+  if (!q_strides || !k_strides || !v_strides) return fail(NNA_ERR_INVALID_ARG, "strides are NULL");
+  if (B && T && (!q_dev || !k_dev || !v_dev || !out_dev)) return fail(NNA_ERR_INVALID_ARG, "q_dev / k_dev / v_dev / out_dev is NULL");
+  DecayMix P = {};
+  s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, decay_segments(B, T, (int)H, (int)dk, (int)dv, &P.segments, &P.segment_chunks));
+  if (s != NNA_OK) return s;
+  set_mix(P, heads_of(q_dev, q_strides, dk), heads_of(k_dev, k_strides, dk), heads_of(v_dev, v_strides, dv));
+  P.out = out_dev;
+  P.decay = decay_dev;
+  P.lengths = lengths_dev;
+  P.first = first_dev;
+  P.last = last_dev;
+  P.parts = static_cast<float*>(workspace_dev);
+  P.factor = (float)scale;
+  P.first_factor = P.last_factor = 1.f;
+  P.B = B;
+  P.T = T;
+  P.H = (int)H;
+  DeviceGuard guard;
+  s = enter_device(guard, device);
+  if (s != NNA_OK || !B) return s;
+  const hipError_t e = launch_decay_mix(P, type, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "linear attention");
+}
+
+nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev, const long long* q_strides, const void* k_dev,
+                                        const long long* k_strides, const void* v_dev, const long long* v_strides, nna_dtype type, long long B,
+                                        long long T, long long H, long long dk, long long dv, const float* decay_dev, double scale,
+                                        const int* lengths_dev, const float* first_dev, const float* glast_dev, void* gq_dev, void* gk_dev,
+                                        void* gv_dev, float* gfirst_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream) {
+  nna_status s = check_heads(type, B, T, H, dk, dv);
+  if (s != NNA_OK) return s;
+  if (!q_strides || !k_strides || !v_strides) return fail(NNA_ERR_INVALID_ARG, "strides are NULL");
+  if (B && T && (!gout_dev || !q_dev || !k_dev || !v_dev)) return fail(NNA_ERR_INVALID_ARG, "gout_dev / q_dev / k_dev / v_dev is NULL");
+  if (!gq_dev && !gk_dev && !gv_dev && B && T) return fail(NNA_ERR_INVALID_ARG, "no gradient is asked for");
+  if (gfirst_dev && !gk_dev && !gv_dev && B && T) return fail(NNA_ERR_INVALID_ARG, "gfirst_dev comes with gk_dev or gv_dev");
+  DecayMix P = {};
+  s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, decay_segments(B, T, (int)H, (int)dk, (int)dv, &P.segments, &P.segment_chunks));
+  if (s != NNA_OK) return s;
+  const long long packed[3] = {T * H * dv, H * dv, dv};
+  const Heads q = heads_of(q_dev, q_strides, dk), k = heads_of(k_dev, k_strides, dk), v = heads_of(v_dev, v_strides, dv), g = heads_of(gout_dev, packed, dv);
+  P.decay = decay_dev;
+  P.lengths = lengths_dev;
+  P.parts = static_cast<float*>(workspace_dev);
+  P.factor = (float)scale;
+  P.B = B;
+  P.T = T;
+  P.H = (int)H;
+  DeviceGuard guard;
+  s = enter_device(guard, device);
+  if (s != NNA_OK || !B) return s;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipError_t e = hipSuccess;
+  if (gq_dev) {
+    set_mix(P, g, v, k);
+    P.out = gq_dev;
+    P.first = first_dev;
+    P.first_factor = 1.f;
+    P.transposed = 1;
+    e = launch_decay_mix(P, type, stream);
+  }
+  // the state's gradient, without q's scale: the outputs get it at the end, as gfirst does
+  P.reverse = 1;
+  P.first = glast_dev;
+  P.first_factor = (float)(1.0 / scale);
+  P.last = gfirst_dev;
+  P.last_factor = (float)scale;
+  if (gv_dev && e == hipSuccess) {
+    set_mix(P, k, q, g);
+    P.out = gv_dev;
+    P.transposed = 0;
+    e = launch_decay_mix(P, type, stream);
+    P.last = nullptr;
+  }
+  if ((gk_dev || (!T && gfirst_dev)) && e == hipSuccess) {
+    set_mix(P, v, g, q);
+    P.out = gk_dev;
+    P.transposed = 1;
+    e = launch_decay_mix(P, type, stream);
+  }
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "linear attention, backward");
+}
+
+nna_status nna_decay_attention_step(const void* q_dev, const long long* q_strides, const void* k_dev, const long long* k_strides, const void* v_dev,
+                                    const long long* v_strides, nna_dtype type, long long B, long long H, long long dk, long long dv,
+                                    const float* decay_dev, double scale, float* state_dev, void* out_dev, int device, void* hip_stream) {
+  nna_status s = check_heads(type, B, 1, H, dk, dv);
+  if (s == NNA_OK) s = check_decay_args(decay_dev, scale, nullptr, 0, 0);
+  if (s != NNA_OK) return s;
+  if (!q_strides || !k_strides || !v_strides) return fail(NNA_ERR_INVALID_ARG, "strides are NULL");
+  if (B && (!q_dev || !k_dev || !v_dev || !state_dev || !out_dev)) return fail(NNA_ERR_INVALID_ARG, "q_dev / k_dev / v_dev / state_dev / out_dev is NULL");
+  DecayStep P = {};
+  P.q = q_dev;
+  P.k = k_dev;
+  P.v = v_dev;
+  P.q_b = q_strides[0];
+  P.q_h = q_strides[1];
+  P.k_b = k_strides[0];
+  P.k_h = k_strides[1];
+  P.v_b = v_strides[0];
+  P.v_h = v_strides[1];
+  P.out = out_dev;
+  P.decay = decay_dev;
+  P.state = state_dev;
+  P.factor = (float)scale;
+  P.B = B;
+  P.H = (int)H;
+  P.dk = (int)dk;
+  P.dv = (int)dv;
+  DeviceGuard guard;
+  s = enter_device(guard, device);
+  if (s != NNA_OK || !B) return s;
+  const hipError_t e = launch_decay_step(P, type, static_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "linear attention, one frame");
 }
 
 }  // extern "C"

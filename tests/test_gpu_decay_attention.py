@@ -1,0 +1,346 @@
+"""Linear attention with a decay for each head against its definition in 64 bits (all pairs of frames), forward, backward and frame by frame.
+
+Tolerances.  With M the same sums over magnitudes, float32 results are off by at most C 2^-24 M: C counts the products summed one after the other
+(dk + dv + 192 in a chunk and two a chunk after it) and the powers (an exponent of up to 126 is rounded twice: 256).  With bfloat16 the weights and the
+state are rounded once where they are multiplied (2^-8 of M at most), and so is the result (2^-8 of it); over many values of either
+sign the roundings add as squares: together at most 2^-8 of the result's norm.
+"""
+import math
+import sys
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U32, U16 = 2.0**-24, 2.0**-8
+
+
+@pytest.fixture(scope="module")
+def nb():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU (there is no CPU fallback)")
+    from paper_1912_12055_amd import binding
+    binding.lib()
+    return binding
+
+
+def _say(*a):
+    print("[case]", *a, file=sys.stderr, flush=True)
+
+
+def _inputs(B, T, H, dk, dv, dtype, seed=0, state=True):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+
+    def normal(*s):
+        return torch.randn(*s, device=DEV, generator=g)
+
+    q, k, v, go = (normal(B, T, H, d).to(dtype) for d in (dk, dk, dv, dv))
+    decay = 1 - 2.0 ** (-1 - 8 * torch.rand(H, device=DEV, generator=g))
+    first, glast = (normal(B, H, dk, dv), normal(B, H, dk, dv)) if state else (None, None)
+    return q, k, v, go, decay, first, glast
+
+
+def _exact(q, k, v, decay, first=None, lengths=None, go=None, glast=None, scale=None):
+    """{name: (value, magnitude)} by the definition, each (sequence, head) over all pairs of its frames"""
+    B, T, H, dk = q.shape
+    dv = v.shape[-1]
+    scale = dk**-0.5 if scale is None else scale
+    lengths = [T] * B if lengths is None else [min(max(int(n), 0), T) for n in lengths]
+    shape = dict(o=(B, T, H, dv), gq=(B, T, H, dk), gk=(B, T, H, dk), gv=(B, T, H, dv), last=(B, H, dk, dv), gfirst=(B, H, dk, dv))
+    out = {name: (torch.zeros(s, dtype=torch.float64, device=DEV), torch.zeros(s, dtype=torch.float64, device=DEV)) for name, s in shape.items()}
+    for b, n in enumerate(lengths):
+        for h in range(H):
+            for m, fn in enumerate((lambda x: x, torch.abs)):
+                l = float(decay[h])
+                Q, K, V = (fn(x[b, :n, h].double()) for x in (q, k, v))
+                S = torch.zeros(dk, dv, dtype=torch.float64, device=DEV) if first is None else fn(first[b, h].double())
+                t = torch.arange(n, device=DEV)
+                gap = (t[:, None] - t).double()
+                D = torch.where(gap >= 0, torch.tensor(l, dtype=torch.float64, device=DEV) ** gap.clamp(min=0), 0)
+                L = torch.tensor(l, dtype=torch.float64, device=DEV)
+                since, left = (L ** (t + 1).double())[:, None], (L ** (n - 1 - t).double())[:, None]
+                sc = scale if m == 0 else abs(scale)
+                W = sc * (Q @ K.T) * D
+                out["o"][m][b, :n, h] = W @ V + sc * since * (Q @ S)
+                out["last"][m][b, h] = L**n * S + (left * K).T @ V
+                if go is not None:
+                    G = fn(go[b, :n, h].double())
+                    GS = torch.zeros_like(S) if glast is None else fn(glast[b, h].double())
+                    out["gv"][m][b, :n, h] = W.T @ G + left * (K @ GS)
+                    W = sc * (G @ V.T) * D
+                    out["gq"][m][b, :n, h] = W @ K + sc * since * (G @ S.T)
+                    out["gk"][m][b, :n, h] = W.T @ Q + left * (V @ GS.T)
+                    out["gfirst"][m][b, h] = L**n * GS + sc * (since * Q).T @ G
+    return out
+
+
+def _close(got, exact, name, T, dk, dv):
+    ref, most = exact[name]
+    assert got.shape == ref.shape, name
+    assert torch.isfinite(got).all(), name
+    d = (got.double() - ref).abs()
+    bound = (dk + dv + 192 + 2 * (T // 64) + 256) * U32 * most + 1e-37
+    if got.dtype == torch.bfloat16:
+        bound = bound + U16 * (ref.abs() + 1.01 * most)
+        if got.numel() > 1000:
+            assert d.norm() <= U16 * ref.norm(), (name, float(d.norm() / ref.norm()))
+    worst = float((d / bound).max()) if d.numel() else 0.0
+    assert worst <= 1, (name, worst)
+
+
+def _check(nb, q, k, v, go, decay, first, glast, lengths=None, scale=None):
+    B, T, H, dk = q.shape
+    dv = v.shape[-1]
+    e = _exact(q, k, v, decay, first, lengths, go, glast, scale)
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    o, last = nb.nna_decay_attention(q, k, v, decay, scale=scale, state=first, lengths=n, want_state=True)
+    gq, gk, gv, gfirst = nb.nna_decay_attention_backward(go, q, k, v, decay, scale=scale, state=first, lengths=n, gstate=glast, want_gstate=True)
+    assert {x.dtype for x in (o, gq, gk, gv)} == {q.dtype}
+    for name, x in dict(o=o, last=last, gq=gq, gk=gk, gv=gv, gfirst=gfirst).items():
+        _close(x, e, name, T, dk, dv)
+    return o, last, gq, gk, gv, gfirst
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [1, 2, 15, 63, 64, 65, 128, 129, 200, 431])
+def test_every_length(nb, dtype, T):
+    for state in (True, False):
+        _say("T", T, dtype, state)
+        _check(nb, *_inputs(2, T, 3, 64, 64, dtype, seed=T, state=state))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dk,dv", [(1, 1), (3, 5), (16, 32), (32, 7), (64, 128), (128, 64), (65, 63), (48, 96), (100, 128), (128, 128), (127, 33)])
+def test_every_head_size(nb, dtype, dk, dv):
+    _say("heads", dk, dv, dtype)
+    _check(nb, *_inputs(2, 150, 2, dk, dv, dtype, seed=dk + dv))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,T,H,dk,dv", [(1, 5000, 1, 64, 64), (1, 2111, 3, 128, 128), (3, 1025, 5, 64, 128), (2, 3000, 4, 40, 24), (600, 70, 2, 32, 32)])
+def test_long_sequences_in_segments_and_many_short_ones(nb, dtype, B, T, H, dk, dv):
+    _say("segments", B, T, H, dk, dv, dtype, nb.nna_decay_attention_workspace(B, T, H, dk, dv))
+    args = _inputs(B, T, H, dk, dv, dtype, seed=T)
+    args[4][0] = 1 - 2.0**-11  # a head that remembers across segments
+    _check(nb, *args)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,lengths", [(200, [0, 200, 1, 64, 65, 199, 128]), (2000, [2000, 0, 700, 1999, 512, 1]), (70, [-3, 1000, 64, 5])])
+def test_lengths_and_what_lies_past_them(nb, dtype, T, lengths):
+    _say("lengths", T, lengths, dtype)
+    q, k, v, go, decay, first, glast = _inputs(len(lengths), T, 2, 64, 96, dtype, seed=T)
+    whole = _check(nb, q, k, v, go, decay, first, glast, lengths)
+    for b, n in enumerate(lengths):  # infinities and NaN past the end change nothing
+        for x in (q, k, v, go):
+            x[b, max(n, 0):] = float("nan")
+            x[b, max(n, 0)::2] = float("inf")
+    n = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    again = (*nb.nna_decay_attention(q, k, v, decay, state=first, lengths=n, want_state=True),
+             *nb.nna_decay_attention_backward(go, q, k, v, decay, state=first, lengths=n, gstate=glast, want_gstate=True))
+    assert all(torch.equal(a, c) for a, c in zip(whole, again))
+    for b, n in enumerate(lengths):
+        n = min(max(n, 0), T)
+        assert not any(x[b, n:].any() for x in (whole[0], *whole[2:5]))
+        if n == 0:
+            assert torch.equal(whole[1][b], first[b])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_strides_shared_heads_and_orders(nb, dtype):
+    B, T, H, dk, dv = 2, 130, 4, 40, 56
+    g = torch.Generator(device=DEV).manual_seed(2)
+    wide = torch.randn(B, T, 1 + H * (2 * dk + dv) + 3, device=DEV, generator=g).to(dtype)
+    q = wide[..., 1:1 + H * dk].unflatten(-1, (H, dk))
+    k = wide[..., 1 + H * dk:1 + 2 * H * dk].unflatten(-1, (H, dk))
+    v = wide[..., 1 + 2 * H * dk:1 + H * (2 * dk + dv)].unflatten(-1, (H, dv))
+    _, _, _, go, decay, first, glast = _inputs(B, T, H, dk, dv, dtype)
+    _check(nb, q, k, v, go, decay, first, glast)  # parts of one projection, no start aligned
+    hq, hk, hv = (x.transpose(1, 2).contiguous().transpose(1, 2) for x in (q, k, v))
+    _check(nb, hq, hk, hv, go, decay, first, glast)  # [B, H, T, d] in memory
+    shared = k[:, :, :1].expand(B, T, H, dk), v[:, :, 1:2].expand(B, T, H, dv)
+    _check(nb, q, *shared, go, decay, first, glast)  # keys and values that the heads share
+    _check(nb, q[:1].expand(B, T, H, dk), k, v, go, decay, first, glast)  # queries that the sequences share
+    _check(nb, q.flip(1)[:, ::2], k[:, ::2], v[:, 1::2], go[:, :65].contiguous(), decay, first, glast)
+
+
+def test_gradients_of_shared_heads_through_autograd_sums(nb):
+    """what autograd makes of an expanded input: the sum of the heads' gradients"""
+    q, k, v, go, decay, _, _ = _inputs(1, 90, 4, 32, 32, torch.float32, state=False)
+    k1 = k[:, :, :1]
+    gk = nb.nna_decay_attention_backward(go, q, k1.expand(-1, -1, 4, -1), v, decay)[1].sum(2, keepdim=True)
+    e = _exact(q, k1.expand(-1, -1, 4, -1), v, decay, go=go)["gk"]
+    assert ((gk.double() - e[0].sum(2, keepdim=True)).abs() <= 800 * U32 * e[1].sum(2, keepdim=True)).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_decays_of_zero_one_and_near_them(nb, dtype):
+    q, k, v, go, decay, first, glast = _inputs(1, 300, 6, 64, 64, dtype, seed=4)
+    decay[:] = torch.tensor([0.0, 1.0, 1e-30, 1 - 2.0**-24, 0.5, 1e-3], device=DEV)
+    _check(nb, q, k, v, go, decay, first, glast)
+    o = nb.nna_decay_attention(q, k, v, decay)[:, :, 0]
+    alone = (q[:, :, 0].double() * k[:, :, 0].double()).sum(-1, keepdim=True) * v[:, :, 0].double() / 8  # a head without memory
+    assert (o.double() - alone).norm() <= U16 * alone.norm()
+
+
+@pytest.mark.parametrize("scale", [1.0, -0.3, 7.5])
+def test_scales(nb, scale):
+    _check(nb, *_inputs(2, 100, 2, 32, 32, torch.float32, seed=8), scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [100, 1500])
+def test_a_value_that_is_not_finite_reaches_no_frame_before_it(nb, dtype, T):
+    q, k, v, go, decay, first, glast = _inputs(2, T, 2, 64, 64, dtype, seed=6)
+    clean = (*nb.nna_decay_attention(q, k, v, decay, state=first, want_state=True), *nb.nna_decay_attention_backward(go, q, k, v, decay, state=first, gstate=glast, want_gstate=True))
+    at = 77
+    for x, value in ((v, float("nan")), (v, float("inf")), (k, float("nan")), (k, -float("inf")), (q, float("nan"))):
+        _say("not finite", "qkv"[[id(q), id(k), id(v)].index(id(x))], value, dtype, T)
+        keep = x.clone()
+        x[1, at, 0, 5] = value
+        o, last = nb.nna_decay_attention(q, k, v, decay, state=first, want_state=True)
+        assert torch.equal(o[0], clean[0][0]) and torch.equal(o[:, :, 1], clean[0][:, :, 1]) and torch.equal(o[1, :at], clean[0][1, :at])
+        assert not torch.isfinite(o[1, at, 0]).all()
+        if x is q:
+            assert torch.equal(o[1, at + 1:], clean[0][1, at + 1:]) and torch.equal(last, clean[1])
+        else:
+            assert not torch.isfinite(o[1, T - 1, 0]).all() and not torch.isfinite(last[1, 0]).all()
+        if x is v:
+            assert torch.isnan(o[1, at:, 0]).all() and torch.isnan(last[1, 0]).all()
+        x.copy_(keep)
+    go[1, at, 0, 3] = float("inf")  # the gradients of frames after it do not know it
+    gq, gk, gv, gfirst = nb.nna_decay_attention_backward(go, q, k, v, decay, state=first, gstate=glast, want_gstate=True)
+    for got, ref in zip((gk, gv), clean[3:5]):
+        assert torch.equal(got[1, at + 1:], ref[1, at + 1:]) and torch.equal(got[0], ref[0])
+    others = [t for t in range(T) if t != at]
+    assert torch.equal(gq[1, others], clean[2][1, others]) and torch.isnan(gv[1, at, 0]).all()
+
+
+def test_the_same_inputs_give_the_same_bits(nb):
+    q, k, v, go, decay, first, glast = _inputs(2, 3000, 4, 64, 64, torch.bfloat16)
+    for _ in range(2):
+        runs = [(*nb.nna_decay_attention(q, k, v, decay, state=first, want_state=True), *nb.nna_decay_attention_backward(go, q, k, v, decay, state=first, gstate=glast, want_gstate=True)) for _ in range(2)]
+        assert all(torch.equal(a, c) for a, c in zip(*runs))
+
+
+def test_gradients_against_differences(nb):
+    """out and the last state are linear in each of q, k and v: the difference along a direction is exact but for rounding, C 2^-24 of the
+    magnitudes at either end."""
+    q, k, v, go, decay, first, glast = _inputs(2, 150, 2, 32, 40, torch.float32, seed=12)
+    go, glast = go.contiguous(), glast.contiguous()
+
+    def loss(q, k, v, first):
+        o, last = nb.nna_decay_attention(q, k, v, decay, state=first, want_state=True)
+        return float((go.double() * o.double()).sum() + (glast.double() * last.double()).sum())
+
+    gq, gk, gv, gfirst = nb.nna_decay_attention_backward(go, q, k, v, decay, state=first, gstate=glast, want_gstate=True)
+    e = _exact(q, k, v, decay, first, None, go, glast)
+    size = float((e["o"][1] * go.abs()).sum() + (e["last"][1] * glast.abs()).sum())
+    g = torch.Generator(device=DEV).manual_seed(1)
+    args = dict(q=q, k=k, v=v, first=first)
+    for name, grad in (("q", gq), ("k", gk), ("v", gv), ("first", gfirst)):
+        d = torch.randn(args[name].shape, device=DEV, generator=g)
+        up, down = (loss(**{**args, name: args[name] + s * d}) for s in (1, -1))
+        got = float((grad.double() * d.double()).sum())
+        assert abs(got - (up - down) / 2) <= 1000 * U32 * 4 * size, name
+
+
+# ---- frame by frame ----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,H,dk,dv", [(1, 1, 1, 1), (1, 8, 64, 64), (3, 2, 33, 31), (2, 3, 128, 128), (5, 4, 96, 50), (300, 2, 64, 128)])
+def test_frames_one_by_one(nb, dtype, B, H, dk, dv):
+    _say("step", B, H, dk, dv, dtype)
+    T = 20
+    q, k, v, go, decay, first, _ = _inputs(B, T, H, dk, dv, dtype, seed=B + dk)
+    e = _exact(q, k, v, decay, first)
+    state = first.clone()
+    for t in range(T):
+        o = nb.nna_decay_attention_step(q[:, t], k[:, t], v[:, t], decay, state)
+        ref, most = e["o"][0][:, t], e["o"][1][:, t]
+        bound = (dk + 64) * U32 * most + 1e-37 + (U16 * ref.abs() if dtype == torch.bfloat16 else 0)
+        assert float(((o.double() - ref).abs() / bound).max()) <= 1, t
+    assert ((state.double() - e["last"][0]).abs() <= 64 * U32 * e["last"][1] + 1e-37).all()
+
+
+def test_a_prompt_and_then_frames_one_by_one(nb):
+    q, k, v, _, decay, _, _ = _inputs(2, 500, 4, 64, 64, torch.float32, state=False)
+    whole, last = nb.nna_decay_attention(q, k, v, decay, want_state=True)
+    e = _exact(q, k, v, decay)
+    o, state = nb.nna_decay_attention(q[:, :450], k[:, :450], v[:, :450], decay, want_state=True)
+    assert torch.equal(o, whole[:, :450])
+    for t in range(450, 500):
+        step = nb.nna_decay_attention_step(q[:, t], k[:, t], v[:, t], decay, state)
+        assert ((step.double() - e["o"][0][:, t]).abs() <= 800 * U32 * e["o"][1][:, t]).all()
+    assert ((state.double() - last.double()).abs() <= 800 * U32 * e["last"][1]).all()
+    # in pieces: the state of one is the first of the next
+    state, pieces = None, []
+    for a, b in ((0, 1), (1, 64), (64, 200), (200, 500)):
+        o, state = nb.nna_decay_attention(q[:, a:b], k[:, a:b], v[:, a:b], decay, state=state, want_state=True)
+        pieces.append(o)
+    assert ((torch.cat(pieces, 1).double() - e["o"][0]).abs() <= 800 * U32 * e["o"][1]).all()
+
+
+# ---- refusals, nothing to do, streams, graphs --------------------------------------------------------------------------------
+def test_nothing_to_do(nb):
+    q, k, v, go, decay, first, glast = _inputs(2, 0, 3, 16, 24, torch.float32)
+    o, last = nb.nna_decay_attention(q, k, v, decay, state=first, want_state=True)
+    assert o.shape == (2, 0, 3, 24) and torch.equal(last, first)
+    gfirst = nb.nna_decay_attention_backward(go, q, k, v, decay, gstate=glast, want_gstate=True)[3]
+    assert torch.allclose(gfirst, glast, rtol=1e-6, atol=0)
+    q, k, v, go, decay, first, glast = _inputs(0, 50, 3, 16, 24, torch.float32)
+    assert nb.nna_decay_attention(q, k, v, decay, state=first, want_state=True)[1].shape == (0, 3, 16, 24)
+    assert nb.nna_decay_attention_backward(go, q, k, v, decay)[0].shape == q.shape
+    assert nb.nna_decay_attention_step(q[:, 0], k[:, 0], v[:, 0], decay, first).shape == (0, 3, 24)
+
+
+def test_refusals(nb):
+    q, k, v, go, decay, first, glast = _inputs(2, 10, 3, 16, 24, torch.float32)
+    call = nb.nna_decay_attention
+    for bad in (lambda: call(q.cpu(), k, v, decay), lambda: call(q.half(), k.half(), v.half(), decay), lambda: call(q, k.bfloat16(), v, decay),
+                lambda: call(q[0], k[0], v[0], decay), lambda: call(q, k[..., :15], v, decay), lambda: call(q, k, v[:, :9], decay),
+                lambda: call(q[..., ::2], k[..., ::2], v, decay), lambda: call(q, k, v, decay[:2]), lambda: call(q, k, v, decay.double()),
+                lambda: call(q, k, v, decay, state=first.bfloat16()), lambda: call(q, k, v, decay, state=first[:, :, :, :5]),
+                lambda: call(q, k, v, decay, lengths=torch.tensor([1, 2], device=DEV)), lambda: call(q, k, v, decay, lengths=torch.tensor([1, 2], dtype=torch.int32)),
+                lambda: call(q, k, v, decay, out=torch.empty_like(q)), lambda: nb.nna_decay_attention_backward(go.bfloat16(), q, k, v, decay),
+                lambda: nb.nna_decay_attention_backward(go[:, :5], q, k, v, decay), lambda: nb.nna_decay_attention_step(q, k, v, decay, first),
+                lambda: nb.nna_decay_attention_step(q[:, 0], k[:, 0], v[:, 0], decay, None)):
+        with pytest.raises(TypeError):
+            bad()
+    wide = torch.empty((1, 4, 1, 129), device=DEV)
+    long = _inputs(1, 5000, 1, 64, 64, torch.float32)
+    for bad, status in ((lambda: call(q, k, v, decay, scale=0.0), nb.NNA_ERR_INVALID_ARG), (lambda: call(q, k, v, decay, scale=float("nan")), nb.NNA_ERR_INVALID_ARG),
+                        (lambda: call(wide, wide, wide, decay[:1]), nb.NNA_ERR_UNSUPPORTED),
+                        (lambda: call(*long[:3], long[4], workspace=torch.empty(256, dtype=torch.uint8, device=DEV)), nb.NNA_ERR_INVALID_ARG)):
+        with pytest.raises(nb.NnaError) as e:
+            bad()
+        assert e.value.status == status
+
+
+def test_on_another_stream_and_in_a_graph(nb):
+    q, k, v, go, decay, first, glast = _inputs(1, 3000, 2, 64, 64, torch.bfloat16)
+    assert nb.nna_decay_attention_workspace(1, 3000, 2, 64, 64)
+
+    def step(stream=None):
+        return (*nb.nna_decay_attention(q, k, v, decay, state=first, want_state=True, stream=stream),
+                *nb.nna_decay_attention_backward(go, q, k, v, decay, state=first, gstate=glast, want_gstate=True, stream=stream))
+
+    eager = step()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    out = step(stream=side.cuda_stream)
+    side.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(eager, out))
+    state = first.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+        one = nb.nna_decay_attention_step(q[:, 0], k[:, 0], v[:, 0], decay, state)
+    check = first.clone()
+    for i in range(3):
+        q.copy_(torch.randn_like(q))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*out, one, state)]
+        want = nb.nna_decay_attention_step(q[:, 0], k[:, 0], v[:, 0], decay, check)
+        assert all(torch.equal(a, c) for a, c in zip((*step(), want, check), got)), i
