@@ -627,7 +627,8 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
  *   S_t = l S_{t-1} + k_t^T v_t,   o_t = scale q_t S_t = scale (sum_{s <= t} l^(t-s) (q_t . k_s) v_s + l^(t+1) q_t S_first).
  * nna_decay_attention takes whole sequences, nna_decay_attention_step one new frame of each.
  *   q_dev, k_dev [B, T, H, dk], v_dev [B, T, H, dv]   of `type`, NNA_F32 or NNA_BF16 (float16 has no range for the weights l^(t-s) q . k); a head's
- *                values next to each other, strides[3] = elements between batches, frames, heads (0 where they are shared).  dk, dv 1..128
+ *                values next to each other, strides[3] = elements between batches, frames (at most
+ *                2^24), heads (0 where they are shared).  dk, dv 1..128
  *   decay_dev    [H] float32, in [0, 1]: a constant of the head (no gradient is taken)
  *   scale        finite, not 0
  *   lengths_dev  [B] int32 in device memory, or NULL: T.  Frames from a sequence's length on (below 0: 0, above T: T) take no part: their values are not
@@ -640,8 +641,8 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
  * outputs of its head NaN from its frame on, and the last state; one of k likewise by the rules of arithmetic; one of q its own frame's.
  *
  * nna_decay_attention_backward: given gout_dev [B, T, H, dv] (contiguous) and glast_dev (or NULL: 0), the gradients of a loss with respect to out and
- * the last state: gq_dev, gk_dev [B, T, H, dk], gv_dev [B, T, H, dv] (each or NULL; contiguous, of `type`) and gfirst_dev [B, H, dk, dv] (or NULL; with gk_dev
- * or gv_dev).  The same inputs give the same bits.
+ * the last state: gq_dev [B, T, H, dk] (or NULL), gk_dev [B, T, H, dk] and gv_dev [B, T, H, dv] (both or neither; contiguous, of `type`), and with
+ * these gfirst_dev [B, H, dk, dv] (or NULL).  The same inputs give the same bits.
  * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_UNSUPPORTED (type, dk or dv above 128), NNA_ERR_SHAPE.  T = 0 or B = 0 is no error.
  */
 nna_status nna_decay_attention_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes);

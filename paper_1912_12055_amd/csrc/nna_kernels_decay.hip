@@ -12,92 +12,80 @@
 
 namespace nna {
 
+constexpr int CHUNK = DECAY_CHUNK;
+
 namespace {
 
 typedef __bf16 bf16;
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int CHUNK = DECAY_CHUNK;
-constexpr int THREADS = 256, WAVES = THREADS / 64;
-
-// A fragment: 16 of a matrix's k, lane (i, g) of (lane % 16, lane / 16) holds k = 4 g .. 4 g + 3 of row (A) or column (B) i.  It is how the 16 x 16
-// accumulator of an earlier product lies (rows 4 g .. 4 g + 3 of column i), so that a state or a block of weights is an operand as it is.
-template <typename T>
-struct Kind;
-
-template <>
-struct Kind<bf16> {
-  typedef bf16x4 frag;
-  static constexpr int pad = 16;  // elements: a row's reads along it, and four rows' across, meet every bank once
-  static constexpr int planes = 3;  // a float32 as this many operands: exactly
-  typedef bf16 oct __attribute__((ext_vector_type(8), aligned(2)));
-  static __device__ __forceinline__ f32x4 mma(frag a0, frag a1, frag b0, frag b1, f32x4 s) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7), __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7), s, 0, 0, 0);
-  }
-  // 8 consecutive k of a row, at p
-  static __device__ __forceinline__ void row8(const bf16* p, frag& f0, frag& f1) {
-    const bf16x8 v = *reinterpret_cast<const bf16x8*>(p);
-    f0 = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-    f1 = __builtin_shufflevector(v, v, 4, 5, 6, 7);
-  }
-  static __device__ __forceinline__ frag row4(const bf16* p) { return *reinterpret_cast<const bf16x4*>(p); }
-  // k along the rows: the fragment of rows k0 .. k0 + 15, columns n0 .. n0 + 15 of a tile
-  static __device__ __forceinline__ frag column(const bf16* tile, int pitch, int k0, int n0, int lane) {
-    const bf16* p = tile + (k0 + (lane >> 2)) * pitch + n0 + (lane & 3) * 4;
-    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
-  }
-  static __device__ __forceinline__ frag round(f32x4 v) { return __builtin_convertvector(v, bf16x4); }
-  // v exactly, as the sum of three
-  static __device__ __forceinline__ void split(f32x4 v, frag (&f)[3]) {
+// ---- operands ----------------------------------------------------------------------------------------------------------
+// All products are bfloat16 matrix instructions with float32 sums, 16 x 16 x 32.  A float32 is the sum of three bfloat16, each the rounding of what the ones
+// before leave; a product of two takes the six of the nine products of planes that a float32 sum can tell from zero.  An operand is
+// planes of eight values a lane: lane (i, g) of (lane % 16, lane / 16) holds row (A) or column (B) i, of the 32 k either 8 g .. 8 g + 7 or, so
+// that a 16 x 16 accumulator of an earlier product (rows 4 g .. 4 g + 3 of column i) is one as it lies, 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3.
+template <int NA, int NB>
+__device__ __forceinline__ f32x4 mma(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x4 s) {
+  constexpr int most = NA > NB ? NA : NB;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      f[i] = __builtin_convertvector(v, bf16x4);
-      v -= __builtin_convertvector(f[i], f32x4);
+  for (int t = most - 1; t >= 0; --t)  // small terms first
+#pragma unroll
+    for (int i = 0; i <= t; ++i)
+      if (i < NA && t - i < NB) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[t - i], s, 0, 0, 0);
+  return s;
+}
+__device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// two accumulators (k and 16 + k) as an operand of N planes
+template <int N>
+__device__ __forceinline__ void split(f32x4 v, f32x4 w, bf16x8 (&o)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bf16x4 a = __builtin_convertvector(v, bf16x4), b = __builtin_convertvector(w, bf16x4);
+    o[i] = join(a, b);
+    if (i + 1 < N) {
+      v -= __builtin_convertvector(a, f32x4);
+      w -= __builtin_convertvector(b, f32x4);
     }
   }
-  // whether one of the eight is not finite
-  static __device__ __forceinline__ bool odd(oct v) {
-    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-    const bf16x8 w = v;
-    const u32x4 u = (__builtin_bit_cast(u32x4, w) & 0x7f807f80u) + 0x00800080u;
-    return ((u[0] | u[1] | u[2] | u[3]) & 0x80008000u) != 0;
-  }
-};
+}
 
-template <>
-struct Kind<float> {
-  typedef f32x4 frag;
-  static constexpr int pad = 4;
-  static constexpr int planes = 1;
-  typedef float oct __attribute__((ext_vector_type(8), aligned(4)));
-  static __device__ __forceinline__ f32x4 mma(frag a0, frag a1, frag b0, frag b1, f32x4 s) {
+// ---- tiles in LDS: planes of rows (frames), a head's values along a row ------------------------------------------------------
+// elements between rows, so that 16 lanes that read along 16 rows, and four across four, meet different banks
+__host__ __device__ constexpr int pitch_of(int d) { return d == 64 ? d + 8 : d + 24; }
+template <int ROWS, int D, int N>
+struct Tile {
+  static constexpr int PITCH = pitch_of(D), PLANE = ROWS * PITCH, SIZE = N * PLANE;
+  // k along a row: values k0 + 8 g .. of row0 + i
+  static __device__ __forceinline__ void rows8(const bf16* tile, int row0, int k0, int li, int lg, bf16x8 (&o)[N]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(a0[e], b0[e], s, 0, 0, 0);
+    for (int p = 0; p < N; ++p) o[p] = *reinterpret_cast<const bf16x8*>(tile + p * PLANE + (row0 + li) * PITCH + k0 + lg * 8);
+  }
+  // ... in the order of accumulators
+  static __device__ __forceinline__ void rows4(const bf16* tile, int row0, int k0, int li, int lg, bf16x8 (&o)[N]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(a1[e], b1[e], s, 0, 0, 0);
-    return s;
+    for (int p = 0; p < N; ++p) {
+      const bf16* at = tile + p * PLANE + (row0 + li) * PITCH + k0 + lg * 4;
+      o[p] = join(*reinterpret_cast<const bf16x4*>(at), *reinterpret_cast<const bf16x4*>(at + 16));
+    }
   }
-  static __device__ __forceinline__ void row8(const float* p, frag& f0, frag& f1) {
-    f0 = *reinterpret_cast<const f32x4*>(p);
-    f1 = *reinterpret_cast<const f32x4*>(p + 4);
-  }
-  static __device__ __forceinline__ frag row4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-  static __device__ __forceinline__ frag column(const float* tile, int pitch, int k0, int n0, int lane) {
-    const float* p = tile + (k0 + (lane >> 4) * 4) * pitch + n0 + (lane & 15);
-    return f32x4{p[0], p[pitch], p[2 * pitch], p[3 * pitch]};
-  }
-  static __device__ __forceinline__ frag round(f32x4 v) { return v; }
-  static __device__ __forceinline__ void split(f32x4 v, frag (&f)[1]) { f[0] = v; }
-  static __device__ __forceinline__ bool odd(oct v) {
-    bool bad = false;
+  // k across rows, in the order of accumulators: rows row0 .. row0 + 31 of column0 + i
+  static __device__ __forceinline__ void columns(const bf16* tile, int row0, int column0, int lane, bf16x8 (&o)[N]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) bad |= !(__builtin_fabsf(v[i]) < __builtin_inff());
-    return bad;
+    for (int p = 0; p < N; ++p) {
+      const bf16* at = tile + p * PLANE + (row0 + (lane >> 2)) * PITCH + column0 + (lane & 3) * 4;
+      bf16x4 f[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        f[h] = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + h * 16 * PITCH)));
+      o[p] = join(f[0], f[1]);
+    }
   }
 };
 
@@ -105,330 +93,497 @@ __device__ __forceinline__ float power(float log2_decay, int n) { return __built
 // log2 of a decay; of zero, one whose first power is zero and whose zeroth is one
 __device__ __forceinline__ float log2_of(float decay) { return decay == 0.f ? -1e5f : log2f(decay); }
 
-// 64 rows of D values (d of them real) as the threads hold them between memory and LDS
-template <typename T, int D>
-struct Rows {
-  static constexpr int PER_ROW = D / 8, N = CHUNK * PER_ROW / THREADS;
-  typename Kind<T>::oct v[N];
+// a value that all lanes hold, in a scalar register
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, uniform(__builtin_bit_cast(int, v))); }
 
-  // frames u0 .. u0 + 63 of n; those past the end are zero
-  __device__ __forceinline__ void load(const T* base, long long step, long long u0, long long n, bool reverse, int d) {
+// What is computed of `v` after this is computed there: not ahead of a loop, to be kept in registers through it.
+template <typename V>
+__device__ __forceinline__ V here_only(V v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+template <typename T>
+struct Kind;
+template <>
+struct Kind<bf16> {
+  static constexpr int planes = 1;
+  typedef bf16 oct __attribute__((ext_vector_type(8), aligned(2)));
+  // zero times the values: NaN where one is not finite
+  static __device__ __forceinline__ float nothing(oct v, float s) {
+    const bf16x8 w = v;
+    const bf16x2 zero = {(bf16)0.f, (bf16)0.f};
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int at = threadIdx.x + i * THREADS, column = at % PER_ROW * 8;
-      const long long u = u0 + at / PER_ROW;
-      v[i] = (T)0;
-      if (u < n && column < d) {
-        const T* p = base + (reverse ? n - 1 - u : u) * step + column;
-        if (column + 8 <= d) {
-          v[i] = *reinterpret_cast<const typename Kind<T>::oct*>(p);
+    for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w[2 * i], w[2 * i + 1]}, zero, s, false);
+    return s;
+  }
+  static __device__ __forceinline__ void put(bf16* p, int plane, oct v) { *reinterpret_cast<bf16x8*>(p) = v; }
+  static __device__ __forceinline__ void put1(bf16* p, int plane, bf16 v) { *p = v; }
+};
+template <>
+struct Kind<float> {
+  static constexpr int planes = 3;
+  typedef float oct __attribute__((ext_vector_type(8), aligned(4)));
+  static __device__ __forceinline__ float nothing(oct v, float s) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = __builtin_fmaf(v[i], 0.f, s);
+    return s;
+  }
+  static __device__ __forceinline__ void put(bf16* p, int plane, oct v) {
+    f32x8 left = v;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const bf16x8 w = __builtin_convertvector(left, bf16x8);
+      *reinterpret_cast<bf16x8*>(p + i * plane) = w;
+      if (i < 2) left -= __builtin_convertvector(w, f32x8);
+    }
+  }
+  static __device__ __forceinline__ void put1(bf16* p, int plane, float v) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      p[i * plane] = (bf16)v;
+      v -= (float)p[i * plane];
+    }
+  }
+};
+
+// ROWS rows of D values (d of them real) as THREADS threads hold them between memory and LDS, eight neighbours a lane at a time.  No lane reads what is not
+// there: a row past the end is read as the last one, a lane past d as column 0, and the octet that d ends in is the row's last eight
+// (which then also lie in LDS where they belong; where d < 8, one value after the other).
+template <typename T, int ROWS, int D, int THREADS, bool FULL, bool REVERSE>
+struct Rows {
+  typedef Kind<T> K;
+  typedef typename K::oct oct;
+  typedef Tile<ROWS, D, K::planes> tile_type;
+  static constexpr int PER_ROW = D / 8, OCTETS = ROWS * PER_ROW, N = OCTETS >= THREADS ? OCTETS / THREADS : 1, STEP = THREADS / PER_ROW;
+  oct v[N];
+
+  static __device__ __forceinline__ bool idle(int thread) { return OCTETS < THREADS && thread >= OCTETS; }
+
+  // frame u (row) of `here` frames, whose first in memory is at `base`; `step` elements (below 2^24) from one to the next
+  __device__ __forceinline__ void load(const T* base, int step, int here, int d, int thread) {
+    thread = here_only(thread);
+    const int row = idle(thread) ? 0 : thread / PER_ROW, column = thread % PER_ROW * 8;
+    const int at = FULL || column + 8 <= d ? column : column < d && d >= 8 ? d - 8 : 0;
+    const char* p = reinterpret_cast<const char*>(base);
+    const unsigned bytes = step * (unsigned)sizeof(T);
+    if (here == ROWS && (FULL || d >= 8)) {
+      unsigned offset = (REVERSE ? ROWS - 1 - row : row) * bytes + at * (unsigned)sizeof(T);
+#pragma unroll
+      for (int i = 0; i < N; ++i, offset += REVERSE ? -STEP * bytes : STEP * bytes) v[i] = *reinterpret_cast<const oct*>(p + offset);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = row + i * STEP < here ? row + i * STEP : here - 1;
+        const T* q = reinterpret_cast<const T*>(p + (REVERSE ? here - 1 - r : r) * bytes) + at;
+        if (FULL || d >= 8) {
+          v[i] = *reinterpret_cast<const oct*>(q);
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (column + e < d) v[i][e] = p[e];
+          for (int e = 0; e < 8; ++e) v[i][e] = q[e < d ? e : 0];
         }
       }
     }
   }
-  __device__ __forceinline__ void store(T* tile) const {
+  // the first `here` rows are real, the others and the columns past d zero
+  __device__ __forceinline__ void store(bf16* tile, int here, int d, int thread) {
+    if (idle(thread)) return;
+    const int column = thread % PER_ROW * 8;
+    if (here < ROWS) {
+      const int row = here_only(thread) / PER_ROW;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int at = threadIdx.x + i * THREADS;
-      T* p = tile + at / PER_ROW * (D + Kind<T>::pad) + at % PER_ROW * 8;
-      typedef T half __attribute__((ext_vector_type(16 / sizeof(T))));
-      const typename Kind<T>::oct w = v[i];
+      for (int i = 0; i < N; ++i)
+        if (row + i * STEP >= here) v[i] = (oct)(T)0;
+    }
+    bf16* p = tile + thread / PER_ROW * tile_type::PITCH + column;
 #pragma unroll
-      for (int e = 0; e < 8; e += 16 / sizeof(T)) {
-        half h;
+    for (int i = 0; i < N; ++i, p += STEP * tile_type::PITCH) {
+      if (FULL) {
+        K::put(p, tile_type::PLANE, v[i]);
+        continue;
+      }
+      K::put(p, tile_type::PLANE, column + 8 <= d ? v[i] : (oct)(T)0);
+      if (column < d && column + 8 > d) {
+        bf16* const q = p + (d >= 8 ? d - 8 - column : 0);
 #pragma unroll
-        for (int k = 0; k < (int)(16 / sizeof(T)); ++k) h[k] = w[e + k];
-        *reinterpret_cast<half*>(p + e) = h;
+        for (int e = 0; e < 8; ++e)
+          if (e < d) K::put1(q + e, tile_type::PLANE, v[i][e]);
       }
     }
   }
-  // zero in the place of octets with a value that is not finite; the first row that has one (64: none)
-  __device__ __forceinline__ int clean() {
-    int first = CHUNK;
+  // zero in the place of octets with a value that is not finite; the first of the `here` rows that has one (ROWS: none)
+  __device__ __forceinline__ int clean(int here, int thread) {
+    float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (Kind<T>::odd(v[i])) {
-        v[i] = (T)0;
-        const int row = (threadIdx.x + i * THREADS) / PER_ROW;
-        first = row < first ? row : first;
-      }
+    for (int i = 0; i < N; ++i) s = K::nothing(v[i], s);
+    int first = ROWS;
+    if (s != s)
+#pragma unroll
+      for (int i = N - 1; i >= 0; --i)
+        if (K::nothing(v[i], 0.f) != 0.f) {
+          v[i] = (oct)(T)0;
+          const int row = here_only(thread) / PER_ROW + i * STEP;
+          if (row < here) first = row;
+        }
     return first;
   }
 };
 
+// What a launch does with the chunks: out = mix(a, b, c); the state alone; or, with twice the threads and time reversed, out = mix(a, b, c) and
+// out2 = mix(a2, c, b), whose states are each other's transpose, from one reading of all four.
+enum { MIX, STATE, PAIR };
+
+// Frames of a chunk: 64; 32 where three planes of 128 columns leave no room for more.  Columns of the state to a wave: 32 where a state of 128 x 32 and
+// the rest fit 256 registers, so that what is read from LDS meets two products; else 16.
 template <typename T, int DA, int DC>
-constexpr int mix_lds(bool state_only) {
-  const int pad = Kind<T>::pad;
-  return (int)sizeof(T) * CHUNK * ((state_only ? 1 : 2) * (DA + pad) + DC + pad) + (state_only ? 0 : 10 * 64 * (int)sizeof(typename Kind<T>::frag)) + 16;
+struct Shape {
+  static constexpr int PLANES = Kind<T>::planes, ROWS = PLANES == 3 && (DA == 128 || DC == 128) ? 32 : 64;
+  static constexpr int CB = PLANES == 1 && DC == 128 ? 2 : 1, WAVES = DC / 16 / CB, THREADS = 64 * WAVES;
+  static constexpr int IB = ROWS / 16, BLOCKS = IB * (IB + 1) / 2;  // 16 x 16 blocks on and below the diagonal
+  static constexpr int WEIGHTS = BLOCKS * 64 * PLANES;              // quads
+  static constexpr int threads(int mode) { return mode == PAIR ? 2 * THREADS : THREADS; }
+  static constexpr int lds(int mode) {
+    const int a = Tile<ROWS, DA, PLANES>::SIZE, c = Tile<ROWS, DC, PLANES>::SIZE;
+    return (int)sizeof(bf16) * (mode == PAIR ? 2 * (a + c) : mode == MIX ? 2 * a + c : a + c) + (mode == STATE ? 0 : WEIGHTS * 8 * (mode == PAIR ? 2 : 1)) + 16;
+  }
+};
+
+__device__ __forceinline__ int length_of(const DecayMix& P, long long batch) {
+  if (!P.lengths) return P.T;
+  const int given = P.lengths[batch];
+  return given < 0 ? 0 : given < P.T ? given : P.T;
 }
 
 // A product that sums over frames j meets c_j = 0 * x where its weight is zero (j after i): an infinity or a NaN there would reach frames before its own.  It is
 // taken out of the tile, and every frame from its own on is NaN, as is the state.
-template <typename T, int DA, int DC, bool STATE_ONLY>
-__global__ __launch_bounds__(THREADS, 2) void decay_mix_kernel(DecayMix P) {
-  typedef Kind<T> K;
-  typedef typename K::frag frag;
-  constexpr int PA = DA + K::pad, PC = DC + K::pad, RB = DA / 16, CB = DC / 16 / WAVES, IB = CHUNK / 16;
+template <typename T, int DA, int DC, int PLANES, int MODE, bool REVERSE, bool FULL>
+__global__ __launch_bounds__((Shape<T, DA, DC>::threads(MODE)), 2) void decay_mix_kernel(DecayMix P) {
+  static_assert(MODE != PAIR || DA == DC, "both halves run the same sizes");
+  typedef Shape<T, DA, DC> S;
+  constexpr int NP = S::PLANES, ROWS = S::ROWS, CB = S::CB, WAVES = S::WAVES, THREADS = S::THREADS, IB = S::IB, RB = DA / 16;
+  typedef Tile<ROWS, DA, NP> TileA;
+  typedef Tile<ROWS, DC, NP> TileC;
   extern __shared__ __align__(16) unsigned char lds[];
-  T* tile_b = reinterpret_cast<T*>(lds);
-  T* tile_c = tile_b + CHUNK * PA;
-  T* tile_a = tile_c + CHUNK * PC;  // (not there where the state alone is summed)
-  frag* weights = reinterpret_cast<frag*>(tile_a + CHUNK * PA);
-  int* bad_row = reinterpret_cast<int*>(STATE_ONLY ? reinterpret_cast<unsigned char*>(tile_a) : reinterpret_cast<unsigned char*>(weights + 10 * 64));
+  const int thread = threadIdx.x & (THREADS - 1), lane = thread & 63, li = lane & 15, lg = lane >> 4;
+  const int wave = uniform(thread >> 6);
+  const bool second = MODE == PAIR && uniform((int)threadIdx.x / THREADS) != 0;
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, lg = lane >> 4;
-  const int segment = blockIdx.x % P.segments;
-  if (STATE_ONLY && segment == P.segments - 1) return;  // nothing comes after it
-  const long long bh = blockIdx.x / P.segments;
-  const long long batch = bh / P.H;
-  const int head = (int)(bh % P.H);
-  const bool reverse = P.reverse;
-  long long n = P.T;
-  if (P.lengths) {
-    const long long given = P.lengths[batch];
-    n = given < 0 ? 0 : given < n ? given : n;
+  bf16* const tiles = reinterpret_cast<bf16*>(lds);
+  bf16* tile_b = tiles;
+  bf16* tile_c = tiles + TileA::SIZE;
+  bf16* tile_a = tile_c + TileC::SIZE;  // (not there where the state alone is summed)
+  bf16x4* weights = reinterpret_cast<bf16x4*>(tile_a + TileA::SIZE * (MODE == PAIR ? 2 : MODE == MIX ? 1 : 0));
+  int* const bad_row = reinterpret_cast<int*>(weights + (MODE == STATE ? 0 : S::WEIGHTS * (MODE == PAIR ? 2 : 1)));
+  if (second) {
+    bf16* const b = tile_b;
+    tile_b = tile_c;
+    tile_c = b;
+    tile_a += TileA::SIZE;
+    weights += S::WEIGHTS;
   }
-  const float log2_decay = log2_of(P.decay[head]);
-  const T* a = static_cast<const T*>(P.a) + batch * P.a_b + head * P.a_h;
-  const T* b = static_cast<const T*>(P.b) + batch * P.b_b + head * P.b_h;
-  const T* c = static_cast<const T*>(P.c) + batch * P.c_b + head * P.c_h;
+
+  // (a quotient is computed a lane at a time: unless it is taken back to a scalar register, all that follows of it is kept for every lane)
+  const int workgroup = blockIdx.x, of_head = uniform(workgroup / P.segments), segment = workgroup - of_head * P.segments;
+  if (MODE == STATE && segment == P.segments - 1) return;  // nothing comes after it
+  const int of_batch = uniform(of_head / P.H), head = of_head - of_batch * P.H;
+  const long long bh = of_head, batch = of_batch;
+  const int n = uniform(length_of(P, batch)), all = P.T;
+  const float log2_decay = uniform(log2_of(P.decay[head]));
+  const int da = second ? P.dc : P.da, dc = second ? P.da : P.dc;
+  const bool transposed = second || P.transposed;
   const int column0 = wave * CB * 16;
 
   // the state: rows 16 r + 4 lg .. + 3 of column column0 + 16 m + li
   f32x4 state[RB][CB];
-  float* part = P.parts + (bh * P.segments + segment) * (DA * DC);
+  float* const part = P.parts + (bh * P.segments + segment) * P.part_size;
 #pragma unroll
   for (int r = 0; r < RB; ++r)
 #pragma unroll
     for (int m = 0; m < CB; ++m) {
       state[r][m] = 0.f;
-      if (STATE_ONLY) continue;
+      if (MODE == STATE) continue;
+      const int column = column0 + m * 16 + li, row = r * 16 + lg * 4;
       if (P.segments > 1) {
-        state[r][m] = *reinterpret_cast<const f32x4*>(part + ((r * CB + m) * THREADS + threadIdx.x) * 4);
-      } else if (P.first) {
-        const int column = column0 + m * 16 + li;
+        if (row < da && column < dc) {
+          if (transposed) {
+            state[r][m] = *reinterpret_cast<const f32x4*>(part + column * P.part_pitch + row);
+          } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = r * 16 + lg * 4 + e;
-          if (row < P.da && column < P.dc)
-            state[r][m][e] = P.first[bh * P.da * P.dc + (P.transposed ? (long long)column * P.da + row : (long long)row * P.dc + column)] * P.first_factor;
+            for (int e = 0; e < 4; ++e) state[r][m][e] = part[(row + e) * P.part_pitch + column];
+          }
         }
+      } else if (P.first) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (row + e < da && column < dc)
+            state[r][m][e] = P.first[bh * da * dc + (transposed ? column * da + row + e : (row + e) * dc + column)] * P.first_factor;
       }
     }
 
-  const long long chunks = (P.T + CHUNK - 1) / CHUNK;
-  const long long from = (long long)segment * P.segment_chunks;
-  const long long to = from + P.segment_chunks < chunks ? from + P.segment_chunks : chunks;
-
-  Rows<T, DA> ra, rb;
-  Rows<T, DC> rc;
-  if (from < to && from * CHUNK < n) {
-    if (!STATE_ONLY) ra.load(a, P.a_t, from * CHUNK, n, reverse, P.da);
-    rb.load(b, P.b_t, from * CHUNK, n, reverse, P.da);
-    rc.load(c, P.c_t, from * CHUNK, n, reverse, P.dc);
-  }
-  for (long long chunk = from; chunk < to; ++chunk) {
-    const long long u0 = chunk * CHUNK;
-    T* out = static_cast<T*>(P.out) + (batch * P.T * P.H + head) * P.dc;
-    if (u0 >= n) {  // past the sequence's end
-      if (!STATE_ONLY)
-        for (int at = threadIdx.x; at < CHUNK * P.dc; at += THREADS)
-          if (u0 + at / P.dc < P.T) out[(u0 + at / P.dc) * P.H * P.dc + at % P.dc] = (T)0;
-      continue;
-    }
-    const int here = (int)(n - u0 < CHUNK ? n - u0 : CHUNK);
-    int* bad_here = bad_row + (chunk & 1);  // two in turn: a wave may still read the last chunk's
-    if (threadIdx.x == 0) *bad_here = CHUNK;
-    __syncthreads();
-    if (!STATE_ONLY) ra.store(tile_a);
-    rb.store(tile_b);
-    const int bad = rc.clean();
-    if (bad < CHUNK) atomicMin(bad_here, bad);
-    rc.store(tile_c);
-    __syncthreads();
-    const int first_bad = *bad_here;
-    if (chunk + 1 < to && u0 + CHUNK < n) {
-      if (!STATE_ONLY) ra.load(a, P.a_t, u0 + CHUNK, n, reverse, P.da);
-      rb.load(b, P.b_t, u0 + CHUNK, n, reverse, P.da);
-      rc.load(c, P.c_t, u0 + CHUNK, n, reverse, P.dc);
-    }
-    if constexpr (!STATE_ONLY) {
-      // the weights l^(i-j) (a_i . b_j) of the ten blocks on and below the diagonal, as (j, i): the operand of frame i's sum over j
+  // powers of the decay that every whole chunk takes, as a lane's own times the block's: of the weights (on the diagonal; one block below it), of the first
+  // state, and of a frame's product in the next state
+  f32x4 on_diagonal, below, left;
 #pragma unroll
-      for (int k = 0; k < 3; ++k) {
+  for (int e = 0; e < 4; ++e) {
+    const int apart = li - lg * 4 - e;
+    on_diagonal[e] = power(log2_decay, apart < 0 ? 0 : apart) * P.factor;
+    below[e] = power(log2_decay, 16 + apart) * P.factor;
+    left[e] = power(log2_decay, 15 - lg * 4 - e + (REVERSE ? 1 : 0));
+  }
+  const float since = power(log2_decay, li + (REVERSE ? 0 : 1)) * P.factor;
+  const float power16 = uniform(power(log2_decay, 16)), power32 = uniform(power(log2_decay, 32)), power48 = uniform(power(log2_decay, 48));
+  const float carry_whole = uniform(power(log2_decay, ROWS));
+  auto block_power = [&](int i) { return i == 0 ? 1.f : here_only(i == 1 ? power16 : i == 2 ? power32 : power48); };
+
+  // between memory and LDS: a, b and c; of a pair, the first half of the threads a and b, the second a2 and c
+  Rows<T, ROWS, DA, THREADS, FULL, REVERSE> ra, rb;
+  Rows<T, ROWS, DC, THREADS, FULL, REVERSE> rc;
+  const T* const a = (second ? static_cast<const T*>(P.a2) + batch * P.a2_b + head * P.a2_h : static_cast<const T*>(P.a) + batch * P.a_b + head * P.a_h);
+  const T* const b = (second ? static_cast<const T*>(P.c) + batch * P.c_b + head * P.c_h : static_cast<const T*>(P.b) + batch * P.b_b + head * P.b_h);
+  const T* const c = static_cast<const T*>(P.c) + batch * P.c_b + head * P.c_h;
+  const int step_a = (int)(second ? P.a2_t : P.a_t), step_b = (int)(second ? P.c_t : P.b_t), step_c = (int)P.c_t;
+  auto load = [&](int u0) {
+    const int here = n - u0 < ROWS ? n - u0 : ROWS;
+    const long long t = REVERSE ? n - u0 - here : u0;
+    if (MODE != STATE) ra.load(a + t * step_a, step_a, here, da, thread);
+    rb.load(b + t * step_b, step_b, here, da, thread);
+    if (MODE != PAIR) rc.load(c + t * step_c, step_c, here, dc, thread);
+  };
+
+  // a chunk's outputs, written behind the next chunk's first barriers: the wait for what is loaded is then no wait for them
+  typedef T quad __attribute__((ext_vector_type(4)));
+  T* const out = static_cast<T*>(second ? P.out2 : P.out) + (batch * all * P.H + head) * dc;
+  const int out_step = P.H * dc;
+  quad done[IB][CB];
+  int done_u0 = -1;
+  auto write = [&]() {
+    typedef T quad_anywhere __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    const int here = n - done_u0 < ROWS ? n - done_u0 : ROWS;
+    const int lane_row = here_only(li), lane_column = column0 + here_only(lg) * 4;
+#pragma unroll
+    for (int i = 0; i < IB; ++i) {
+      const int u = i * 16 + lane_row;
+      if (here < ROWS && done_u0 + u >= all) continue;
+      const long long t = REVERSE && u < here ? n - 1 - (done_u0 + u) : done_u0 + u;
+      T* const row = out + t * out_step + lane_column;
+#pragma unroll
+      for (int m = 0; m < CB; ++m) {
+        if (FULL || lane_column + m * 16 + 4 <= dc) {
+          *reinterpret_cast<quad_anywhere*>(row + m * 16) = done[i][m];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (lane_column + m * 16 + e < dc) row[m * 16 + e] = done[i][m][e];
+        }
+      }
+    }
+  };
+
+  // a segment's frames; the kernel's own chunks divide its
+  const int from = segment * P.segment_chunks * CHUNK, left_frames = all - from;
+  const int to = left_frames < P.segment_chunks * CHUNK ? all : from + P.segment_chunks * CHUNK;
+  const int real_to = to < n ? to : n;
+  if (from < real_to) load(from);
+  for (int u0 = from; u0 < real_to; u0 += ROWS) {
+    const int here = n - u0 < ROWS ? n - u0 : ROWS;
+    int* bad_here = bad_row + (u0 / ROWS & 1);  // two in turn: a wave may still read the last chunk's
+    if (threadIdx.x == 0) *bad_here = ROWS;
+    __syncthreads();
+    // tile_b of a pair's half is the other's c
+    if (MODE != STATE) ra.store(tile_a, here, da, thread);
+    const int bad = MODE == PAIR ? rb.clean(here, thread) : rc.clean(here, thread);
+    rb.store(tile_b, here, da, thread);
+    if (MODE != PAIR) rc.store(tile_c, here, dc, thread);
+    if (bad < ROWS) atomicMin(bad_here, bad);
+    __syncthreads();
+    const int first_bad = uniform(*bad_here);
+    if (MODE != STATE && done_u0 >= 0) write();
+    if (u0 + ROWS < real_to) load(u0 + ROWS);
+    f32x4 o[IB][CB];
+    if constexpr (MODE != STATE) {
+      // the weights l^(i-j) (a_i . b_j) of the blocks on and below the diagonal, as (j, i): the operand of frame i's sum over j
+#pragma unroll
+      for (int k = 0; k < (S::BLOCKS + WAVES - 1) / WAVES; ++k) {
         const int block = wave + k * WAVES;
-        if (block < 10) {
+        if (block < S::BLOCKS) {
           const int ib = block >= 6 ? 3 : block >= 3 ? 2 : block >= 1 ? 1 : 0, jb = block - ib * (ib + 1) / 2;
           f32x4 s = 0.f;
 #pragma unroll
           for (int d = 0; d < DA; d += 32) {
-            frag b0, b1, a0, a1;
-            K::row8(tile_b + (jb * 16 + li) * PA + d + lg * 8, b0, b1);
-            K::row8(tile_a + (ib * 16 + li) * PA + d + lg * 8, a0, a1);
-            s = K::mma(b0, b1, a0, a1, s);
+            bf16x8 vb[NP], va[NP];
+            TileA::rows8(tile_b, jb * 16, d, li, lg, vb);
+            TileA::rows8(tile_a, ib * 16, d, li, lg, va);
+            s = mma(vb, va, s);
           }
-          const int apart = (ib - jb) * 16 + li - lg * 4;
+          if (ib == jb) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[e] = apart - e < 0 ? 0.f : s[e] * power(log2_decay, apart - e);
-          weights[block * 64 + lane] = K::round(s);
+            for (int e = 0; e < 4; ++e) s[e] = li < lg * 4 + e ? 0.f : s[e] * on_diagonal[e];  // a frame after this one has no part, whatever it is
+          } else {
+            s *= below * block_power(ib - jb - 1);
+          }
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const bf16x4 w = __builtin_convertvector(s, bf16x4);
+            weights[(block * NP + p) * 64 + lane] = w;
+            s -= __builtin_convertvector(w, f32x4);
+          }
         }
       }
-      __syncthreads();
-    }
-    frag cf[IB][CB];
-#pragma unroll
-    for (int j = 0; j < IB; ++j)
-#pragma unroll
-      for (int m = 0; m < CB; ++m) cf[j][m] = K::column(tile_c, PC, j * 16, column0 + m * 16, lane);
-    if constexpr (!STATE_ONLY) {
-      // out, as (column, frame): l^(i+1) (a S) + weights c
-      f32x4 o[IB][CB];
+      // out, as (column, frame): l^(i+1) (a S) ...
 #pragma unroll
       for (int i = 0; i < IB; ++i)
 #pragma unroll
         for (int m = 0; m < CB; ++m) o[i][m] = 0.f;
 #pragma unroll
       for (int r = 0; r < RB; r += 2) {
-        frag s0[CB], s1[CB];
+        bf16x8 vs[CB][NP];
 #pragma unroll
-        for (int m = 0; m < CB; ++m) {
-          s0[m] = K::round(state[r][m]);
-          s1[m] = K::round(state[r + 1][m]);
-        }
+        for (int m = 0; m < CB; ++m) split(state[r][m], state[r + 1][m], vs[m]);
 #pragma unroll
         for (int i = 0; i < IB; ++i) {
-          const T* p = tile_a + (i * 16 + li) * PA + r * 16 + lg * 4;
-          const frag a0 = K::row4(p), a1 = K::row4(p + 16);
+          bf16x8 va[NP];
+          TileA::rows4(tile_a, i * 16, r * 16, li, lg, va);
 #pragma unroll
-          for (int m = 0; m < CB; ++m) o[i][m] = K::mma(s0[m], s1[m], a0, a1, o[i][m]);
+          for (int m = 0; m < CB; ++m) o[i][m] = mma(vs[m], va, o[i][m]);
         }
       }
-      const frag zero = {};
 #pragma unroll
-      for (int i = 0; i < IB; ++i) {
-        const float since = power(log2_decay, i * 16 + li + (reverse ? 0 : 1));
+      for (int i = 0; i < IB; ++i)
 #pragma unroll
-        for (int m = 0; m < CB; ++m) o[i][m] *= since;
-#pragma unroll
-        for (int j = 0; j <= i; j += 2) {
-          const frag w0 = weights[(i * (i + 1) / 2 + j) * 64 + lane];
-          const frag w1 = j + 1 <= i ? weights[(i * (i + 1) / 2 + j + 1) * 64 + lane] : zero;
-#pragma unroll
-          for (int m = 0; m < CB; ++m) o[i][m] = K::mma(cf[j][m], j + 1 <= i ? cf[j + 1][m] : zero, w0, w1, o[i][m]);
-        }
-        const int u = i * 16 + li;
-        if (u0 + u < P.T) {
-          T* row = out + (reverse && u < here ? n - 1 - (u0 + u) : u0 + u) * P.H * P.dc;
-#pragma unroll
-          for (int m = 0; m < CB; ++m) {
-            const int column = column0 + m * 16 + lg * 4;
-            f32x4 v = o[i][m] * P.factor;
-            if (u >= here) v = 0.f;
-            else if (u >= first_bad) v = __builtin_nanf("");
-            typedef T quad __attribute__((ext_vector_type(4)));
-            typedef T quad_anywhere __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-            const quad w = __builtin_convertvector(v, quad);
-            if (column + 4 <= P.dc) {
-              *reinterpret_cast<quad_anywhere*>(row + column) = w;
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (column + e < P.dc) row[column + e] = w[e];
-            }
-          }
-        }
-      }
+        for (int m = 0; m < CB; ++m) o[i][m] *= since * block_power(i);
+      __syncthreads();
     }
-    // S' = l^n S + sum over j of b_j^T (l^(n-1-j) c_j): the scaled c as the sum of three operands, so that the state is as exact as its float32 sums
-    const float carry = power(log2_decay, here);
+    const float carry = here == ROWS ? carry_whole : power(log2_decay, here);
 #pragma unroll
     for (int r = 0; r < RB; ++r)
 #pragma unroll
       for (int m = 0; m < CB; ++m) state[r][m] *= carry;
 #pragma unroll
     for (int j = 0; j < IB; j += 2) {
-      frag s0[CB][K::planes], s1[CB][K::planes];
+      bf16x8 vc[CB][NP];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        f32x4 left;
+      for (int m = 0; m < CB; ++m) TileC::columns(tile_c, j * 16, column0 + m * 16, lane, vc[m]);
+      if constexpr (MODE != STATE) {
+        // ... + weights c
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int after = here - 1 - ((j + half) * 16 + lg * 4 + e);
-          left[e] = after < 0 ? 0.f : power(log2_decay, after + (reverse ? 1 : 0));
+        for (int i = j; i < IB; ++i) {
+          bf16x8 vw[NP];
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            const bf16x4 zero = {};
+            const int block = i * (i + 1) / 2 + j;
+            vw[p] = join(weights[(block * NP + p) * 64 + lane], j < i ? weights[((block + 1) * NP + p) * 64 + lane] : zero);
+          }
+#pragma unroll
+          for (int m = 0; m < CB; ++m) o[i][m] = mma(vc[m], vw, o[i][m]);
         }
+      }
+      // S' = l^n S + sum over j of b_j^T (l^(n-1-j) c_j): the scaled c as the sum of PLANES operands
+      bf16x8 vs[CB][PLANES];
+      f32x4 weight[2];
 #pragma unroll
-        for (int m = 0; m < CB; ++m) K::split(__builtin_convertvector(cf[j + half][m], f32x4) * left, half ? s1[m] : s0[m]);
+      for (int h = 0; h < 2; ++h) {
+        weight[h] = left * block_power(IB - 1 - j - h);
+        if (here < ROWS) {
+          const int lane_row = here_only(lg) * 4;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int after = here - 1 - ((j + h) * 16 + lane_row + e);
+            weight[h][e] = after < 0 ? 0.f : power(log2_decay, after + (REVERSE ? 1 : 0));
+          }
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < CB; ++m) {
+        f32x8 v = 0.f;
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p) v += __builtin_convertvector(vc[m][p], f32x8);
+        split(__builtin_shufflevector(v, v, 0, 1, 2, 3) * weight[0], __builtin_shufflevector(v, v, 4, 5, 6, 7) * weight[1], vs[m]);
       }
 #pragma unroll
       for (int r = 0; r < RB; ++r) {
-        const frag b0 = K::column(tile_b, PA, j * 16, r * 16, lane), b1 = K::column(tile_b, PA, j * 16 + 16, r * 16, lane);
+        bf16x8 vb[NP];
+        TileA::columns(tile_b, j * 16, r * 16, lane, vb);
 #pragma unroll
-        for (int m = 0; m < CB; ++m)
-#pragma unroll
-          for (int p = K::planes - 1; p >= 0; --p) state[r][m] = K::mma(b0, b1, s0[m][p], s1[m][p], state[r][m]);
+        for (int m = 0; m < CB; ++m) state[r][m] = mma(vb, vs[m], state[r][m]);
       }
     }
-    if (first_bad < CHUNK)
+    if constexpr (MODE != STATE) {
+      if (here < ROWS || first_bad < ROWS)
+#pragma unroll
+        for (int i = 0; i < IB; ++i) {
+          const int u = i * 16 + here_only(li);
+#pragma unroll
+          for (int m = 0; m < CB; ++m) o[i][m] = u >= here ? (f32x4)0.f : u >= first_bad ? o[i][m] * here_only(__builtin_nanf("")) : o[i][m];
+        }
+#pragma unroll
+      for (int i = 0; i < IB; ++i)
+#pragma unroll
+        for (int m = 0; m < CB; ++m) done[i][m] = __builtin_convertvector(o[i][m], quad);
+      done_u0 = u0;
+    }
+    if (first_bad < ROWS)
 #pragma unroll
       for (int r = 0; r < RB; ++r)
 #pragma unroll
-        for (int m = 0; m < CB; ++m) state[r][m] = __builtin_nanf("");
+        for (int m = 0; m < CB; ++m) state[r][m] *= here_only(__builtin_nanf(""));
   }
 
-  if (STATE_ONLY) {
+  if (MODE != STATE) {
+    if (done_u0 >= 0) write();
+    // past the sequence's end, from the first frame that no chunk held
+    const int lane_column = thread % (DC / 4) * 4;
+    for (int u = (done_u0 >= 0 ? done_u0 + ROWS : from > n ? from : n) + thread / (DC / 4); u < to; u += THREADS / (DC / 4)) {
+      T* const row = out + (long long)u * out_step + lane_column;
 #pragma unroll
-    for (int r = 0; r < RB; ++r)
-#pragma unroll
-      for (int m = 0; m < CB; ++m) *reinterpret_cast<f32x4*>(part + ((r * CB + m) * THREADS + threadIdx.x) * 4) = state[r][m];
-  } else if (P.last && segment == P.segments - 1) {
-#pragma unroll
-    for (int r = 0; r < RB; ++r)
-#pragma unroll
-      for (int m = 0; m < CB; ++m) {
-        const int column = column0 + m * 16 + li;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = r * 16 + lg * 4 + e;
-          if (row < P.da && column < P.dc)
-            P.last[bh * P.da * P.dc + (P.transposed ? (long long)column * P.da + row : (long long)row * P.dc + column)] = state[r][m][e] * P.last_factor;
-        }
-      }
+      for (int e = 0; e < 4; ++e)
+        if (lane_column + e < dc) row[e] = (T)0;
+    }
+    if (second || !P.last || segment != P.segments - 1) return;
   }
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int m = 0; m < CB; ++m) {
+      const int column = column0 + m * 16 + li, row = r * 16 + lg * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (MODE == STATE)
+          part[(row + e) * P.part_pitch + column] = state[r][m][e];
+        else if (row + e < da && column < dc)
+          P.last[bh * da * dc + (transposed ? column * da + row + e : (row + e) * dc + column)] = state[r][m][e] * P.last_factor;
+      }
+    }
 }
 
-// parts[s]: from each segment's own state to the state before it, in order
-template <int DA, int DC>
+// parts[s]: from each segment's own state to the state before it, in order; four values of a (sequence, head) to a thread, JOIN_AHEAD segments read before the
+// first of them is written
+constexpr int JOIN_AHEAD = 16;
 __global__ __launch_bounds__(256) void decay_join_kernel(DecayMix P) {
-  constexpr int CB = DC / 16 / WAVES, WGS = DA * DC / 1024;
-  const long long bh = blockIdx.x / WGS, batch = bh / P.H;
-  const int quad = blockIdx.x % WGS, r = quad / CB, m = quad % CB;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, column = wave * CB * 16 + m * 16 + (lane & 15);
-  long long n = P.T;
-  if (P.lengths) {
-    const long long given = P.lengths[batch];
-    n = given < 0 ? 0 : given < n ? given : n;
-  }
-  const float log2_decay = log2_of(P.decay[bh % P.H]);
+  const int workgroups = P.part_size / 1024, of_head = uniform((int)blockIdx.x / workgroups);
+  const int at = ((int)blockIdx.x - of_head * workgroups) * 1024 + threadIdx.x * 4, row = at / P.part_pitch, column = at % P.part_pitch;
+  const long long bh = of_head;
+  const int n = uniform(length_of(P, of_head / P.H)), frames = P.segment_chunks * CHUNK;
+  const float log2_decay = log2_of(P.decay[of_head % P.H]), whole = power(log2_decay, frames);
   f32x4 s = 0.f;
-  if (P.first)
+  if (P.first && row < P.da)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int row = r * 16 + (lane >> 4) * 4 + e;
-      if (row < P.da && column < P.dc)
-        s[e] = P.first[bh * P.da * P.dc + (P.transposed ? (long long)column * P.da + row : (long long)row * P.dc + column)] * P.first_factor;
-    }
-  float* at = P.parts + bh * P.segments * (DA * DC) + (quad * THREADS + threadIdx.x) * 4;
-  const long long frames = (long long)P.segment_chunks * CHUNK;
-  for (int i = 0; i < P.segments; ++i, at += DA * DC) {
-    f32x4 own = 0.f;
-    if (i + 1 < P.segments) own = *reinterpret_cast<const f32x4*>(at);
-    *reinterpret_cast<f32x4*>(at) = s;
-    const long long left = n - i * frames, here = left < 0 ? 0 : left < frames ? left : frames;
-    s = s * __builtin_amdgcn_exp2f(log2_decay * (float)here) + own;
+    for (int e = 0; e < 4; ++e)
+      if (column + e < P.dc) s[e] = P.first[(bh * P.da + row) * P.dc + column + e] * P.first_factor;
+  float* part = P.parts + bh * P.segments * P.part_size + at;
+  for (int i = 0; i < P.segments; i += JOIN_AHEAD) {
+    f32x4 own[JOIN_AHEAD];
+#pragma unroll
+    for (int k = 0; k < JOIN_AHEAD; ++k)
+      if (i + k + 1 < P.segments) own[k] = *reinterpret_cast<const f32x4*>(part + (long long)(i + k) * P.part_size);
+#pragma unroll
+    for (int k = 0; k < JOIN_AHEAD; ++k)
+      if (i + k < P.segments) {
+        *reinterpret_cast<f32x4*>(part + (long long)(i + k) * P.part_size) = s;
+        const long long left = n - (long long)(i + k) * frames;
+        if (i + k + 1 < P.segments) s = s * (left >= frames ? whole : power(log2_decay, left < 0 ? 0 : (int)left)) + own[k];
+      }
   }
 }
 
@@ -495,49 +650,65 @@ hipError_t by_heads(int da, int dc, F fn) {
   return fn(std::integral_constant<int, 128>(), std::integral_constant<int, 128>());
 }
 
-template <typename T, int DA, int DC, bool STATE_ONLY>
-hipError_t mix_init() {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(&decay_mix_kernel<T, DA, DC, STATE_ONLY>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             mix_lds<T, DA, DC>(STATE_ONLY));
+// planes of a state's new products: where a state is given back it is as exact as its float32 sums; where it only meets frames again, rounded to the
+// inputs' type, two are more than that holds
+template <typename T, bool GIVEN>
+constexpr int planes_of() { return sizeof(T) == 4 || GIVEN ? 3 : 2; }
+
+template <typename T, int DA, int DC, bool GIVEN, int MODE, bool REVERSE, bool FULL>
+hipError_t run_mix(const DecayMix& P, int workgroups, hipStream_t stream) {
+  typedef Shape<T, DA, DC> S;
+  const auto kernel = &decay_mix_kernel<T, DA, DC, planes_of<T, GIVEN>(), MODE, REVERSE, FULL>;
+  if (workgroups < 0) return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds(MODE));
+  hipLaunchKernelGGL(kernel, dim3(workgroups), dim3(S::threads(MODE)), S::lds(MODE), stream, P);
+  return hipGetLastError();
 }
+template <typename F>
+hipError_t by_bool(bool v, F fn) { return v ? fn(std::true_type()) : fn(std::false_type()); }
 
 template <typename T>
-hipError_t launch_mix(const DecayMix& P, hipStream_t stream) {
-  return by_heads(P.da, P.dc, [&](auto a, auto c) {
+hipError_t launch_mode(const DecayMix& P, int mode, bool given, int workgroups, hipStream_t stream) {
+  const int da = mode == PAIR ? std::max(P.da, P.dc) : P.da, dc = mode == PAIR ? da : P.dc;
+  return by_heads(da, dc, [&](auto a, auto c) {
     constexpr int DA = a.value, DC = c.value;
-    const unsigned grid = (unsigned)(P.B * P.H * P.segments);
-    if (P.segments > 1) {
-      hipLaunchKernelGGL((decay_mix_kernel<T, DA, DC, true>), dim3(grid), dim3(THREADS), (mix_lds<T, DA, DC>(true)), stream, P);
-      hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((decay_join_kernel<DA, DC>), dim3((unsigned)(P.B * P.H * (DA * DC / 1024))), dim3(256), 0, stream, P);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((decay_mix_kernel<T, DA, DC, false>), dim3(grid), dim3(THREADS), (mix_lds<T, DA, DC>(false)), stream, P);
-    return hipGetLastError();
+    return by_bool(P.da == DA && P.dc == DC, [&](auto full) {
+      return by_bool(given || sizeof(T) == 4, [&](auto exact) {
+        constexpr bool FULL = full.value, GIVEN = exact.value;
+        if constexpr (sizeof(T) == 4 && !GIVEN) return hipErrorInvalidValue;
+        else {
+          if constexpr (DA == DC)
+            if (mode == PAIR) return run_mix<T, DA, DC, GIVEN, PAIR, true, FULL>(P, workgroups, stream);
+          if (mode == STATE)
+            return by_bool(P.reverse != 0, [&](auto reverse) { return run_mix<T, DA, DC, GIVEN, STATE, reverse.value, FULL>(P, workgroups, stream); });
+          return run_mix<T, DA, DC, GIVEN, MIX, false, FULL>(P, workgroups, stream);
+        }
+      });
+    });
   });
 }
+hipError_t launch_mode(const DecayMix& P, int type, int mode, bool given, int workgroups, hipStream_t stream) {
+  return type == NNA_F32 ? launch_mode<float>(P, mode, given, workgroups, stream) : launch_mode<bf16>(P, mode, given, workgroups, stream);
+}
+
+int padded(int d) { return d <= 64 ? 64 : 128; }
 
 }  // namespace
 
 hipError_t decay_kernels_init() {
-  for (int da : {64, 128})
-    for (int dc : {64, 128}) {
-      const hipError_t e = by_heads(da, dc, [&](auto a, auto c) {
-        constexpr int A = a.value, C = c.value;
-        hipError_t e = mix_init<bf16, A, C, false>();
-        if (e == hipSuccess) e = mix_init<bf16, A, C, true>();
-        if (e == hipSuccess) e = mix_init<float, A, C, false>();
-        if (e == hipSuccess) e = mix_init<float, A, C, true>();
-        return e;
-      });
-      if (e != hipSuccess) return e;
-    }
+  DecayMix P = {};
+  for (int type : {NNA_F32, NNA_BF16})
+    for (int mode : {MIX, STATE, PAIR})
+      for (int all = 0; all < 32; ++all) {
+        P.da = (all & 1 ? 128 : 64) - (all & 4 ? 1 : 0);
+        P.dc = all & 2 ? 128 : 64;
+        P.reverse = all & 8;
+        const hipError_t e = launch_mode(P, type, mode, all & 16, -1, nullptr);
+        if (e != hipSuccess) return e;
+      }
   return hipSuccess;
 }
 
-size_t decay_segments(long long B, long long T, int H, int da, int dc, int* segments, int* chunks) {
+size_t decay_segments(long long B, long long T, int H, int dk, int dv, int* segments, int* chunks) {
   const long long all = std::max(1LL, (T + CHUNK - 1) / CHUNK), heads = std::max(1LL, B * H);
   // two workgroups on each of 256 CUs, segments of four chunks at least
   long long n = std::max(1LL, std::min((512 + heads - 1) / heads, all / 4));
@@ -545,10 +716,25 @@ size_t decay_segments(long long B, long long T, int H, int da, int dc, int* segm
   n = (all + each - 1) / each;
   *segments = (int)n;
   *chunks = (int)each;
-  return n == 1 ? 0 : (size_t)(heads * n) * (da <= 64 ? 64 : 128) * (dc <= 64 ? 64 : 128) * sizeof(float);
+  return n == 1 ? 0 : (size_t)(heads * n) * padded(dk) * padded(dv) * sizeof(float);
 }
 
-hipError_t launch_decay_mix(const DecayMix& P, int type, hipStream_t stream) { return type == NNA_F32 ? launch_mix<float>(P, stream) : launch_mix<bf16>(P, stream); }
+hipError_t launch_decay_states(DecayMix P, int type, bool given, hipStream_t stream) {
+  if (P.segments == 1) return hipSuccess;
+  P.part_pitch = padded(P.dc);
+  P.part_size = padded(P.da) * P.part_pitch;
+  const hipError_t e = launch_mode(P, type, STATE, given, (int)(P.B * P.H * P.segments), stream);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(decay_join_kernel, dim3((unsigned)(P.B * P.H * (P.part_size / 1024))), dim3(256), 0, stream, P);
+  return hipGetLastError();
+}
+
+hipError_t launch_decay_mix(DecayMix P, int type, hipStream_t stream) {
+  const int rows = P.transposed ? P.dc : P.da, columns = P.transposed ? P.da : P.dc;
+  P.part_pitch = padded(columns);
+  P.part_size = padded(rows) * P.part_pitch;
+  return launch_mode(P, type, P.a2 || P.reverse ? PAIR : MIX, P.last != nullptr, (int)(P.B * P.H * P.segments), stream);
+}
 
 hipError_t launch_decay_step(const DecayStep& P, int type, hipStream_t stream) {
   const unsigned grid = (unsigned)(P.B * P.H * ((P.dv + STEP_COLUMNS - 1) / STEP_COLUMNS));

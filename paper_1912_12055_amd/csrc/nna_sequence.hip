@@ -88,8 +88,8 @@ nna_status check_heads(int type, long long B, long long T, long long H, long lon
   if (B < 0 || T < 0 || H < 1 || dk < 1 || dv < 1) return fail(NNA_ERR_SHAPE, "B and T must not be negative, H, dk and dv at least 1");
   if (dk > DECAY_HEAD_MAX || dv > DECAY_HEAD_MAX) return fail(NNA_ERR_UNSUPPORTED, "heads of more than " + std::to_string(DECAY_HEAD_MAX) + " values");
   // a workgroup for each (sequence, head), its segments and its blocks of 1,024 values of a state
-  if (H > (1LL << 24) || B > (1LL << 24) / H) return fail(NNA_ERR_SHAPE, "B H is too large");
-  if (T > (1LL << 36)) return fail(NNA_ERR_SHAPE, "T is too large");
+  if (H > 65536 || B > (1LL << 24) / H) return fail(NNA_ERR_SHAPE, "H or B H is too large");
+  if (T > INT_MAX - 4 * DECAY_CHUNK) return fail(NNA_ERR_SHAPE, "T is too large");
   return NNA_OK;
 }
 
@@ -98,6 +98,14 @@ nna_status check_decay_args(const void* decay, double scale, const void* workspa
   if (!(scale != 0.0) || !(std::fabs(scale) < 1e30) || !(std::fabs(scale) > 1e-30)) return fail(NNA_ERR_INVALID_ARG, "scale must be finite and not 0");
   if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || bytes < need))
     return fail(NNA_ERR_INVALID_ARG, "workspace_dev is NULL, misaligned or smaller than nna_decay_attention_workspace asks for");
+  return NNA_OK;
+}
+
+nna_status check_strides(const long long* const (&strides)[3]) {
+  for (const long long* s : strides) {
+    if (!s) return fail(NNA_ERR_INVALID_ARG, "strides are NULL");
+    if (s[1] < 0 || s[1] > DECAY_STEP_MAX) return fail(NNA_ERR_SHAPE, "more than " + std::to_string(DECAY_STEP_MAX) + " elements from one frame to the next");
+  }
   return NNA_OK;
 }
 
@@ -124,6 +132,13 @@ void set_mix(DecayMix& P, const Heads& a, const Heads& b, const Heads& c) {
   P.c_h = c.strides[2];
   P.da = a.width;
   P.dc = c.width;
+}
+void set_pair(DecayMix& P, const Heads& a2, void* out2) {
+  P.a2 = a2.at;
+  P.a2_b = a2.strides[0];
+  P.a2_t = a2.strides[1];
+  P.a2_h = a2.strides[2];
+  P.out2 = out2;
 }
 
 }  // namespace
@@ -255,7 +270,8 @@ nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, co
                                void* out_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream) {
   nna_status s = check_heads(type, B, T, H, dk, dv);
   if (s != NNA_OK) return s;
-  if (!q_strides || !k_strides || !v_strides) return fail(NNA_ERR_INVALID_ARG, "strides are NULL");
+  s = check_strides({q_strides, k_strides, v_strides});
+  if (s != NNA_OK) return s;
   if (B && T && (!q_dev || !k_dev || !v_dev || !out_dev)) return fail(NNA_ERR_INVALID_ARG, "q_dev / k_dev / v_dev / out_dev is NULL");
   DecayMix P = {};
   s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, decay_segments(B, T, (int)H, (int)dk, (int)dv, &P.segments, &P.segment_chunks));
@@ -270,12 +286,14 @@ nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, co
   P.factor = (float)scale;
   P.first_factor = P.last_factor = 1.f;
   P.B = B;
-  P.T = T;
+  P.T = (int)T;
   P.H = (int)H;
   DeviceGuard guard;
   s = enter_device(guard, device);
   if (s != NNA_OK || !B) return s;
-  const hipError_t e = launch_decay_mix(P, type, static_cast<hipStream_t>(hip_stream));
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipError_t e = launch_decay_states(P, type, last_dev != nullptr, stream);
+  if (e == hipSuccess) e = launch_decay_mix(P, type, stream);
   return e == hipSuccess ? NNA_OK : fail_hip(e, "linear attention");
 }
 
@@ -286,10 +304,12 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
                                         void* gv_dev, float* gfirst_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream) {
   nna_status s = check_heads(type, B, T, H, dk, dv);
   if (s != NNA_OK) return s;
-  if (!q_strides || !k_strides || !v_strides) return fail(NNA_ERR_INVALID_ARG, "strides are NULL");
+  s = check_strides({q_strides, k_strides, v_strides});
+  if (s != NNA_OK) return s;
   if (B && T && (!gout_dev || !q_dev || !k_dev || !v_dev)) return fail(NNA_ERR_INVALID_ARG, "gout_dev / q_dev / k_dev / v_dev is NULL");
-  if (!gq_dev && !gk_dev && !gv_dev && B && T) return fail(NNA_ERR_INVALID_ARG, "no gradient is asked for");
-  if (gfirst_dev && !gk_dev && !gv_dev && B && T) return fail(NNA_ERR_INVALID_ARG, "gfirst_dev comes with gk_dev or gv_dev");
+  if (B && T && !gk_dev != !gv_dev) return fail(NNA_ERR_INVALID_ARG, "gk_dev and gv_dev come together");
+  if (B && T && !gq_dev && !gk_dev) return fail(NNA_ERR_INVALID_ARG, "no gradient is asked for");
+  if (B && T && gfirst_dev && !gk_dev) return fail(NNA_ERR_INVALID_ARG, "gfirst_dev comes with gk_dev and gv_dev");
   DecayMix P = {};
   s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, decay_segments(B, T, (int)H, (int)dk, (int)dv, &P.segments, &P.segment_chunks));
   if (s != NNA_OK) return s;
@@ -300,39 +320,36 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
   P.parts = static_cast<float*>(workspace_dev);
   P.factor = (float)scale;
   P.B = B;
-  P.T = T;
+  P.T = (int)T;
   P.H = (int)H;
   DeviceGuard guard;
   s = enter_device(guard, device);
   if (s != NNA_OK || !B) return s;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   hipError_t e = hipSuccess;
-  if (gq_dev) {
-    set_mix(P, g, v, k);
-    P.out = gq_dev;
+  if (gq_dev) {  // the states of the forward pass, transposed
+    set_mix(P, q, k, v);
     P.first = first_dev;
     P.first_factor = 1.f;
+    e = launch_decay_states(P, type, false, stream);
+    set_mix(P, g, v, k);
+    P.out = gq_dev;
     P.transposed = 1;
-    e = launch_decay_mix(P, type, stream);
+    if (e == hipSuccess) e = launch_decay_mix(P, type, stream);
   }
-  // the state's gradient, without q's scale: the outputs get it at the end, as gfirst does
-  P.reverse = 1;
-  P.first = glast_dev;
-  P.first_factor = (float)(1.0 / scale);
-  P.last = gfirst_dev;
-  P.last_factor = (float)scale;
-  if (gv_dev && e == hipSuccess) {
-    set_mix(P, k, q, g);
-    P.out = gv_dev;
+  if (e == hipSuccess && (gk_dev || gfirst_dev)) {
+    // the state's gradient, without q's scale: the outputs get it at the end, as gfirst does
+    P.reverse = 1;
+    P.first = glast_dev;
+    P.first_factor = (float)(1.0 / scale);
+    P.last = gfirst_dev;
+    P.last_factor = (float)scale;
     P.transposed = 0;
-    e = launch_decay_mix(P, type, stream);
-    P.last = nullptr;
-  }
-  if ((gk_dev || (!T && gfirst_dev)) && e == hipSuccess) {
-    set_mix(P, v, g, q);
-    P.out = gk_dev;
-    P.transposed = 1;
-    e = launch_decay_mix(P, type, stream);
+    set_mix(P, k, q, g);
+    e = launch_decay_states(P, type, gfirst_dev != nullptr, stream);
+    P.out = gv_dev;
+    set_pair(P, v, gk_dev);
+    if (e == hipSuccess) e = launch_decay_mix(P, type, stream);
   }
   return e == hipSuccess ? NNA_OK : fail_hip(e, "linear attention, backward");
 }
