@@ -820,6 +820,20 @@ def nna_backward_kept(plan: Plan, x, gout, kept, want_gmelw=False, want_gw=True,
 NNA_F32, NNA_BF16, NNA_F16 = 0, 1, 2
 NNA_BLOCK8 = 128
 _types = {}
+_current_stream = None
+
+
+def _stream_on(device, stream):
+    """The handle of torch's current stream on `device`, or `stream`.  (These operators' calls take ten microseconds where there is little to do: asking
+    torch for the handle alone takes 0.1 us, for its stream object 2.1.)"""
+    global _current_stream
+    if stream is not None:
+        return stream
+    if _current_stream is None:
+        import torch
+
+        _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _current_stream(device.index)
 
 
 def _type_of(t, name, allowed=("float32", "bfloat16", "float16")):
@@ -842,7 +856,7 @@ def _vector(t, name, shape, device, none=False):
 
     if t is None and none:
         return None
-    if not (isinstance(t, torch.Tensor) and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == tuple(shape) and t.device == device):
+    if not (isinstance(t, torch.Tensor) and t.dtype == torch.float32 and t.is_contiguous() and t.shape == shape and t.device == device):
         raise TypeError(f"{name} must be a contiguous float32 tensor of shape {tuple(shape)} on {device}")
     return t.data_ptr()
 
@@ -905,7 +919,7 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
     shape, width, device = x.shape, x.shape[-1], x.device
     out_dtype = x.dtype if out_dtype is None else out_dtype
     if out is None:
-        out = torch.empty(shape, dtype=out_dtype, device=device)
+        out = torch.empty_like(x, dtype=out_dtype, memory_format=torch.contiguous_format)
     elif not (isinstance(out, torch.Tensor) and out.device == device and out.dtype == out_dtype and out.is_contiguous() and out.shape == shape):
         raise TypeError(f"out must be a contiguous {out_dtype} CUDA tensor of shape {tuple(shape)}")
     yt = _type_of(out, "out")
@@ -921,7 +935,7 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
         kept = NormKept()
         kept.shape, kept.dtype, kept.out_dtype, kept.rows, kept.row_stride = shape, x.dtype, out_dtype, rows, step
         kept.x, kept.stats, kept.codes, kept.scales = x if keep == 32 else None, stats, codes, scales
-    sp, st = stats.data_ptr() if keep else None, _stream_of(x, stream)
+    sp, st = stats.data_ptr() if keep else None, _stream_on(x.device, stream)
     if step is not None:
         _check(lib().nna_layer_norm(x.data_ptr(), xt, rows, width, step, w, b, eps, out.data_ptr(), yt, sp,
                                     codes.data_ptr() if keep == 8 else None, scales.data_ptr() if keep == 8 else None, device.index, st))
@@ -949,15 +963,15 @@ def nna_layer_norm_backward(gout, kept, weight=None, want_gx=True, want_gw=True,
     B, T = (shape[0], shape[1]) if frames else (0, 0)
     gx = gw = gb = None
     if want_gx:
-        gx = torch.empty((B, width, T), dtype=kept.dtype, device=device).transpose(1, 2) if frames else torch.empty(shape, dtype=kept.dtype, device=device)
+        gx = gout.new_empty((B, width, T), dtype=kept.dtype).transpose(1, 2) if frames else torch.empty_like(gout, dtype=kept.dtype)
     need = 0
     if want_gw:
-        gw, gb = torch.empty((2, width), dtype=torch.float32, device=device).unbind(0)
+        gw, gb = kept.stats.new_empty((2, width)).unbind(0)
         need = nna_layer_norm_backward_workspace(rows, width, B, T)
         workspace = _workspace_on(stream, need, workspace, device)
     ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if want_gw else (None, 0)
     grads = (gx.data_ptr() if want_gx else None, gw.data_ptr() if want_gw else None, gb.data_ptr() if want_gw else None)
-    sp, st = kept.stats.data_ptr(), _stream_of(gout, stream)
+    sp, st = kept.stats.data_ptr(), _stream_on(device, stream)
     if frames:
         _check(lib().nna_layer_norm_frames_backward(gout.data_ptr(), gt, kept.x.data_ptr(), B, width, T, sp, w, *grads, *ws, device.index, st))
     else:
@@ -985,10 +999,10 @@ def nna_pack8(x, stream=None):
     if step is None:
         raise TypeError("x must be rows at one distance from each other")
     width = x.shape[-1]
-    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    scales = torch.empty((*x.shape[:-1], -(-width // NNA_BLOCK8)), dtype=torch.float32, device=x.device)
+    codes = torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format)
+    scales = x.new_empty((*x.shape[:-1], -(-width // NNA_BLOCK8)), dtype=torch.float32)
     _check(lib().nna_pack8(x.data_ptr(), xt, x.numel() // width if width else 0, width, step, codes.data_ptr(), scales.data_ptr(), x.device.index,
-                           _stream_of(x, stream)))
+                           _stream_on(x.device, stream)))
     return codes, scales
 
 
@@ -1001,12 +1015,12 @@ def nna_unpack8(codes, scales, dtype=None, out=None, stream=None):
     width = codes.shape[-1]
     sp = _vector(scales, "scales", (*codes.shape[:-1], -(-width // NNA_BLOCK8)), codes.device)
     if out is None:
-        out = torch.empty(codes.shape, dtype=torch.float32 if dtype is None else dtype, device=codes.device)
+        out = torch.empty_like(codes, dtype=torch.float32 if dtype is None else dtype)
     elif not (out.is_contiguous() and out.shape == codes.shape and out.device == codes.device and dtype in (None, out.dtype)):
         raise TypeError(f"out must be a contiguous CUDA tensor of shape {tuple(codes.shape)}")
     ot = _type_of(out, "out")
     _check(lib().nna_unpack8(codes.data_ptr(), sp, codes.numel() // width if width else 0, width, out.data_ptr(), ot, codes.device.index,
-                             _stream_of(codes, stream)))
+                             _stream_on(codes.device, stream)))
     return out
 
 
@@ -1055,17 +1069,17 @@ def nna_decay_attention(q, k, v, decay, scale=None, state=None, lengths=None, wa
     device = q.device
     dp, sp, lp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device, none=True), _lengths(lengths, B, device)
     if out is None:
-        out = torch.empty((B, T, H, dv), dtype=q.dtype, device=device)
+        out = q.new_empty((B, T, H, dv))
     elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == (B, T, H, dv) and out.device == device):
         raise TypeError(f"out must be a contiguous {q.dtype} tensor of shape {(B, T, H, dv)}")
-    last = torch.empty((B, H, dk, dv), dtype=torch.float32, device=device) if want_state else None
+    last = decay.new_empty((B, H, dk, dv)) if want_state else None
     need = nna_decay_attention_workspace(B, T, H, dk, dv)
     ws = (None, 0)
     if need:
         workspace = _workspace_on(stream, need, workspace, device)
         ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     _check(lib().nna_decay_attention(*args, t, B, T, H, dk, dv, dp, dk**-0.5 if scale is None else scale, lp, sp, last.data_ptr() if want_state else None,
-                                     out.data_ptr(), *ws, device.index, _stream_of(q, stream)))
+                                     out.data_ptr(), *ws, device.index, _stream_on(device, stream)))
     return (out, last) if want_state else out
 
 
@@ -1080,9 +1094,8 @@ def nna_decay_attention_backward(gout, q, k, v, decay, scale=None, state=None, l
     lastp = _vector(gstate, "gstate", (B, H, dk, dv), device, none=True)
     if not (isinstance(gout, torch.Tensor) and gout.dtype == q.dtype and gout.is_contiguous() and tuple(gout.shape) == (B, T, H, dv) and gout.device == device):
         raise TypeError(f"gout must be a contiguous {q.dtype} tensor of shape {(B, T, H, dv)}")
-    gq, gk = (torch.empty((B, T, H, dk), dtype=q.dtype, device=device) for _ in range(2))
-    gv = torch.empty((B, T, H, dv), dtype=q.dtype, device=device)
-    first = torch.empty((B, H, dk, dv), dtype=torch.float32, device=device) if want_gstate else None
+    gq, gk, gv = q.new_empty((B, T, H, dk)), q.new_empty((B, T, H, dk)), torch.empty_like(gout)
+    first = decay.new_empty((B, H, dk, dv)) if want_gstate else None
     need = nna_decay_attention_workspace(B, T, H, dk, dv)
     ws = (None, 0)
     if need:
@@ -1090,7 +1103,7 @@ def nna_decay_attention_backward(gout, q, k, v, decay, scale=None, state=None, l
         ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     _check(lib().nna_decay_attention_backward(gout.data_ptr(), *args, t, B, T, H, dk, dv, dp, dk**-0.5 if scale is None else scale, lp, sp, lastp,
                                               gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), first.data_ptr() if want_gstate else None, *ws,
-                                              device.index, _stream_of(q, stream)))
+                                              device.index, _stream_on(device, stream)))
     return gq, gk, gv, first
 
 
@@ -1102,9 +1115,9 @@ def nna_decay_attention_step(q, k, v, decay, state, scale=None, out=None, stream
     device = q.device
     dp, sp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device)
     if out is None:
-        out = torch.empty((B, H, dv), dtype=q.dtype, device=device)
+        out = q.new_empty((B, H, dv))
     elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == (B, H, dv) and out.device == device):
         raise TypeError(f"out must be a contiguous {q.dtype} tensor of shape {(B, H, dv)}")
     _check(lib().nna_decay_attention_step(*args, t, B, H, dk, dv, dp, dk**-0.5 if scale is None else scale, sp, out.data_ptr(), device.index,
-                                          _stream_of(q, stream)))
+                                          _stream_on(device, stream)))
     return out

@@ -7,7 +7,7 @@ namespace nna {
 
 constexpr int NORM_BLOCK8 = 128;          // neighbours of a row that share a scale
 constexpr int NORM_WIDTH_MAX = 16384;     // values of a row that a workgroup holds in registers
-constexpr int NORM_FRAMES_WIDTH_MAX = 2112;  // ... of a frame that a lane's 33 columns cover
+constexpr int NORM_FRAMES_WIDTH_MAX = 2112;  // ... of a frame, eight of which fit half a CU's LDS
 
 struct NormParams {
   // forward: x -> y; backward: gout (and x or its codes) -> gx.  Rows of `width`; frames: x and gx are [batch, width, T]

@@ -11,9 +11,7 @@ namespace {
 // enters the device for a call without a plan, its kernels set up
 nna_status enter_device(DeviceGuard& guard, int device) {
   if (device < 0) return fail(NNA_ERR_INVALID_ARG, "device must be the HIP device of the arrays");
-  nna_status s = check_device(device);
-  if (s != NNA_OK) return s;
-  hipError_t e = guard.enter(device);
+  hipError_t e = guard.enter(device);  // (refuses a device that there is not)
   if (e != hipSuccess) return fail_hip(e, "hipSetDevice");
   e = ensure_kernels_init(device);
   return e == hipSuccess ? NNA_OK : fail_hip(e, "kernel set-up");
