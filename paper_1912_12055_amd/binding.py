@@ -772,14 +772,19 @@ def nna_kept_bytes(plan: Plan, B: int, L: int) -> int:
     return n.value
 
 
-def nna_forward_keep(plan: Plan, x, stream=None, size=None):
+def nna_forward_keep(plan: Plan, x, stream=None, size=None, kept=None):
     """(out, kept): nna_stft, nna_mel or nna_cqt of a trainable plan, and what nna_backward_kept takes instead of computing it again.
-    `size`: nna_kept_bytes of the call, where the caller has asked for it."""
+    `size`: nna_kept_bytes of the call, where the caller has asked for it.  `kept`: a CUDA tensor of that many bytes to write it to (places that
+    stand for no frame or no kernel are left as they are)."""
     import torch
 
     if size is None:
         size = nna_kept_bytes(plan, *x.shape)
-    kept, spec = torch.empty(size, dtype=torch.uint8, device=x.device), None
+    spec = None
+    if kept is None:
+        kept = torch.empty(size, dtype=torch.uint8, device=x.device)
+    elif not (kept.is_cuda and kept.is_contiguous() and kept.device == x.device and kept.numel() * kept.element_size() >= size):
+        raise TypeError(f"kept must be a contiguous CUDA tensor of {size} bytes on x's device")
     kind, rows, _ = plan.constants()
     if kind == NNA_KIND_MEL:
         spec = torch.empty((x.shape[0], rows // 2, nna_out_shape(plan, *x.shape)[1]), dtype=torch.float32, device=x.device)
@@ -901,6 +906,13 @@ class NormKept:
 
     def tensors(self):
         return tuple(t for t in (self.x, self.stats, self.codes, self.scales) if t is not None)
+
+    def with_tensors(self, tensors, bits):
+        """The same with what tensors() gave (kept 8 or 32 `bits`)."""
+        kept = NormKept()
+        kept.shape, kept.dtype, kept.out_dtype, kept.rows, kept.row_stride = self.shape, self.dtype, self.out_dtype, self.rows, self.row_stride
+        kept.x, kept.stats, kept.codes, kept.scales = (*tensors, None, None) if bits == 32 else (None, *tensors)
+        return kept
 
 
 def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, out=None, stream=None):

@@ -10,6 +10,10 @@ Input ``x``: float32 CUDA tensor ``[B, L]`` (or ``[L]``); output ``[B, bins, T]`
 Memory: a call of a trainable ``MelSpectrogram`` (power 2), ``STFT`` (``output_format='Power'``) or ``CQT1992v2`` (every format but
 ``'Complex'``) that autograd records holds, until its backward pass, the kernels' products with the waveform besides ``x``: bank rows
 rounded up to 128 times frames times 4 bytes, at most 1 GiB a call.  Larger batches hold ``x`` alone and compute the products again.
+``kept_bits=8`` on these layers holds the products in 8 bits (``nna_pack8``), about a quarter of that; gradients are then those of the values the
+codes stand for, off by up to 1/254 of the largest of 128 neighbouring products.
+
+``LayerNorm`` and ``DecayAttention`` are what a network on the transforms' frames is built of.
 """
 from __future__ import annotations
 
@@ -71,8 +75,13 @@ def _forward(ctx, plan, x, keep, run):
     if keep and x.is_cuda and x.dim() == 2 and x.shape[1] >= 4:
         size = nb.nna_kept_bytes(plan, *x.shape)
         if 0 < size <= _KEPT_BYTES:
-            out, kept = nb.nna_forward_keep(plan, x, size=size)
-            ctx.save_for_backward(x, kept)
+            if ctx.layer.kept_bits == 8:  # (places between the products share their blocks: zeros, which change no scale)
+                kept = torch.zeros(size // 4, dtype=torch.float32, device=x.device)
+                out, _ = nb.nna_forward_keep(plan, x, size=size, kept=kept)
+                ctx.save_for_backward(x, *nb.nna_pack8(kept))
+            else:
+                out, kept = nb.nna_forward_keep(plan, x, size=size)
+                ctx.save_for_backward(x, kept)
             ctx.bank_sets = plan.bank_sets
             return out
     ctx.save_for_backward(x)
@@ -82,7 +91,9 @@ def _forward(ctx, plan, x, keep, run):
 def _saved(ctx):
     """(x, what was kept or None): a bank set since the forward pass is the one the gradients are taken with, so C is computed again."""
     x, *kept = ctx.saved_tensors
-    return x, kept[0] if kept and ctx.bank_sets == ctx.layer.plan.bank_sets else None
+    if not kept or ctx.bank_sets != ctx.layer.plan.bank_sets:
+        return x, None
+    return x, kept[0] if len(kept) == 1 else nb.nna_unpack8(*kept)
 
 
 class _StftFn(torch.autograd.Function):
@@ -141,7 +152,12 @@ class _MelFn(torch.autograd.Function):
 class _Trainable(torch.nn.Module):
     """Keeps the library's copy of a parameter in step with the ``nn.Parameter`` an optimiser updates."""
 
-    def _make_trainable(self):
+    kept_bits = 32
+
+    def _make_trainable(self, kept_bits=32):
+        if kept_bits not in (8, 32):
+            raise ValueError("kept_bits: 8 or 32")
+        self.kept_bits = kept_bits
         nb.nna_plan_trainable(self.plan)
         # (a property of the transform and its output format, the same for every batch)
         self._keeps = nb.nna_kept_bytes(self.plan, 1, 2 * self.plan.constants()[2] + 4) > 0
@@ -166,7 +182,7 @@ class STFT(_Trainable):
 
     def __init__(self, n_fft=2048, freq_bins=None, hop_length=512, window="hann", freq_scale="no", center=True,
                  pad_mode="reflect", fmin=50, fmax=6000, sr=22050, trainable=False, output_format="Magnitude",
-                 device="cuda:0"):
+                 device="cuda:0", kept_bits=32):
         super().__init__()
         _check_pad(center, pad_mode)
         dev = _device_index(device)
@@ -184,7 +200,7 @@ class STFT(_Trainable):
             raise ValueError("freq_scale: 'no', 'linear' or 'log'")
         self.trainable = bool(trainable)
         if self.trainable:
-            self._make_trainable()
+            self._make_trainable(kept_bits)
             self.wsin_wcos = torch.nn.Parameter(nb.nna_plan_get_bank(self.plan))
 
     def forward(self, x):
@@ -202,7 +218,7 @@ class MelSpectrogram(_Trainable):
 
     def __init__(self, sr=22050, n_fft=2048, n_mels=128, hop_length=512, window="hann", center=True,
                  pad_mode="reflect", htk=False, fmin=0.0, fmax=None, norm=1, trainable_mel=False, trainable_STFT=False,
-                 power=2.0, device="cuda:0"):
+                 power=2.0, device="cuda:0", kept_bits=32):
         super().__init__()
         _check_pad(center, pad_mode)
         self.plan = nb.nna_plan_mel(sr=sr, n_fft=n_fft, hop=hop_length, win=_window(window), center=center,
@@ -212,7 +228,7 @@ class MelSpectrogram(_Trainable):
         self.hop_length = hop_length
         self.trainable = bool(trainable_mel or trainable_STFT)
         if self.trainable:
-            self._make_trainable()
+            self._make_trainable(kept_bits)
             self.mel_basis = torch.nn.Parameter(nb.nna_plan_get_mel_weights(self.plan), requires_grad=bool(trainable_mel))
             self.wsin_wcos = torch.nn.Parameter(nb.nna_plan_get_bank(self.plan), requires_grad=bool(trainable_STFT))
 
@@ -273,7 +289,7 @@ class CQT1992v2(_Cqt):
 
     def __init__(self, sr=22050, hop_length=512, fmin=32.70, fmax=None, n_bins=84, bins_per_octave=12, norm=1,
                  window="hann", center=True, pad_mode="reflect", trainable=False, output_format="Magnitude",
-                 device="cuda:0"):
+                 device="cuda:0", kept_bits=32):
         super().__init__(False)
         _check_pad(center, pad_mode)
         if norm != 1:
@@ -283,7 +299,7 @@ class CQT1992v2(_Cqt):
                                     fmt=_format(output_format), device=_device_index(device))
         self.trainable = bool(trainable)
         if self.trainable:
-            self._make_trainable()
+            self._make_trainable(kept_bits)
             self.cqt_kernels = torch.nn.Parameter(nb.nna_plan_get_bank(self.plan))
 
     def forward(self, x):
@@ -350,3 +366,105 @@ class CQT2010(_Cqt2010):
 
 # The constant-Q layer the paper recommends (fastest on a GPU, best output: Sec. IV-A, IV-B) under the plain name.
 CQT = CQT1992v2
+
+
+# ---- networks on the transforms' frames --------------------------------------------------------------------------------
+
+
+class _NormFn(torch.autograd.Function):
+    """nna_layer_norm with nna_layer_norm_backward as its derivative."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, out_dtype, bits):
+        y, kept = nb.nna_layer_norm(x, weight, bias, eps=eps, out_dtype=out_dtype, keep=bits)
+        ctx.save_for_backward(weight, *kept.tensors())
+        kept.x = kept.stats = kept.codes = kept.scales = None  # (autograd holds the tensors, and looks after x being changed)
+        ctx.kept, ctx.bits = kept, bits
+        return y
+
+    @staticmethod
+    def backward(ctx, gout):
+        weight, *tensors = ctx.saved_tensors
+        kept = ctx.kept.with_tensors(tensors, ctx.bits)
+        need_x, need_w, need_b = ctx.needs_input_grad[:3]
+        gx, gw, gb = nb.nna_layer_norm_backward(gout.contiguous(), kept, weight, want_gx=need_x, want_gw=need_w or need_b)
+        return gx, gw if need_w else None, gb if need_b else None, None, None, None
+
+
+class LayerNorm(torch.nn.Module):
+    """Layer norm over the last axis, of `width` values; ``weight`` and ``bias`` are float32 parameters.
+
+    Input: rows ``x[..., width]`` of float32, bfloat16 or float16, or frames as the transforms write them, ``spec.transpose(1, 2)`` of
+    ``spec[B, bins, T]``, read as they lie and returned as tokens ``[B, T, bins]``.  ``out_dtype``: the tokens' type (float32 input; its own if None).
+    ``kept_bits=8`` keeps the input for the backward pass in 8 bits (rows)."""
+
+    def __init__(self, width, eps=1e-5, affine=True, bias=True, out_dtype=None, kept_bits=32, device="cuda:0"):
+        super().__init__()
+        if kept_bits not in (8, 32):
+            raise ValueError("kept_bits: 8 or 32")
+        dev = torch.device("cuda", _device_index(device))
+        self.width, self.eps, self.out_dtype, self.kept_bits = int(width), float(eps), out_dtype, kept_bits
+        self.weight = torch.nn.Parameter(torch.ones(self.width, device=dev)) if affine else None
+        self.bias = torch.nn.Parameter(torch.zeros(self.width, device=dev)) if affine and bias else None
+
+    def forward(self, x):
+        if x.shape[-1] != self.width:
+            raise ValueError(f"x must have {self.width} values along its last axis")
+        frames = x.dim() == 3 and x.dtype == torch.float32 and x.transpose(1, 2).is_contiguous()
+        if nb._row_stride(x) is None and (not frames or self.kept_bits == 8):
+            x = x.contiguous()
+        if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, self.weight, self.bias)):
+            return _NormFn.apply(x, self.weight, self.bias, self.eps, self.out_dtype, self.kept_bits)
+        return nb.nna_layer_norm(x, self.weight, self.bias, eps=self.eps, out_dtype=self.out_dtype)
+
+
+class _DecayFn(torch.autograd.Function):
+    """nna_decay_attention with nna_decay_attention_backward as its derivative."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, state, decay, scale, lengths, want_state):
+        ctx.save_for_backward(q, k, v, state, decay, lengths)
+        ctx.scale, ctx.want_state = scale, want_state
+        ctx.set_materialize_grads(False)
+        return nb.nna_decay_attention(q, k, v, decay, scale=scale, state=state, lengths=lengths, want_state=want_state)
+
+    @staticmethod
+    def backward(ctx, gout, gstate=None):
+        q, k, v, state, decay, lengths = ctx.saved_tensors
+        gout = torch.zeros((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device) if gout is None else gout.contiguous()
+        if gstate is not None:
+            gstate = gstate.contiguous()
+        gq, gk, gv, gfirst = nb.nna_decay_attention_backward(gout, q, k, v, decay, scale=ctx.scale, state=state, lengths=lengths, gstate=gstate,
+                                                             want_gstate=ctx.needs_input_grad[3])
+        return gq, gk, gv, gfirst, None, None, None, None
+
+
+class DecayAttention(torch.nn.Module):
+    """Linear attention over frames with a decay for each head: S_t = decay S_{t-1} + k_t^T v_t, o_t = scale q_t S_t.
+
+    ``decay``: `heads` numbers in [0, 1], constants of the layer; if None, 1 - 2^(-5 - 7 h / heads): heads that remember from some 30 frames to
+    thousands.  ``forward`` takes whole sequences, q and k ``[B, T, heads, dk]``, v ``[B, T, heads, dv]`` (float32 or bfloat16), of `lengths`
+    frames (int32 on the GPU) and going on from `state`; ``step`` one new frame of each."""
+
+    def __init__(self, heads, decay=None, scale=None, device="cuda:0"):
+        super().__init__()
+        dev = torch.device("cuda", _device_index(device))
+        decay = 1 - torch.exp2(-5 - 7 * torch.arange(heads) / heads) if decay is None else torch.as_tensor(decay, dtype=torch.float32)
+        if decay.requires_grad:
+            raise ValueError("decay is a constant of the layer: no gradient is taken")
+        if tuple(decay.shape) != (heads,) or not bool(((decay >= 0) & (decay <= 1)).all()):
+            raise ValueError(f"decay: {heads} numbers from 0 to 1")
+        self.scale = scale
+        self.register_buffer("decay", decay.to(device=dev, dtype=torch.float32).contiguous())
+
+    def forward(self, q, k, v, state=None, lengths=None, return_state=False):
+        """o ``[B, T, heads, dv]``, or (o, state after the last frame ``[B, heads, dk, dv]`` float32)."""
+        if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, state)):
+            return _DecayFn.apply(q, k, v, state, self.decay, self.scale, lengths, return_state)
+        return nb.nna_decay_attention(q, k, v, self.decay, scale=self.scale, state=state, lengths=lengths, want_state=return_state)
+
+    def step(self, q, k, v, state):
+        """o ``[B, heads, dv]`` of one frame; ``state`` is updated in place (not differentiable)."""
+        if torch.is_grad_enabled() and any(t.requires_grad for t in (q, k, v, state)):
+            raise RuntimeError("step has no derivative: call forward on sequences, or step under torch.no_grad()")
+        return nb.nna_decay_attention_step(q, k, v, self.decay, state, scale=self.scale)
