@@ -641,11 +641,12 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
  * outputs of its head NaN from its frame on, and the last state; one of k likewise by the rules of arithmetic; one of q its own frame's.
  *
  * nna_decay_attention_backward: given gout_dev [B, T, H, dv] (contiguous) and glast_dev (or NULL: 0), the gradients of a loss with respect to out and
- * the last state: gq_dev [B, T, H, dk] (or NULL), gk_dev [B, T, H, dk] and gv_dev [B, T, H, dv] (both or neither; contiguous, of `type`), and with
- * these gfirst_dev [B, H, dk, dv] (or NULL).  The same inputs give the same bits.
+ * the last state: gq_dev [B, T, H, dk] (or NULL), gk_dev [B, T, H, dk], gv_dev [B, T, H, dv] (contiguous, of `type`) and gfirst_dev [B, H, dk, dv]
+ * (or NULL), in nna_decay_attention_backward_workspace bytes.  The same inputs give the same bits.
  * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_UNSUPPORTED (type, dk or dv above 128), NNA_ERR_SHAPE.  T = 0 or B = 0 is no error.
  */
 nna_status nna_decay_attention_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes);
+nna_status nna_decay_attention_backward_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes);
 nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, const void* k_dev, const long long* k_strides, const void* v_dev,
                                const long long* v_strides, nna_dtype type, long long B, long long T, long long H, long long dk, long long dv,
                                const float* decay_dev, double scale, const int* lengths_dev, const float* first_dev, float* last_dev,

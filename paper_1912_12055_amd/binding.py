@@ -40,7 +40,7 @@ EXPORTS = [
     "nna_cqt_workspace", "nna_cqt_in_workspace",
     "nna_layer_norm", "nna_layer_norm_frames", "nna_layer_norm_backward_workspace", "nna_layer_norm_backward",
     "nna_layer_norm_frames_backward", "nna_pack8", "nna_unpack8",
-    "nna_decay_attention_workspace", "nna_decay_attention", "nna_decay_attention_backward", "nna_decay_attention_step",
+    "nna_decay_attention_workspace", "nna_decay_attention_backward_workspace", "nna_decay_attention", "nna_decay_attention_backward", "nna_decay_attention_step",
 ]
 
 _c = ctypes
@@ -126,7 +126,7 @@ def lib():
         L.nna_pack8.argtypes = [_VP, _I, _LL, _LL, _LL, _VP, _VP, _I, _VP]
         L.nna_unpack8.argtypes = [_VP, _VP, _LL, _LL, _VP, _I, _I, _VP]
         qkv, shape = 3 * [_VP, _c.POINTER(_LL)], 5 * [_LL]
-        L.nna_decay_attention_workspace.argtypes = [*shape, _c.POINTER(_c.c_size_t)]
+        L.nna_decay_attention_workspace.argtypes = L.nna_decay_attention_backward_workspace.argtypes = [*shape, _c.POINTER(_c.c_size_t)]
         L.nna_decay_attention.argtypes = [*qkv, _I, *shape, _VP, _D, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
         L.nna_decay_attention_backward.argtypes = [_VP, *qkv, _I, *shape, _VP, _D, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
         L.nna_decay_attention_step.argtypes = [*qkv, _I, _LL, _LL, _LL, _LL, _VP, _D, _VP, _VP, _I, _VP]
@@ -1036,6 +1036,9 @@ def nna_unpack8(codes, scales, dtype=None, out=None, stream=None):
     return out
 
 
+_strides3, _strides2 = _LL * 3, _LL * 2
+
+
 def _heads(q, k, v, axes):
     """(nna_dtype, sizes, the arguments q, k, v stand for) of [B, (T,) H, d] tensors; their strides but for the last are their own."""
     t = _type_of(q, "q", ("float32", "bfloat16"))
@@ -1049,7 +1052,7 @@ def _heads(q, k, v, axes):
         s = x.stride()
         if x.shape[-1] != 1 and s[-1] != 1:
             raise TypeError("a head's values must lie next to each other")
-        args += [x.data_ptr(), (_LL * (axes - 1))(*s[:-1])]
+        args += [x.data_ptr(), (_strides3 if axes == 4 else _strides2)(*s[:-1])]
     return t, (*q.shape, v.shape[-1]), args
 
 
@@ -1064,9 +1067,15 @@ def _lengths(lengths, B, device):
 
 
 def nna_decay_attention_workspace(B: int, T: int, H: int, dk: int, dv: int) -> int:
-    """Bytes that nna_decay_attention and its backward call need; 0 where there are sequences and heads enough to fill the card."""
+    """Bytes that nna_decay_attention needs; 0 where there are sequences and heads enough to fill the card."""
     n = _c.c_size_t()
     _check(lib().nna_decay_attention_workspace(B, T, H, dk, dv, _c.byref(n)))
+    return n.value
+
+
+def nna_decay_attention_backward_workspace(B: int, T: int, H: int, dk: int, dv: int) -> int:
+    n = _c.c_size_t()
+    _check(lib().nna_decay_attention_backward_workspace(B, T, H, dk, dv, _c.byref(n)))
     return n.value
 
 
@@ -1097,7 +1106,7 @@ def nna_decay_attention(q, k, v, decay, scale=None, state=None, lengths=None, wa
 
 def nna_decay_attention_backward(gout, q, k, v, decay, scale=None, state=None, lengths=None, gstate=None, want_gstate=False, workspace=None, stream=None):
     """(gq, gk, gv, gradient of the first state or None): the gradients of a loss through nna_decay_attention, given gout = dLoss/do (contiguous)
-    and gstate = dLoss/d(last state) (None: zero)."""
+    and gstate = dLoss/d(last state) (None: zero).  `workspace`: nna_decay_attention_backward_workspace bytes (taken here if None)."""
     import torch
 
     t, (B, T, H, dk, dv), args = _heads(q, k, v, 4)
@@ -1108,7 +1117,7 @@ def nna_decay_attention_backward(gout, q, k, v, decay, scale=None, state=None, l
         raise TypeError(f"gout must be a contiguous {q.dtype} tensor of shape {(B, T, H, dv)}")
     gq, gk, gv = q.new_empty((B, T, H, dk)), q.new_empty((B, T, H, dk)), torch.empty_like(gout)
     first = decay.new_empty((B, H, dk, dv)) if want_gstate else None
-    need = nna_decay_attention_workspace(B, T, H, dk, dv)
+    need = nna_decay_attention_backward_workspace(B, T, H, dk, dv)
     ws = (None, 0)
     if need:
         workspace = _workspace_on(stream, need, workspace, device)

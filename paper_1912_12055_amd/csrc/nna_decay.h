@@ -46,9 +46,10 @@ struct DecayStep {
 // segments of a mix, chunks in each, and the bytes of `parts` (0 for one segment)
 size_t decay_segments(long long B, long long T, int H, int dk, int dv, int* segments, int* chunks);
 hipError_t decay_kernels_init();  // per device, before the first launch
-// parts: the states before the segments, from b and c; nothing to do for one segment.  given: a state that is given back comes of them
-hipError_t launch_decay_states(DecayMix P, int type, bool given, hipStream_t stream);
-hipError_t launch_decay_mix(DecayMix P, int type, hipStream_t stream);
+// out, and its states before (parts is as large as decay_segments says)
+hipError_t launch_decay(DecayMix P, int type, hipStream_t stream);
+// gq (out NULL: not wanted) with the states that `states` = (q, k, v) has, parts the same, and the pair gv, gk with its own parts
+hipError_t launch_decay_gradients(DecayMix states, DecayMix gq, DecayMix pair, int type, hipStream_t stream);
 hipError_t launch_decay_step(const DecayStep& P, int type, hipStream_t stream);
 
 }  // namespace nna

@@ -257,14 +257,32 @@ __device__ __forceinline__ int length_of(const DecayMix& P, long long batch) {
 
 // A product that sums over frames j meets c_j = 0 * x where its weight is zero (j after i): an infinity or a NaN there would reach frames before its own.  It is
 // taken out of the tile, and every frame from its own on is NaN, as is the state.
+typedef float quad_anywhere_t __attribute__((ext_vector_type(4), aligned(4)));
+
+// the frames of a workgroup's segment, and those of them that are their sequence's
+struct Span {
+  int head, segment, n, from, to, real_to;  // head: of all sequences' heads
+};
+__device__ __forceinline__ Span span_of(const DecayMix& P, int workgroup) {
+  Span s;
+  // (a quotient is computed a lane at a time: unless it is taken back to a scalar register, all that follows of it is kept for every lane)
+  s.head = uniform(workgroup / P.segments);
+  s.segment = workgroup - s.head * P.segments;
+  s.n = uniform(length_of(P, uniform(s.head / P.H)));
+  const int frames = P.segment_chunks * CHUNK;
+  s.from = s.segment * frames;
+  s.to = P.T - s.from < frames ? P.T : s.from + frames;
+  s.real_to = s.to < s.n ? s.to : s.n;
+  return s;
+}
+
 template <typename T, int DA, int DC, int PLANES, int MODE, bool REVERSE, bool FULL>
-__global__ __launch_bounds__((Shape<T, DA, DC>::threads(MODE)), 2) void decay_mix_kernel(DecayMix P) {
+__device__ __forceinline__ void mix_chunks(const DecayMix& P, const int workgroup, unsigned char* const lds) {
   static_assert(MODE != PAIR || DA == DC, "both halves run the same sizes");
   typedef Shape<T, DA, DC> S;
   constexpr int NP = S::PLANES, ROWS = S::ROWS, CB = S::CB, WAVES = S::WAVES, THREADS = S::THREADS, IB = S::IB, RB = DA / 16;
   typedef Tile<ROWS, DA, NP> TileA;
   typedef Tile<ROWS, DC, NP> TileC;
-  extern __shared__ __align__(16) unsigned char lds[];
   const int thread = threadIdx.x & (THREADS - 1), lane = thread & 63, li = lane & 15, lg = lane >> 4;
   const int wave = uniform(thread >> 6);
   const bool second = MODE == PAIR && uniform((int)threadIdx.x / THREADS) != 0;
@@ -283,58 +301,23 @@ __global__ __launch_bounds__((Shape<T, DA, DC>::threads(MODE)), 2) void decay_mi
     weights += S::WEIGHTS;
   }
 
-  // (a quotient is computed a lane at a time: unless it is taken back to a scalar register, all that follows of it is kept for every lane)
-  const int workgroup = blockIdx.x, of_head = uniform(workgroup / P.segments), segment = workgroup - of_head * P.segments;
-  if (MODE == STATE && segment == P.segments - 1) return;  // nothing comes after it
-  const int of_batch = uniform(of_head / P.H), head = of_head - of_batch * P.H;
-  const long long bh = of_head, batch = of_batch;
-  const int n = uniform(length_of(P, batch)), all = P.T;
+  const Span span = span_of(P, workgroup);
+  if (MODE == STATE && span.segment == P.segments - 1) return;  // nothing comes after it
+  const int segment = span.segment, of_batch = uniform(span.head / P.H), head = span.head - of_batch * P.H;
+  const long long bh = span.head, batch = of_batch;
+  const int n = span.n, all = P.T;
   const float log2_decay = uniform(log2_of(P.decay[head]));
   const int da = second ? P.dc : P.da, dc = second ? P.da : P.dc;
   const bool transposed = second || P.transposed;
   const int column0 = wave * CB * 16;
 
-  // the state: rows 16 r + 4 lg .. + 3 of column column0 + 16 m + li
-  f32x4 state[RB][CB];
-  float* const part = P.parts + (bh * P.segments + segment) * P.part_size;
+  // fn(row, column, value) of the state's quads a lane holds: four rows of a column
+  auto state_values = [&](f32x4 (&state)[RB][CB], auto fn) {
 #pragma unroll
-  for (int r = 0; r < RB; ++r)
+    for (int r = 0; r < RB; ++r)
 #pragma unroll
-    for (int m = 0; m < CB; ++m) {
-      state[r][m] = 0.f;
-      if (MODE == STATE) continue;
-      const int column = column0 + m * 16 + li, row = r * 16 + lg * 4;
-      if (P.segments > 1) {
-        if (row < da && column < dc) {
-          if (transposed) {
-            state[r][m] = *reinterpret_cast<const f32x4*>(part + column * P.part_pitch + row);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) state[r][m][e] = part[(row + e) * P.part_pitch + column];
-          }
-        }
-      } else if (P.first) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (row + e < da && column < dc)
-            state[r][m][e] = P.first[bh * da * dc + (transposed ? column * da + row + e : (row + e) * dc + column)] * P.first_factor;
-      }
-    }
-
-  // powers of the decay that every whole chunk takes, as a lane's own times the block's: of the weights (on the diagonal; one block below it), of the first
-  // state, and of a frame's product in the next state
-  f32x4 on_diagonal, below, left;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int apart = li - lg * 4 - e;
-    on_diagonal[e] = power(log2_decay, apart < 0 ? 0 : apart) * P.factor;
-    below[e] = power(log2_decay, 16 + apart) * P.factor;
-    left[e] = power(log2_decay, 15 - lg * 4 - e + (REVERSE ? 1 : 0));
-  }
-  const float since = power(log2_decay, li + (REVERSE ? 0 : 1)) * P.factor;
-  const float power16 = uniform(power(log2_decay, 16)), power32 = uniform(power(log2_decay, 32)), power48 = uniform(power(log2_decay, 48));
-  const float carry_whole = uniform(power(log2_decay, ROWS));
-  auto block_power = [&](int i) { return i == 0 ? 1.f : here_only(i == 1 ? power16 : i == 2 ? power32 : power48); };
+      for (int m = 0; m < CB; ++m) fn(r * 16 + lg * 4, column0 + m * 16 + li, state[r][m]);
+  };
 
   // between memory and LDS: a, b and c; of a pair, the first half of the threads a and b, the second a2 and c
   Rows<T, ROWS, DA, THREADS, FULL, REVERSE> ra, rb;
@@ -380,11 +363,52 @@ __global__ __launch_bounds__((Shape<T, DA, DC>::threads(MODE)), 2) void decay_mi
     }
   };
 
-  // a segment's frames; the kernel's own chunks divide its
-  const int from = segment * P.segment_chunks * CHUNK, left_frames = all - from;
-  const int to = left_frames < P.segment_chunks * CHUNK ? all : from + P.segment_chunks * CHUNK;
-  const int real_to = to < n ? to : n;
-  if (from < real_to) load(from);
+  const int from = span.from, to = span.to, real_to = span.real_to;
+  if (from < real_to) load(from);  // on its way while the state is read and the powers are taken
+
+  // the state: rows 16 r + 4 lg .. + 3 of column column0 + 16 m + li
+  f32x4 state[RB][CB];
+  float* const part = P.parts + (bh * P.segments + segment) * P.part_size;
+  {
+    const bool parts = P.segments > 1;
+    const float* from_state = parts ? part : P.first ? P.first + bh * da * dc : nullptr;
+    const int pitch = parts ? P.part_pitch : transposed ? da : dc;  // from one of its rows to the next
+    const float factor = parts ? 1.f : P.first_factor;
+    state_values(state, [&](int row, int column, f32x4& v) {
+      v = 0.f;
+      if (MODE == STATE || !from_state) return;
+      // (where the head's sizes are not the tile's, what is not there is read at a place that is)
+      const int c = FULL || column < dc ? column : dc - 1;
+      if (transposed && (FULL || (parts && row < da))) {
+        v = *reinterpret_cast<const quad_anywhere_t*>(from_state + c * pitch + row) * factor;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = FULL || row + e < da ? row + e : da - 1;
+          v[e] = from_state[transposed ? c * pitch + r : r * pitch + c] * factor;
+        }
+      }
+      if (!FULL)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = row + e < da && column < dc ? v[e] : 0.f;
+    });
+  }
+
+  // powers of the decay that every whole chunk takes, as a lane's own times the block's: of the weights (on the diagonal; one block below it), of the first
+  // state, and of a frame's product in the next state
+  f32x4 on_diagonal, below, left;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int apart = li - lg * 4 - e;
+    on_diagonal[e] = power(log2_decay, apart < 0 ? 0 : apart) * P.factor;
+    below[e] = power(log2_decay, 16 + apart) * P.factor;
+    left[e] = power(log2_decay, 15 - lg * 4 - e + (REVERSE ? 1 : 0));
+  }
+  const float since = power(log2_decay, li + (REVERSE ? 0 : 1)) * P.factor;
+  const float power16 = uniform(power(log2_decay, 16)), power32 = uniform(power(log2_decay, 32)), power48 = uniform(power(log2_decay, 48));
+  const float carry_whole = uniform(power(log2_decay, ROWS));
+  auto block_power = [&](int i) { return i == 0 ? 1.f : here_only(i == 1 ? power16 : i == 2 ? power32 : power48); };
+
   for (int u0 = from; u0 < real_to; u0 += ROWS) {
     const int here = n - u0 < ROWS ? n - u0 : ROWS;
     int* bad_here = bad_row + (u0 / ROWS & 1);  // two in turn: a wave may still read the last chunk's
@@ -542,28 +566,63 @@ __global__ __launch_bounds__((Shape<T, DA, DC>::threads(MODE)), 2) void decay_mi
     }
     if (second || !P.last || segment != P.segments - 1) return;
   }
+  float* const to_state = MODE == STATE ? part : P.last + bh * da * dc;
+  const int pitch = MODE == STATE ? P.part_pitch : transposed ? da : dc;
+  state_values(state, [&](int row, int column, f32x4& v) {
 #pragma unroll
-  for (int r = 0; r < RB; ++r)
-#pragma unroll
-    for (int m = 0; m < CB; ++m) {
-      const int column = column0 + m * 16 + li, row = r * 16 + lg * 4;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (MODE == STATE)
-          part[(row + e) * P.part_pitch + column] = state[r][m][e];
-        else if (row + e < da && column < dc)
-          P.last[bh * da * dc + (transposed ? column * da + row + e : (row + e) * dc + column)] = state[r][m][e] * P.last_factor;
-      }
-    }
+    for (int e = 0; e < 4; ++e)
+      if (MODE == STATE || FULL || (row + e < da && column < dc))
+        to_state[MODE != STATE && transposed ? column * pitch + row + e : (row + e) * pitch + column] = MODE == STATE ? v[e] : v[e] * P.last_factor;
+  });
 }
 
-// parts[s]: from each segment's own state to the state before it, in order; four values of a (sequence, head) to a thread, JOIN_AHEAD segments read before the
-// first of them is written
-constexpr int JOIN_AHEAD = 16;
-__global__ __launch_bounds__(256) void decay_join_kernel(DecayMix P) {
-  const int workgroups = P.part_size / 1024, of_head = uniform((int)blockIdx.x / workgroups);
-  const int at = ((int)blockIdx.x - of_head * workgroups) * 1024 + threadIdx.x * 4, row = at / P.part_pitch, column = at % P.part_pitch;
+template <typename T, int DA, int DC, int PLANES, int MODE, bool REVERSE, bool FULL>
+__global__ __launch_bounds__((Shape<T, DA, DC>::threads(MODE)), 2) void decay_mix_kernel(DecayMix P) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  mix_chunks<T, DA, DC, PLANES, MODE, REVERSE, FULL>(P, blockIdx.x, lds);
+}
+
+// The backward pass's launches of two directions in one.  The states before the segments, of the forward pass and of the gradient:
+template <typename T, int DA, int DC, int PLANES, bool FULL>
+__global__ __launch_bounds__((Shape<T, DA, DC>::threads(STATE)), 2) void decay_both_states_kernel(DecayMix P, DecayMix R, int workgroups) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  if ((int)blockIdx.x < workgroups)
+    mix_chunks<T, DA, DC, sizeof(T) == 4 ? 3 : 2, STATE, false, FULL>(P, blockIdx.x, lds);
+  else
+    mix_chunks<T, DA, DC, PLANES, STATE, true, FULL>(R, blockIdx.x - workgroups, lds);
+}
+// All three gradients, where the two launches together are one workgroup a CU at most: gk and gv in the first workgroups, gq in the others, half of whose waves only
+// keep up with the barriers, three a chunk.
+template <typename T, int D, int PLANES, bool FULL>
+__global__ __launch_bounds__((Shape<T, D, D>::threads(PAIR)), 2) void decay_gradients_kernel(DecayMix R, DecayMix P, int workgroups) {
+  typedef Shape<T, D, D> S;
+  extern __shared__ __align__(16) unsigned char lds[];
+  if ((int)blockIdx.x < workgroups) {
+    mix_chunks<T, D, D, PLANES, PAIR, true, FULL>(R, blockIdx.x, lds);
+  } else if (uniform((int)threadIdx.x / S::THREADS) == 0) {
+    mix_chunks<T, D, D, sizeof(T) == 4 ? 3 : 2, MIX, false, FULL>(P, blockIdx.x - workgroups, lds);
+  } else {
+    const Span span = span_of(P, blockIdx.x - workgroups);
+    for (int u0 = span.from; u0 < span.real_to; u0 += S::ROWS) {
+      __syncthreads();
+      __syncthreads();
+      __syncthreads();
+    }
+  }
+}
+
+// parts[s]: from each segment's own state to the state before it, in order; four values of a (sequence, head) to a thread, all segments of a round read before
+// the first of them is written.  For few segments (8 of 64 heads of 128: 11 us, 30 by the kernel below).
+constexpr int JOIN_FEW = 16;
+__device__ __forceinline__ void join_few(const DecayMix& P, int block) {
+  const int workgroups = P.part_size / 1024, of_head = uniform(block / workgroups);
+  const int at = (block - of_head * workgroups) * 1024 + threadIdx.x * 4, row = at / P.part_pitch, column = at % P.part_pitch;
   const long long bh = of_head;
+  float* const part = P.parts + bh * P.segments * P.part_size + at;
+  f32x4 own[JOIN_FEW];
+#pragma unroll
+  for (int k = 0; k < JOIN_FEW; ++k)
+    if (k + 1 < P.segments) own[k] = *reinterpret_cast<const f32x4*>(part + (long long)k * P.part_size);
   const int n = uniform(length_of(P, of_head / P.H)), frames = P.segment_chunks * CHUNK;
   const float log2_decay = log2_of(P.decay[of_head % P.H]), whole = power(log2_decay, frames);
   f32x4 s = 0.f;
@@ -571,20 +630,78 @@ __global__ __launch_bounds__(256) void decay_join_kernel(DecayMix P) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (column + e < P.dc) s[e] = P.first[(bh * P.da + row) * P.dc + column + e] * P.first_factor;
-  float* part = P.parts + bh * P.segments * P.part_size + at;
-  for (int i = 0; i < P.segments; i += JOIN_AHEAD) {
-    f32x4 own[JOIN_AHEAD];
+#pragma unroll
+  for (int k = 0; k < JOIN_FEW; ++k)
+    if (k < P.segments) {
+      *reinterpret_cast<f32x4*>(part + (long long)k * P.part_size) = s;
+      const long long left = n - (long long)k * frames;
+      if (k + 1 < P.segments) s = s * (left >= frames ? whole : power(log2_decay, left < 0 ? 0 : (int)left)) + own[k];
+    }
+}
+
+// (and of a second direction from workgroup `workgroups` on)
+__global__ __launch_bounds__(256) void decay_join_few_kernel(DecayMix P, DecayMix R, int workgroups) {
+  if ((int)blockIdx.x < workgroups)
+    join_few(P, blockIdx.x);
+  else
+    join_few(R, blockIdx.x - workgroups);
+}
+
+// ... and for many: a lane has four values, each of JOIN_WAVES waves JOIN_AHEAD segments; all are read at once, every wave's own run is joined, and then
+// the runs (61 segments of 8 heads of 64: 7 us, 15 one after the other).
+constexpr int JOIN_WAVES = 8, JOIN_AHEAD = 8;
+__device__ __forceinline__ void join_many(const DecayMix& P, int block, f32x4 (&sums)[2][JOIN_WAVES][64]) {
+  const int workgroups = P.part_size / 256, of_head = uniform(block / workgroups), lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+  const int at = (block - of_head * workgroups) * 256 + lane * 4, row = at / P.part_pitch, column = at % P.part_pitch;
+  const long long bh = of_head;
+  float* const part = P.parts + bh * P.segments * P.part_size + at;
+  const int n = uniform(length_of(P, of_head / P.H)), frames = P.segment_chunks * CHUNK;
+  const float log2_decay = log2_of(P.decay[of_head % P.H]);
+  f32x4 s = 0.f;  // the state before the next JOIN_WAVES * JOIN_AHEAD segments
+  if (P.first && row < P.da)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (column + e < P.dc) s[e] = P.first[(bh * P.da + row) * P.dc + column + e] * P.first_factor;
+  // the decay over segments i .. j - 1
+  auto over = [&](int i, int j) {
+    const long long a = (long long)i * frames, b = (long long)j * frames;
+    return power(log2_decay, (int)((b < n ? b : n) - (a < n ? a : n)));
+  };
+  for (int i0 = 0, turn = 0; i0 < P.segments; i0 += JOIN_WAVES * JOIN_AHEAD, turn ^= 1) {
+    const int each = P.segments - i0 < JOIN_WAVES * JOIN_AHEAD ? (P.segments - i0 + JOIN_WAVES - 1) / JOIN_WAVES : JOIN_AHEAD;
+    const int first = i0 + wave * each < P.segments ? i0 + wave * each : P.segments, end = first + each < P.segments ? first + each : P.segments;
+    f32x4 own[JOIN_AHEAD], run = 0.f;
+#pragma unroll
+    for (int k = 0; k < JOIN_AHEAD; ++k) {
+      own[k] = 0.f;
+      if (first + k < end && first + k + 1 < P.segments) own[k] = *reinterpret_cast<const f32x4*>(part + (long long)(first + k) * P.part_size);
+    }
 #pragma unroll
     for (int k = 0; k < JOIN_AHEAD; ++k)
-      if (i + k + 1 < P.segments) own[k] = *reinterpret_cast<const f32x4*>(part + (long long)(i + k) * P.part_size);
+      if (first + k < end) run = run * over(first + k, first + k + 1) + own[k];
+    sums[turn][wave][lane] = run;
+    __syncthreads();  // (two buffers in turn: the next runs never meet a wave that still reads these)
+    f32x4 before = s;
+    for (int w = 0; w < JOIN_WAVES; ++w) {
+      const int a = i0 + w * each < P.segments ? i0 + w * each : P.segments, b = a + each < P.segments ? a + each : P.segments;
+      if (w == wave) before = s;
+      s = s * over(a, b) + sums[turn][w][lane];
+    }
 #pragma unroll
     for (int k = 0; k < JOIN_AHEAD; ++k)
-      if (i + k < P.segments) {
-        *reinterpret_cast<f32x4*>(part + (long long)(i + k) * P.part_size) = s;
-        const long long left = n - (long long)(i + k) * frames;
-        if (i + k + 1 < P.segments) s = s * (left >= frames ? whole : power(log2_decay, left < 0 ? 0 : (int)left)) + own[k];
+      if (first + k < end) {
+        *reinterpret_cast<f32x4*>(part + (long long)(first + k) * P.part_size) = before;
+        before = before * over(first + k, first + k + 1) + own[k];
       }
   }
+}
+
+__global__ __launch_bounds__(64 * JOIN_WAVES) void decay_join_kernel(DecayMix P, DecayMix R, int workgroups) {
+  __shared__ f32x4 sums[2][JOIN_WAVES][64];
+  if ((int)blockIdx.x < workgroups)
+    join_many(P, blockIdx.x, sums);
+  else
+    join_many(R, blockIdx.x - workgroups, sums);
 }
 
 // One frame: the state is read and written once, four columns of it to a lane, a slab of 32 columns to a workgroup
@@ -690,6 +807,39 @@ hipError_t launch_mode(const DecayMix& P, int type, int mode, bool given, int wo
   return type == NNA_F32 ? launch_mode<float>(P, mode, given, workgroups, stream) : launch_mode<bf16>(P, mode, given, workgroups, stream);
 }
 
+// P and R in one launch: their states, or (gradients) gq and the pair
+template <typename T>
+hipError_t launch_both(const DecayMix& P, const DecayMix& R, bool given, int workgroups, bool gradients, hipStream_t stream) {
+  const int most = std::max(R.da, R.dc), da = gradients ? most : R.da, dc = gradients ? most : R.dc;
+  return by_heads(da, dc, [&](auto a, auto c) {
+    constexpr int DA = a.value, DC = c.value;
+    typedef Shape<T, DA, DC> S;
+    return by_bool(R.da == DA && R.dc == DC, [&](auto full) {
+      return by_bool(given || sizeof(T) == 4, [&](auto exact) {
+        constexpr bool FULL = full.value, GIVEN = exact.value;
+        if constexpr (sizeof(T) == 4 && !GIVEN) return hipErrorInvalidValue;
+        else {
+          constexpr int PLANES = planes_of<T, GIVEN>();
+          if constexpr (DA == DC)
+            if (gradients) {
+              const auto kernel = &decay_gradients_kernel<T, DA, PLANES, FULL>;
+              if (workgroups < 0) return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds(PAIR));
+              hipLaunchKernelGGL(kernel, dim3(2 * workgroups), dim3(S::threads(PAIR)), S::lds(PAIR), stream, R, P, workgroups);
+              return hipGetLastError();
+            }
+          const auto kernel = &decay_both_states_kernel<T, DA, DC, PLANES, FULL>;
+          if (workgroups < 0) return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds(STATE));
+          hipLaunchKernelGGL(kernel, dim3(2 * workgroups), dim3(S::threads(STATE)), S::lds(STATE), stream, P, R, workgroups);
+          return hipGetLastError();
+        }
+      });
+    });
+  });
+}
+hipError_t launch_both(const DecayMix& P, const DecayMix& R, int type, bool given, int workgroups, bool gradients, hipStream_t stream) {
+  return type == NNA_F32 ? launch_both<float>(P, R, given, workgroups, gradients, stream) : launch_both<bf16>(P, R, given, workgroups, gradients, stream);
+}
+
 int padded(int d) { return d <= 64 ? 64 : 128; }
 
 }  // namespace
@@ -702,7 +852,8 @@ hipError_t decay_kernels_init() {
         P.da = (all & 1 ? 128 : 64) - (all & 4 ? 1 : 0);
         P.dc = all & 2 ? 128 : 64;
         P.reverse = all & 8;
-        const hipError_t e = launch_mode(P, type, mode, all & 16, -1, nullptr);
+        hipError_t e = launch_mode(P, type, mode, all & 16, -1, nullptr);
+        if (e == hipSuccess) e = launch_both(P, P, type, all & 16, -1, mode == PAIR, nullptr);
         if (e != hipSuccess) return e;
       }
   return hipSuccess;
@@ -719,21 +870,53 @@ size_t decay_segments(long long B, long long T, int H, int dk, int dv, int* segm
   return n == 1 ? 0 : (size_t)(heads * n) * padded(dk) * padded(dv) * sizeof(float);
 }
 
-hipError_t launch_decay_states(DecayMix P, int type, bool given, hipStream_t stream) {
-  if (P.segments == 1) return hipSuccess;
-  P.part_pitch = padded(P.dc);
-  P.part_size = padded(P.da) * P.part_pitch;
-  const hipError_t e = launch_mode(P, type, STATE, given, (int)(P.B * P.H * P.segments), stream);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(decay_join_kernel, dim3((unsigned)(P.B * P.H * (P.part_size / 1024))), dim3(256), 0, stream, P);
+static void set_parts(DecayMix& P) {
+  P.part_pitch = padded(P.transposed ? P.da : P.dc);
+  P.part_size = padded(P.transposed ? P.dc : P.da) * P.part_pitch;
+}
+
+// the states before the segments of P, and of R if it is given (of the same sizes)
+static hipError_t launch_join(const DecayMix& P, const DecayMix* R, hipStream_t stream) {
+  const bool few = P.segments <= JOIN_FEW;
+  const int workgroups = (int)(P.B * P.H) * (P.part_size / (few ? 1024 : 256)), both = R ? 2 * workgroups : workgroups;
+  if (few)
+    hipLaunchKernelGGL(decay_join_few_kernel, dim3(both), dim3(256), 0, stream, P, R ? *R : P, workgroups);
+  else
+    hipLaunchKernelGGL(decay_join_kernel, dim3(both), dim3(64 * JOIN_WAVES), 0, stream, P, R ? *R : P, workgroups);
   return hipGetLastError();
 }
 
-hipError_t launch_decay_mix(DecayMix P, int type, hipStream_t stream) {
-  const int rows = P.transposed ? P.dc : P.da, columns = P.transposed ? P.da : P.dc;
-  P.part_pitch = padded(columns);
-  P.part_size = padded(rows) * P.part_pitch;
-  return launch_mode(P, type, P.a2 || P.reverse ? PAIR : MIX, P.last != nullptr, (int)(P.B * P.H * P.segments), stream);
+hipError_t launch_decay(DecayMix P, int type, hipStream_t stream) {
+  const int workgroups = (int)(P.B * P.H * P.segments);
+  const bool given = P.last != nullptr;
+  set_parts(P);
+  if (P.segments > 1) {
+    hipError_t e = launch_mode(P, type, STATE, given, workgroups, stream);
+    if (e == hipSuccess) e = launch_join(P, nullptr, stream);
+    if (e != hipSuccess) return e;
+  }
+  return launch_mode(P, type, MIX, given, workgroups, stream);
+}
+
+hipError_t launch_decay_gradients(DecayMix states, DecayMix gq, DecayMix pair, int type, hipStream_t stream) {
+  const int workgroups = (int)(pair.B * pair.H * pair.segments);
+  const bool given = pair.last != nullptr;
+  set_parts(states);
+  set_parts(gq);
+  set_parts(pair);
+  if (pair.segments > 1) {
+    hipError_t e = gq.out ? launch_both(states, pair, type, given, workgroups, false, stream) : launch_mode(pair, type, STATE, given, workgroups, stream);
+    if (e == hipSuccess) e = gq.out ? launch_join(states, &pair, stream) : launch_join(pair, nullptr, stream);
+    if (e != hipSuccess) return e;
+  }
+  // a workgroup a CU at most: together (16 clips of up to 431 frames, 8 heads of 64, float32: 63 us, 48 and 60 in two launches); more than that, the waves that
+  // only wait would hold registers that a second workgroup runs in
+  if (gq.out && 2 * workgroups <= 256) return launch_both(gq, pair, type, given, workgroups, true, stream);
+  if (gq.out) {
+    const hipError_t e = launch_mode(gq, type, MIX, false, workgroups, stream);
+    if (e != hipSuccess) return e;
+  }
+  return launch_mode(pair, type, PAIR, given, workgroups, stream);
 }
 
 hipError_t launch_decay_step(const DecayStep& P, int type, hipStream_t stream) {

@@ -95,7 +95,7 @@ nna_status check_decay_args(const void* decay, double scale, const void* workspa
   if (!decay) return fail(NNA_ERR_INVALID_ARG, "decay_dev is NULL");
   if (!(scale != 0.0) || !(std::fabs(scale) < 1e30) || !(std::fabs(scale) > 1e-30)) return fail(NNA_ERR_INVALID_ARG, "scale must be finite and not 0");
   if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || bytes < need))
-    return fail(NNA_ERR_INVALID_ARG, "workspace_dev is NULL, misaligned or smaller than nna_decay_attention_workspace asks for");
+    return fail(NNA_ERR_INVALID_ARG, "workspace_dev is NULL, misaligned or smaller than the call's _workspace function asks for");
   return NNA_OK;
 }
 
@@ -262,6 +262,12 @@ nna_status nna_decay_attention_workspace(long long B, long long T, long long H, 
   return NNA_OK;
 }
 
+nna_status nna_decay_attention_backward_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes) {
+  const nna_status s = nna_decay_attention_workspace(B, T, H, dk, dv, bytes);
+  if (s == NNA_OK) *bytes *= 2;  // both directions' states
+  return s;
+}
+
 nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, const void* k_dev, const long long* k_strides, const void* v_dev,
                                const long long* v_strides, nna_dtype type, long long B, long long T, long long H, long long dk, long long dv,
                                const float* decay_dev, double scale, const int* lengths_dev, const float* first_dev, float* last_dev,
@@ -290,8 +296,7 @@ nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, co
   s = enter_device(guard, device);
   if (s != NNA_OK || !B) return s;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  hipError_t e = launch_decay_states(P, type, last_dev != nullptr, stream);
-  if (e == hipSuccess) e = launch_decay_mix(P, type, stream);
+  const hipError_t e = launch_decay(P, type, stream);
   return e == hipSuccess ? NNA_OK : fail_hip(e, "linear attention");
 }
 
@@ -305,11 +310,10 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
   s = check_strides({q_strides, k_strides, v_strides});
   if (s != NNA_OK) return s;
   if (B && T && (!gout_dev || !q_dev || !k_dev || !v_dev)) return fail(NNA_ERR_INVALID_ARG, "gout_dev / q_dev / k_dev / v_dev is NULL");
-  if (B && T && !gk_dev != !gv_dev) return fail(NNA_ERR_INVALID_ARG, "gk_dev and gv_dev come together");
-  if (B && T && !gq_dev && !gk_dev) return fail(NNA_ERR_INVALID_ARG, "no gradient is asked for");
-  if (B && T && gfirst_dev && !gk_dev) return fail(NNA_ERR_INVALID_ARG, "gfirst_dev comes with gk_dev and gv_dev");
+  if (B && T && (!gk_dev || !gv_dev)) return fail(NNA_ERR_INVALID_ARG, "gk_dev / gv_dev is NULL");
   DecayMix P = {};
-  s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, decay_segments(B, T, (int)H, (int)dk, (int)dv, &P.segments, &P.segment_chunks));
+  const size_t half = decay_segments(B, T, (int)H, (int)dk, (int)dv, &P.segments, &P.segment_chunks);
+  s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, 2 * half);
   if (s != NNA_OK) return s;
   const long long packed[3] = {T * H * dv, H * dv, dv};
   const Heads q = heads_of(q_dev, q_strides, dk), k = heads_of(k_dev, k_strides, dk), v = heads_of(v_dev, v_strides, dv), g = heads_of(gout_dev, packed, dv);
@@ -324,31 +328,27 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
   s = enter_device(guard, device);
   if (s != NNA_OK || !B) return s;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  hipError_t e = hipSuccess;
-  if (gq_dev) {  // the states of the forward pass, transposed
-    set_mix(P, q, k, v);
-    P.first = first_dev;
-    P.first_factor = 1.f;
-    e = launch_decay_states(P, type, false, stream);
-    set_mix(P, g, v, k);
-    P.out = gq_dev;
-    P.transposed = 1;
-    if (e == hipSuccess) e = launch_decay_mix(P, type, stream);
-  }
-  if (e == hipSuccess && (gk_dev || gfirst_dev)) {
-    // the state's gradient, without q's scale: the outputs get it at the end, as gfirst does
-    P.reverse = 1;
-    P.first = glast_dev;
-    P.first_factor = (float)(1.0 / scale);
-    P.last = gfirst_dev;
-    P.last_factor = (float)scale;
-    P.transposed = 0;
-    set_mix(P, k, q, g);
-    e = launch_decay_states(P, type, gfirst_dev != nullptr, stream);
-    P.out = gv_dev;
-    set_pair(P, v, gk_dev);
-    if (e == hipSuccess) e = launch_decay_mix(P, type, stream);
-  }
+  DecayMix states = P, gq = P, pair = P;
+  set_mix(states, q, k, v);
+  states.first = first_dev;
+  states.first_factor = 1.f;
+  set_mix(gq, g, v, k);  // on those states, transposed
+  gq.first = first_dev;
+  gq.first_factor = 1.f;
+  gq.transposed = 1;
+  gq.out = gq_dev;
+  // the state's gradient, without q's scale: the outputs get it at the end, as gfirst does
+  set_mix(pair, k, q, g);
+  set_pair(pair, v, gk_dev);
+  pair.out = gv_dev;
+  pair.reverse = 1;
+  pair.first = glast_dev;
+  pair.first_factor = (float)(1.0 / scale);
+  pair.last = gfirst_dev;
+  pair.last_factor = (float)scale;
+  pair.parts = P.parts + half / sizeof(float);
+  if (!gq_dev && !gk_dev && !gfirst_dev) return NNA_OK;  // (no frames)
+  const hipError_t e = launch_decay_gradients(states, gq, pair, type, stream);
   return e == hipSuccess ? NNA_OK : fail_hip(e, "linear attention, backward");
 }
 
