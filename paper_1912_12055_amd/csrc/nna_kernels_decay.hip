@@ -372,7 +372,7 @@ __device__ __forceinline__ void mix_chunks(const DecayMix& P, const int workgrou
   {
     const bool parts = P.segments > 1;
     const float* from_state = parts ? part : P.first ? P.first + bh * da * dc : nullptr;
-    const int pitch = parts ? P.part_pitch : transposed ? da : dc;  // from one of its rows to the next
+    const int pitch = parts ? P.part_pitch : transposed ? da : dc, to_row = transposed ? 1 : pitch, to_column = transposed ? pitch : 1;
     const float factor = parts ? 1.f : P.first_factor;
     state_values(state, [&](int row, int column, f32x4& v) {
       v = 0.f;
@@ -380,12 +380,12 @@ __device__ __forceinline__ void mix_chunks(const DecayMix& P, const int workgrou
       // (where the head's sizes are not the tile's, what is not there is read at a place that is)
       const int c = FULL || column < dc ? column : dc - 1;
       if (transposed && (FULL || (parts && row < da))) {
-        v = *reinterpret_cast<const quad_anywhere_t*>(from_state + c * pitch + row) * factor;
+        v = *reinterpret_cast<const quad_anywhere_t*>(from_state + c * to_column + row) * factor;
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = FULL || row + e < da ? row + e : da - 1;
-          v[e] = from_state[transposed ? c * pitch + r : r * pitch + c] * factor;
+          v[e] = from_state[r * to_row + c * to_column] * factor;
         }
       }
       if (!FULL)
@@ -520,9 +520,9 @@ __device__ __forceinline__ void mix_chunks(const DecayMix& P, const int workgrou
       }
 #pragma unroll
       for (int m = 0; m < CB; ++m) {
-        f32x8 v = 0.f;
+        f32x8 v = __builtin_convertvector(vc[m][NP - 1], f32x8);
 #pragma unroll
-        for (int p = NP - 1; p >= 0; --p) v += __builtin_convertvector(vc[m][p], f32x8);
+        for (int p = NP - 2; p >= 0; --p) v += __builtin_convertvector(vc[m][p], f32x8);
         split(__builtin_shufflevector(v, v, 0, 1, 2, 3) * weight[0], __builtin_shufflevector(v, v, 4, 5, 6, 7) * weight[1], vs[m]);
       }
 #pragma unroll
@@ -567,12 +567,13 @@ __device__ __forceinline__ void mix_chunks(const DecayMix& P, const int workgrou
     if (second || !P.last || segment != P.segments - 1) return;
   }
   float* const to_state = MODE == STATE ? part : P.last + bh * da * dc;
-  const int pitch = MODE == STATE ? P.part_pitch : transposed ? da : dc;
+  const bool turned = MODE != STATE && transposed;
+  const int pitch = MODE == STATE ? P.part_pitch : turned ? da : dc, to_row = turned ? 1 : pitch, to_column = turned ? pitch : 1;
   state_values(state, [&](int row, int column, f32x4& v) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (MODE == STATE || FULL || (row + e < da && column < dc))
-        to_state[MODE != STATE && transposed ? column * pitch + row + e : (row + e) * pitch + column] = MODE == STATE ? v[e] : v[e] * P.last_factor;
+        to_state[(row + e) * to_row + column * to_column] = MODE == STATE ? v[e] : v[e] * P.last_factor;
   });
 }
 
