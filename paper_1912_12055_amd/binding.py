@@ -940,7 +940,7 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
     step = _row_stride(x)
     kept = stats = codes = scales = None
     if keep:
-        stats = torch.empty((rows, 2), dtype=torch.float32, device=device)
+        stats = x.new_empty((rows, 2), dtype=torch.float32)
         if keep == 8:
             codes = torch.empty((rows, width), dtype=torch.int8, device=device)
             scales = torch.empty((rows, -(-width // NNA_BLOCK8)), dtype=torch.float32, device=device)
@@ -951,7 +951,7 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
     if step is not None:
         _check(lib().nna_layer_norm(x.data_ptr(), xt, rows, width, step, w, b, eps, out.data_ptr(), yt, sp,
                                     codes.data_ptr() if keep == 8 else None, scales.data_ptr() if keep == 8 else None, device.index, st))
-    elif x.dim() == 3 and xt == NNA_F32 and x.transpose(1, 2).is_contiguous():
+    elif x.dim() == 3 and xt == NNA_F32 and (x.stride() == (width * shape[1], 1, shape[1]) or x.transpose(1, 2).is_contiguous()):
         if keep == 8:
             raise TypeError("keep=8: x must be rows (consecutive values next to each other)")
         _check(lib().nna_layer_norm_frames(x.data_ptr(), shape[0], width, shape[1], w, b, eps, out.data_ptr(), yt, sp, device.index, st))
@@ -975,10 +975,10 @@ def nna_layer_norm_backward(gout, kept, weight=None, want_gx=True, want_gw=True,
     B, T = (shape[0], shape[1]) if frames else (0, 0)
     gx = gw = gb = None
     if want_gx:
-        gx = gout.new_empty((B, width, T), dtype=kept.dtype).transpose(1, 2) if frames else torch.empty_like(gout, dtype=kept.dtype)
+        gx = kept.x.new_empty_strided(shape, (width * T, 1, T)) if frames else torch.empty_like(gout, dtype=kept.dtype)
     need = 0
     if want_gw:
-        gw, gb = kept.stats.new_empty((2, width)).unbind(0)
+        gw, gb = kept.stats.new_empty(width), kept.stats.new_empty(width)
         need = nna_layer_norm_backward_workspace(rows, width, B, T)
         workspace = _workspace_on(stream, need, workspace, device)
     ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if want_gw else (None, 0)
