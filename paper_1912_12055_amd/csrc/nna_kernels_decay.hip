@@ -57,21 +57,23 @@ __device__ __forceinline__ void split(f32x4 v, f32x4 w, bf16x8 (&o)[N]) {
 }
 
 // ---- tiles in LDS: planes of rows (frames), a head's values along a row ------------------------------------------------------
-// elements between rows, so that 16 lanes that read along 16 rows, and four across four, meet different banks
-__host__ __device__ constexpr int pitch_of(int d) { return d == 64 ? d + 8 : d + 24; }
+// Rows are an odd multiple of 32 bytes apart, and in the lower half of every 16 rows the octets of a pair change places: 16 lanes that read octets along 16 rows,
+// and eight rows' pairs of octets read across, then meet all 64 banks once.
+__host__ __device__ constexpr int pitch_of(int d) { return d + 16; }
+__device__ __forceinline__ int swap_of(int row) { return row & 8; }
 template <int ROWS, int D, int N>
 struct Tile {
   static constexpr int PITCH = pitch_of(D), PLANE = ROWS * PITCH, SIZE = N * PLANE;
   // k along a row: values k0 + 8 g .. of row0 + i
   static __device__ __forceinline__ void rows8(const bf16* tile, int row0, int k0, int li, int lg, bf16x8 (&o)[N]) {
 #pragma unroll
-    for (int p = 0; p < N; ++p) o[p] = *reinterpret_cast<const bf16x8*>(tile + p * PLANE + (row0 + li) * PITCH + k0 + lg * 8);
+    for (int p = 0; p < N; ++p) o[p] = *reinterpret_cast<const bf16x8*>(tile + p * PLANE + (row0 + li) * PITCH + k0 + (lg * 8 ^ swap_of(li)));
   }
   // ... in the order of accumulators
   static __device__ __forceinline__ void rows4(const bf16* tile, int row0, int k0, int li, int lg, bf16x8 (&o)[N]) {
 #pragma unroll
     for (int p = 0; p < N; ++p) {
-      const bf16* at = tile + p * PLANE + (row0 + li) * PITCH + k0 + lg * 4;
+      const bf16* at = tile + p * PLANE + (row0 + li) * PITCH + k0 + (lg * 4 ^ swap_of(li));
       o[p] = join(*reinterpret_cast<const bf16x4*>(at), *reinterpret_cast<const bf16x4*>(at + 16));
     }
   }
@@ -79,7 +81,7 @@ struct Tile {
   static __device__ __forceinline__ void columns(const bf16* tile, int row0, int column0, int lane, bf16x8 (&o)[N]) {
 #pragma unroll
     for (int p = 0; p < N; ++p) {
-      const bf16* at = tile + p * PLANE + (row0 + (lane >> 2)) * PITCH + column0 + (lane & 3) * 4;
+      const bf16* at = tile + p * PLANE + (row0 + (lane >> 2)) * PITCH + column0 + ((lane & 3) * 4 ^ swap_of(lane >> 2));
       bf16x4 f[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -196,19 +198,21 @@ struct Rows {
       for (int i = 0; i < N; ++i)
         if (row + i * STEP >= here) v[i] = (oct)(T)0;
     }
-    bf16* p = tile + thread / PER_ROW * tile_type::PITCH + column;
+    bf16* p = tile + thread / PER_ROW * tile_type::PITCH;
+    static_assert(STEP % 16 == 0 || N == 1, "a lane's octets change places in all of its rows or in none");
+    const int swap = swap_of(thread / PER_ROW);
 #pragma unroll
     for (int i = 0; i < N; ++i, p += STEP * tile_type::PITCH) {
       if (FULL) {
-        K::put(p, tile_type::PLANE, v[i]);
+        K::put(p + (column ^ swap), tile_type::PLANE, v[i]);
         continue;
       }
-      K::put(p, tile_type::PLANE, column + 8 <= d ? v[i] : (oct)(T)0);
+      K::put(p + (column ^ swap), tile_type::PLANE, column + 8 <= d ? v[i] : (oct)(T)0);
       if (column < d && column + 8 > d) {
-        bf16* const q = p + (d >= 8 ? d - 8 - column : 0);
+        const int first = d >= 8 ? d - 8 : 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (e < d) K::put1(q + e, tile_type::PLANE, v[i][e]);
+          if (e < d) K::put1(p + (first + e ^ here_only(swap)), tile_type::PLANE, v[i][e]);
       }
     }
   }
@@ -233,12 +237,14 @@ struct Rows {
 // What a launch does with the chunks: out = mix(a, b, c); the state alone; or, with twice the threads and time reversed, out = mix(a, b, c) and
 // out2 = mix(a2, c, b), whose states are each other's transpose, from one reading of all four.
 enum { MIX, STATE, PAIR };
+constexpr int XCDS = 8;  // workgroups go to them in turn
 
-// Frames of a chunk: 64; 32 where three planes of 128 columns leave no room for more.  Columns of the state to a wave: 32 where a state of 128 x 32 and
+// Frames of a chunk: 64; of three planes 32, so that heads of 64 leave room for two workgroups on a CU (64 clips of 431 frames, 8 heads of 64, float32: 61 us forward
+// and 153 backward, 87 and 208 with 64; one workgroup a CU: the same) and heads of 128 for one.  Columns of the state to a wave: 32 where a state of 128 x 32 and
 // the rest fit 256 registers, so that what is read from LDS meets two products; else 16.
 template <typename T, int DA, int DC>
 struct Shape {
-  static constexpr int PLANES = Kind<T>::planes, ROWS = PLANES == 3 && (DA == 128 || DC == 128) ? 32 : 64;
+  static constexpr int PLANES = Kind<T>::planes, ROWS = PLANES == 3 ? 32 : 64;
   static constexpr int CB = PLANES == 1 && DC == 128 ? 2 : 1, WAVES = DC / 16 / CB, THREADS = 64 * WAVES;
   static constexpr int IB = ROWS / 16, BLOCKS = IB * (IB + 1) / 2;  // 16 x 16 blocks on and below the diagonal
   static constexpr int WEIGHTS = BLOCKS * 64 * PLANES;              // quads
@@ -577,6 +583,16 @@ __device__ __forceinline__ void mix_chunks(const DecayMix& P, const int workgrou
   });
 }
 
+// Where gk and gv are computed as a pair, of sizes padded to the larger: the mixes of three planes of 128 columns leave no room for two workgroups on a CU.
+template <typename T, int DA, int DC>
+constexpr bool in_pairs() { return sizeof(T) == 4 && (DA == 128 || DC == 128); }
+bool in_pairs(int type, int da, int dc) { return type == NNA_F32 && (da > 64 || dc > 64); }
+
+// planes of a state's new products: where a state is given back it is as exact as its float32 sums; where it only meets frames again, rounded to the
+// inputs' type, two are more than that holds
+template <typename T, bool GIVEN>
+constexpr int planes_of() { return sizeof(T) == 4 || GIVEN ? 3 : 2; }
+
 template <typename T, int DA, int DC, int PLANES, int MODE, bool REVERSE, bool FULL>
 __global__ __launch_bounds__((Shape<T, DA, DC>::threads(MODE)), 2) void decay_mix_kernel(DecayMix P) {
   extern __shared__ __align__(16) unsigned char lds[];
@@ -588,12 +604,12 @@ template <typename T, int DA, int DC, int PLANES, bool FULL>
 __global__ __launch_bounds__((Shape<T, DA, DC>::threads(STATE)), 2) void decay_both_states_kernel(DecayMix P, DecayMix R, int workgroups) {
   extern __shared__ __align__(16) unsigned char lds[];
   if ((int)blockIdx.x < workgroups)
-    mix_chunks<T, DA, DC, sizeof(T) == 4 ? 3 : 2, STATE, false, FULL>(P, blockIdx.x, lds);
+    mix_chunks<T, DA, DC, planes_of<T, false>(), STATE, false, FULL>(P, blockIdx.x, lds);
   else
     mix_chunks<T, DA, DC, PLANES, STATE, true, FULL>(R, blockIdx.x - workgroups, lds);
 }
-// All three gradients, where the two launches together are one workgroup a CU at most: gk and gv in the first workgroups, gq in the others, half of whose waves only
-// keep up with the barriers, three a chunk.
+// All three gradients, gk and gv as a pair, where the two launches together are one workgroup a CU at most: the pairs in the first workgroups, gq in the others, half
+// of whose waves only keep up with the barriers, three a chunk.
 template <typename T, int D, int PLANES, bool FULL>
 __global__ __launch_bounds__((Shape<T, D, D>::threads(PAIR)), 2) void decay_gradients_kernel(DecayMix R, DecayMix P, int workgroups) {
   typedef Shape<T, D, D> S;
@@ -601,7 +617,7 @@ __global__ __launch_bounds__((Shape<T, D, D>::threads(PAIR)), 2) void decay_grad
   if ((int)blockIdx.x < workgroups) {
     mix_chunks<T, D, D, PLANES, PAIR, true, FULL>(R, blockIdx.x, lds);
   } else if (uniform((int)threadIdx.x / S::THREADS) == 0) {
-    mix_chunks<T, D, D, sizeof(T) == 4 ? 3 : 2, MIX, false, FULL>(P, blockIdx.x - workgroups, lds);
+    mix_chunks<T, D, D, planes_of<T, false>(), MIX, false, FULL>(P, blockIdx.x - workgroups, lds);
   } else {
     const Span span = span_of(P, blockIdx.x - workgroups);
     for (int u0 = span.from; u0 < span.real_to; u0 += S::ROWS) {
@@ -610,6 +626,24 @@ __global__ __launch_bounds__((Shape<T, D, D>::threads(PAIR)), 2) void decay_grad
       __syncthreads();
     }
   }
+}
+
+// The gradients as mixes of their own, all in one launch: gv, gk and (if wanted) gq of a segment in workgroups of one XCD, begun together, so that what two of them
+// read comes from its cache the second time.  Two such workgroups fit a CU and one's products run beside the other's loads and barriers; a pair reads a third less but
+// has the CU for itself (bfloat16, 64 heads of 128, 16,384 frames: 820 us, gq and then the pair 863; float32, 32 clips of 431 frames, 8 heads of 64: 80 and 102).
+// Heads of 128 in float32 fill a CU either way: there the pair is ahead (16 clips of 431 frames, 8 heads: 119 us, 150 as mixes).
+template <typename T, int DK, int DV, int PLANES, bool FULL>
+__global__ __launch_bounds__((Shape<T, DK, DV>::THREADS), 2) void decay_mixes_kernel(DecayMix V, DecayMix K, DecayMix Q, int workgroups, int mixes) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  static_assert(Shape<T, DK, DV>::THREADS == Shape<T, DV, DK>::THREADS, "one launch");
+  const int round = (int)blockIdx.x / XCDS, at = uniform(round / mixes), which = round - at * mixes, workgroup = at * XCDS + (int)blockIdx.x % XCDS;
+  if (workgroup >= workgroups) return;
+  if (which == 0)
+    mix_chunks<T, DK, DV, PLANES, MIX, true, FULL>(V, workgroup, lds);
+  else if (which == 1)
+    mix_chunks<T, DV, DK, planes_of<T, false>(), MIX, true, FULL>(K, workgroup, lds);
+  else
+    mix_chunks<T, DV, DK, planes_of<T, false>(), MIX, false, FULL>(Q, workgroup, lds);
 }
 
 // parts[s]: from each segment's own state to the state before it, in order; four values of a (sequence, head) to a thread, all segments of a round read before
@@ -768,11 +802,6 @@ hipError_t by_heads(int da, int dc, F fn) {
   return fn(std::integral_constant<int, 128>(), std::integral_constant<int, 128>());
 }
 
-// planes of a state's new products: where a state is given back it is as exact as its float32 sums; where it only meets frames again, rounded to the
-// inputs' type, two are more than that holds
-template <typename T, bool GIVEN>
-constexpr int planes_of() { return sizeof(T) == 4 || GIVEN ? 3 : 2; }
-
 template <typename T, int DA, int DC, bool GIVEN, int MODE, bool REVERSE, bool FULL>
 hipError_t run_mix(const DecayMix& P, int workgroups, hipStream_t stream) {
   typedef Shape<T, DA, DC> S;
@@ -794,8 +823,9 @@ hipError_t launch_mode(const DecayMix& P, int mode, bool given, int workgroups, 
         constexpr bool FULL = full.value, GIVEN = exact.value;
         if constexpr (sizeof(T) == 4 && !GIVEN) return hipErrorInvalidValue;
         else {
-          if constexpr (DA == DC)
+          if constexpr (DA == DC && in_pairs<T, DA, DC>())
             if (mode == PAIR) return run_mix<T, DA, DC, GIVEN, PAIR, true, FULL>(P, workgroups, stream);
+          if (mode == PAIR) return hipErrorInvalidValue;
           if (mode == STATE)
             return by_bool(P.reverse != 0, [&](auto reverse) { return run_mix<T, DA, DC, GIVEN, STATE, reverse.value, FULL>(P, workgroups, stream); });
           return run_mix<T, DA, DC, GIVEN, MIX, false, FULL>(P, workgroups, stream);
@@ -821,13 +851,14 @@ hipError_t launch_both(const DecayMix& P, const DecayMix& R, bool given, int wor
         if constexpr (sizeof(T) == 4 && !GIVEN) return hipErrorInvalidValue;
         else {
           constexpr int PLANES = planes_of<T, GIVEN>();
-          if constexpr (DA == DC)
+          if constexpr (DA == DC && in_pairs<T, DA, DC>())
             if (gradients) {
               const auto kernel = &decay_gradients_kernel<T, DA, PLANES, FULL>;
               if (workgroups < 0) return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds(PAIR));
               hipLaunchKernelGGL(kernel, dim3(2 * workgroups), dim3(S::threads(PAIR)), S::lds(PAIR), stream, R, P, workgroups);
               return hipGetLastError();
             }
+          if (gradients) return hipErrorInvalidValue;
           const auto kernel = &decay_both_states_kernel<T, DA, DC, PLANES, FULL>;
           if (workgroups < 0) return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds(STATE));
           hipLaunchKernelGGL(kernel, dim3(2 * workgroups), dim3(S::threads(STATE)), S::lds(STATE), stream, P, R, workgroups);
@@ -841,6 +872,40 @@ hipError_t launch_both(const DecayMix& P, const DecayMix& R, int type, bool give
   return type == NNA_F32 ? launch_both<float>(P, R, given, workgroups, gradients, stream) : launch_both<bf16>(P, R, given, workgroups, gradients, stream);
 }
 
+// gv, gk of R, its pair, and gq = P (out NULL: not wanted)
+template <typename T>
+hipError_t launch_mixes(const DecayMix& P, const DecayMix& R, bool given, int workgroups, hipStream_t stream) {
+  return by_heads(R.da, R.dc, [&](auto a, auto c) {
+    constexpr int DK = a.value, DV = c.value;
+    return by_bool(R.da == DK && R.dc == DV, [&](auto full) {
+      return by_bool(given || sizeof(T) == 4, [&](auto exact) {
+        constexpr bool FULL = full.value, GIVEN = exact.value;
+        if constexpr (in_pairs<T, DK, DV>() || (sizeof(T) == 4 && !GIVEN)) return hipErrorInvalidValue;
+        else {
+          const auto kernel = &decay_mixes_kernel<T, DK, DV, planes_of<T, GIVEN>(), FULL>;
+          constexpr int LDS = std::max(Shape<T, DK, DV>::lds(MIX), Shape<T, DV, DK>::lds(MIX));
+          if (workgroups < 0) return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+          DecayMix V = R, K = R;
+          V.out2 = nullptr;
+          K.a = R.a2, K.a_b = R.a2_b, K.a_t = R.a2_t, K.a_h = R.a2_h;
+          K.b = R.c, K.b_b = R.c_b, K.b_t = R.c_t, K.b_h = R.c_h;
+          K.c = R.b, K.c_b = R.b_b, K.c_t = R.b_t, K.c_h = R.b_h;
+          K.out = R.out2;
+          K.last = nullptr;
+          K.da = R.dc, K.dc = R.da;
+          K.transposed = 1;
+          const int mixes = P.out ? 3 : 2, rounds = (workgroups + XCDS - 1) / XCDS;
+          hipLaunchKernelGGL(kernel, dim3(XCDS * mixes * rounds), dim3(Shape<T, DK, DV>::THREADS), LDS, stream, V, K, P, workgroups, mixes);
+          return hipGetLastError();
+        }
+      });
+    });
+  });
+}
+hipError_t launch_mixes(const DecayMix& P, const DecayMix& R, int type, bool given, int workgroups, hipStream_t stream) {
+  return type == NNA_F32 ? launch_mixes<float>(P, R, given, workgroups, stream) : launch_mixes<bf16>(P, R, given, workgroups, stream);
+}
+
 int padded(int d) { return d <= 64 ? 64 : 128; }
 
 }  // namespace
@@ -850,11 +915,16 @@ hipError_t decay_kernels_init() {
   for (int type : {NNA_F32, NNA_BF16})
     for (int mode : {MIX, STATE, PAIR})
       for (int all = 0; all < 32; ++all) {
+        hipError_t e = hipSuccess;
         P.da = (all & 1 ? 128 : 64) - (all & 4 ? 1 : 0);
         P.dc = all & 2 ? 128 : 64;
         P.reverse = all & 8;
-        hipError_t e = launch_mode(P, type, mode, all & 16, -1, nullptr);
-        if (e == hipSuccess) e = launch_both(P, P, type, all & 16, -1, mode == PAIR, nullptr);
+        if (mode == PAIR && !in_pairs(type, P.da, P.dc)) {
+          e = launch_mixes(P, P, type, all & 16, -1, nullptr);
+        } else {
+          e = launch_mode(P, type, mode, all & 16, -1, nullptr);
+          if (e == hipSuccess) e = launch_both(P, P, type, all & 16, -1, mode == PAIR, nullptr);
+        }
         if (e != hipSuccess) return e;
       }
   return hipSuccess;
@@ -910,6 +980,7 @@ hipError_t launch_decay_gradients(DecayMix states, DecayMix gq, DecayMix pair, i
     if (e == hipSuccess) e = gq.out ? launch_join(states, &pair, stream) : launch_join(pair, nullptr, stream);
     if (e != hipSuccess) return e;
   }
+  if (!in_pairs(type, pair.da, pair.dc)) return launch_mixes(gq, pair, type, given, workgroups, stream);
   // a workgroup a CU at most: together (16 clips of up to 431 frames, 8 heads of 64, float32: 63 us, 48 and 60 in two launches); more than that, the waves that
   // only wait would hold registers that a second workgroup runs in
   if (gq.out && 2 * workgroups <= 256) return launch_both(gq, pair, type, given, workgroups, true, stream);
