@@ -44,7 +44,7 @@ struct DecayStep {
 };
 
 // segments of a mix, chunks in each, and the bytes of `parts` (0 for one segment)
-size_t decay_segments(long long B, long long T, int H, int dk, int dv, int* segments, int* chunks);
+size_t decay_segments(long long B, long long T, int H, int dk, int dv, int type, bool backward, int* segments, int* chunks);
 hipError_t decay_kernels_init();  // per device, before the first launch
 // out, and its states before (parts is as large as decay_segments says)
 hipError_t launch_decay(DecayMix P, int type, hipStream_t stream);

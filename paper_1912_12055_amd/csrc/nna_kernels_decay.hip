@@ -930,10 +930,26 @@ hipError_t decay_kernels_init() {
   return hipSuccess;
 }
 
-size_t decay_segments(long long B, long long T, int H, int dk, int dv, int* segments, int* chunks) {
+// Segments cost half as much again (their states) and a launch that joins them, so there are some only where the heads alone leave the card idle, and then as many as
+// its workgroups: 512 forward (256 in float32 with heads of 128: one a CU), 256 backward, of three mixes each.  Forward / backward in us, the number of segments before
+// the colon:
+//   float32, heads of 64    8 heads, 2,048 frames      1: 174/182  8: 45/49    32: 27/37
+//                           64 heads, 1,024 frames     1: 89/96    4: 48/76    8: 41/79
+//                           128 heads, 1,024 frames    1: 89/123   4: 63/128
+//   bfloat16, heads of 64   8 heads, 512 frames        1: 23/25    4: 25/28            (float32: 1: 47/50  4: 31/32)
+//                           128 heads, 16,384 frames   1: 600/775  4: 355/841
+//                           256 heads, 2,048 frames    1: 79/170   2: 85/201
+//   bfloat16, heads of 128  64 heads, 1,024 frames     1: 69/73    4: 50/92
+//                           64 heads, 16,384 frames    1: 1088/1117  4: 419/939  8: 397/938
+//   float32, heads of 128   128 heads, 2,048 frames    1: 334/556  2: 270/626  4: 283/669
+size_t decay_segments(long long B, long long T, int H, int dk, int dv, int type, bool backward, int* segments, int* chunks) {
   const long long all = std::max(1LL, (T + CHUNK - 1) / CHUNK), heads = std::max(1LL, B * H);
-  // two workgroups on each of 256 CUs, segments of four chunks at least
-  long long n = std::max(1LL, std::min((512 + heads - 1) / heads, all / 4));
+  const bool wide = dk > 64 || dv > 64;
+  const long long workgroups = backward || in_pairs(type, dk, dv) ? 256 : 512;
+  long long n = std::min(workgroups / heads, all / 2);
+  if (backward && wide && type == NNA_BF16) n = std::max(std::min(512 / heads, all / 16), std::min(128 / heads, all / 2));  // (three mixes of 64 heads: nearly two a CU)
+  const long long fewest = backward ? 4 : in_pairs(type, dk, dv) ? 2 : 3;
+  if (n < fewest || (backward && heads >= 128) || all < (type == NNA_F32 ? 8 : 12)) n = 1;
   const long long each = (all + n - 1) / n;
   n = (all + each - 1) / each;
   *segments = (int)n;

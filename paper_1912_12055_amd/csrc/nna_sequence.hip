@@ -91,6 +91,17 @@ nna_status check_heads(int type, long long B, long long T, long long H, long lon
   return NNA_OK;
 }
 
+// bytes of the states before all segments, of either type
+nna_status states_size(long long B, long long T, long long H, long long dk, long long dv, bool backward, size_t* bytes) {
+  if (!bytes) return fail(NNA_ERR_INVALID_ARG, "bytes is NULL");
+  const nna_status s = check_heads(NNA_F32, B, T, H, dk, dv);
+  if (s != NNA_OK) return s;
+  int segments, chunks;
+  *bytes = std::max(decay_segments(B, T, (int)H, (int)dk, (int)dv, NNA_F32, backward, &segments, &chunks),
+                    decay_segments(B, T, (int)H, (int)dk, (int)dv, NNA_BF16, backward, &segments, &chunks));
+  return NNA_OK;
+}
+
 nna_status check_decay_args(const void* decay, double scale, const void* workspace, size_t bytes, size_t need) {
   if (!decay) return fail(NNA_ERR_INVALID_ARG, "decay_dev is NULL");
   if (!(scale != 0.0) || !(std::fabs(scale) < 1e30) || !(std::fabs(scale) > 1e-30)) return fail(NNA_ERR_INVALID_ARG, "scale must be finite and not 0");
@@ -254,16 +265,11 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
 }
 
 nna_status nna_decay_attention_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes) {
-  if (!bytes) return fail(NNA_ERR_INVALID_ARG, "bytes is NULL");
-  nna_status s = check_heads(NNA_F32, B, T, H, dk, dv);
-  if (s != NNA_OK) return s;
-  int segments, chunks;
-  *bytes = decay_segments(B, T, (int)H, (int)dk, (int)dv, &segments, &chunks);
-  return NNA_OK;
+  return states_size(B, T, H, dk, dv, false, bytes);
 }
 
 nna_status nna_decay_attention_backward_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes) {
-  const nna_status s = nna_decay_attention_workspace(B, T, H, dk, dv, bytes);
+  const nna_status s = states_size(B, T, H, dk, dv, true, bytes);
   if (s == NNA_OK) *bytes *= 2;  // both directions' states
   return s;
 }
@@ -278,8 +284,11 @@ nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, co
   if (s != NNA_OK) return s;
   if (B && T && (!q_dev || !k_dev || !v_dev || !out_dev)) return fail(NNA_ERR_INVALID_ARG, "q_dev / k_dev / v_dev / out_dev is NULL");
   DecayMix P = {};
-  s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, decay_segments(B, T, (int)H, (int)dk, (int)dv, &P.segments, &P.segment_chunks));
+  size_t need = 0;
+  s = nna_decay_attention_workspace(B, T, H, dk, dv, &need);
+  if (s == NNA_OK) s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, need);
   if (s != NNA_OK) return s;
+  decay_segments(B, T, (int)H, (int)dk, (int)dv, type, false, &P.segments, &P.segment_chunks);
   set_mix(P, heads_of(q_dev, q_strides, dk), heads_of(k_dev, k_strides, dk), heads_of(v_dev, v_strides, dv));
   P.out = out_dev;
   P.decay = decay_dev;
@@ -312,9 +321,11 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
   if (B && T && (!gout_dev || !q_dev || !k_dev || !v_dev)) return fail(NNA_ERR_INVALID_ARG, "gout_dev / q_dev / k_dev / v_dev is NULL");
   if (B && T && (!gk_dev || !gv_dev)) return fail(NNA_ERR_INVALID_ARG, "gk_dev / gv_dev is NULL");
   DecayMix P = {};
-  const size_t half = decay_segments(B, T, (int)H, (int)dk, (int)dv, &P.segments, &P.segment_chunks);
-  s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, 2 * half);
+  size_t need = 0;
+  s = nna_decay_attention_backward_workspace(B, T, H, dk, dv, &need);
+  if (s == NNA_OK) s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, need);
   if (s != NNA_OK) return s;
+  decay_segments(B, T, (int)H, (int)dk, (int)dv, type, true, &P.segments, &P.segment_chunks);
   const long long packed[3] = {T * H * dv, H * dv, dv};
   const Heads q = heads_of(q_dev, q_strides, dk), k = heads_of(k_dev, k_strides, dk), v = heads_of(v_dev, v_strides, dv), g = heads_of(gout_dev, packed, dv);
   P.decay = decay_dev;
@@ -346,7 +357,7 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
   pair.first_factor = (float)(1.0 / scale);
   pair.last = gfirst_dev;
   pair.last_factor = (float)scale;
-  pair.parts = P.parts + half / sizeof(float);
+  pair.parts = P.parts + need / 2 / sizeof(float);
   if (!gq_dev && !gk_dev && !gfirst_dev) return NNA_OK;  // (no frames)
   const hipError_t e = launch_decay_gradients(states, gq, pair, type, stream);
   return e == hipSuccess ? NNA_OK : fail_hip(e, "linear attention, backward");
