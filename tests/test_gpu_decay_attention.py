@@ -344,3 +344,35 @@ def test_on_another_stream_and_in_a_graph(nb):
         got = [t.clone() for t in (*out, one, state)]
         want = nb.nna_decay_attention_step(q[:, 0], k[:, 0], v[:, 0], decay, check)
         assert all(torch.equal(a, c) for a, c in zip((*step(), want, check), got)), i
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,T,H,dk,dv", [(13, 1100, 10, 16, 16), (16, 800, 4, 33, 17), (4, 1100, 25, 40, 100), (16, 4160, 4, 16, 80), (2, 520, 3, 64, 64)])
+def test_segments_of_either_direction(nb, dtype, B, T, H, dk, dv):
+    """Many heads are cut forward alone, some neither way, some in one type only."""
+    _say("directions", B, T, H, dk, dv, dtype, nb.nna_decay_attention_workspace(B, T, H, dk, dv), nb.nna_decay_attention_backward_workspace(B, T, H, dk, dv))
+    args = _inputs(B, T, H, dk, dv, dtype, seed=T + H)
+    args[4][0] = 1 - 2.0**-11
+    _check(nb, *args)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,d", [(100, 64), (1500, 64), (100, 128), (1500, 100)])
+def test_gradients_of_keys_and_values_alone(nb, dtype, T, d):
+    """Without gq the others have the same bits."""
+    from ctypes import c_longlong
+
+    q, k, v, go, decay, first, glast = _inputs(2, T, 3, d, d, dtype, seed=d)
+    _say("no gq", T, d, dtype)
+    _, gk, gv, gfirst = nb.nna_decay_attention_backward(go, q, k, v, decay, state=first, gstate=glast, want_gstate=True)
+    alone = torch.full_like(k, float("nan")), torch.full_like(v, float("nan")), torch.full_like(first, float("nan"))
+    strides = (c_longlong * 3)(T * 3 * d, 3 * d, d)
+    need = nb.nna_decay_attention_backward_workspace(2, T, 3, d, d)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    status = nb.lib().nna_decay_attention_backward(
+        go.data_ptr(), q.data_ptr(), strides, k.data_ptr(), strides, v.data_ptr(), strides, nb.NNA_F32 if dtype == torch.float32 else nb.NNA_BF16, 2, T, 3, d, d,
+        decay.data_ptr(), d**-0.5, None, first.data_ptr(), glast.data_ptr(), None, alone[0].data_ptr(), alone[1].data_ptr(), alone[2].data_ptr(),
+        ws.data_ptr() if need else None, need, 0, torch.cuda.current_stream().cuda_stream)
+    assert status == nb.NNA_OK
+    for a, b in zip(alone, (gk, gv, gfirst)):
+        assert torch.equal(a, b)
