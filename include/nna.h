@@ -642,7 +642,7 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
  *
  * nna_decay_attention_backward: given gout_dev [B, T, H, dv] (contiguous) and glast_dev (or NULL: 0), the gradients of a loss with respect to out and
  * the last state: gq_dev [B, T, H, dk] (or NULL), gk_dev [B, T, H, dk], gv_dev [B, T, H, dv] (contiguous, of `type`) and gfirst_dev [B, H, dk, dv]
- * (or NULL), in nna_decay_attention_backward_workspace bytes.  The same inputs give the same bits.
+ * (or NULL; not glast_dev), in nna_decay_attention_backward_workspace bytes.  The same inputs give the same bits.
  * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_UNSUPPORTED (type, dk or dv above 128), NNA_ERR_SHAPE.  T = 0 or B = 0 is no error.
  */
 nna_status nna_decay_attention_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes);

@@ -97,6 +97,8 @@ nna_status states_size(long long B, long long T, long long H, long long dk, long
   const nna_status s = check_heads(NNA_F32, B, T, H, dk, dv);
   if (s != NNA_OK) return s;
   int segments, chunks;
+  *bytes = 0;
+  if (!B) return NNA_OK;
   *bytes = std::max(decay_segments(B, T, (int)H, (int)dk, (int)dv, NNA_F32, backward, &segments, &chunks),
                     decay_segments(B, T, (int)H, (int)dk, (int)dv, NNA_BF16, backward, &segments, &chunks));
   return NNA_OK;
