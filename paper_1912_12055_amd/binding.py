@@ -1041,19 +1041,19 @@ _strides3, _strides2 = _LL * 3, _LL * 2
 
 def _heads(q, k, v, axes):
     """(nna_dtype, sizes, the arguments q, k, v stand for) of [B, (T,) H, d] tensors; their strides but for the last are their own."""
-    t = _type_of(q, "q", ("float32", "bfloat16"))
-    for name, x in (("k", k), ("v", v)):
-        if _type_of(x, name, ("float32", "bfloat16")) != t or x.device != q.device:
-            raise TypeError("q, k and v must be of one type, on one device")
-    if q.dim() != axes or k.shape != q.shape or v.dim() != axes or v.shape[:-1] != q.shape[:-1]:
+    import torch
+
+    t, tensor, dtype, device = _type_of(q, "q", ("float32", "bfloat16")), torch.Tensor, q.dtype, q.device
+    if not (isinstance(k, tensor) and isinstance(v, tensor) and k.dtype == dtype and v.dtype == dtype and k.device == device and v.device == device):
+        raise TypeError("q, k and v must be tensors of one type, on one device")
+    shape, wide = q.shape, v.shape
+    if len(shape) != axes or k.shape != shape or len(wide) != axes or wide[:-1] != shape[:-1]:
         raise TypeError("q and k must be " + ("[B, T, H, dk] and v [B, T, H, dv]" if axes == 4 else "[B, H, dk] and v [B, H, dv]"))
-    args = []
-    for x in (q, k, v):
-        s = x.stride()
-        if x.shape[-1] != 1 and s[-1] != 1:
-            raise TypeError("a head's values must lie next to each other")
-        args += [x.data_ptr(), (_strides3 if axes == 4 else _strides2)(*s[:-1])]
-    return t, (*q.shape, v.shape[-1]), args
+    dk, dv, array = shape[-1], wide[-1], _strides3 if axes == 4 else _strides2
+    (*sq, lq), (*sk, lk), (*sv, lv) = q.stride(), k.stride(), v.stride()
+    if (dk != 1 and (lq != 1 or lk != 1)) or (dv != 1 and lv != 1):
+        raise TypeError("a head's values must lie next to each other")
+    return t, (*shape, dv), (q.data_ptr(), array(*sq), k.data_ptr(), array(*sk), v.data_ptr(), array(*sv))
 
 
 def _lengths(lengths, B, device):

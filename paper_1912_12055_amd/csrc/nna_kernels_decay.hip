@@ -746,7 +746,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void decay_join_kernel(DecayMix P,
 }
 
 // One frame: the state is read and written once, four columns of it to a lane, a slab of 32 columns to a workgroup.  Bound by the state's bytes: 256 streams of 16
-// heads of 128 x 128, 98 us, 5.5 TB/s; one stream of 8 heads of 64 x 64, 4 us of a call of 11.
+// heads of 128 x 128, 98 us, 5.5 TB/s; one stream of 8 heads of 64 x 64, 4 us of a call of 10.
 constexpr int STEP_COLUMNS = 32, STEP_RUNS = 256 / (STEP_COLUMNS / 4);
 template <typename T>
 __global__ __launch_bounds__(256) void decay_step_kernel(DecayStep P) {
