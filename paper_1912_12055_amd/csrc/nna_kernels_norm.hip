@@ -357,6 +357,7 @@ __global__ __launch_bounds__(JOIN_COLUMNS* JOIN_RUNS) void norm_join_kernel(cons
 // 16 x 1,025 x 431, float32: 17 us forward (3.2 TB/s), 33 backward (2.6); 64 x 128 x 216 to bfloat16: 7 and 9.  Two workgroups a CU, each of which reads, turns and
 // writes in turn: loads, LDS and stores have to come from different workgroups to overlap.
 constexpr int FR_THREADS = 512, FR_WAVES = FR_THREADS / 64;
+constexpr long long MAX_TILES = 1LL << 22;  // of a launch: its threads are counted in 32 bits
 __host__ __device__ constexpr int frames_pitch(int width) { return width | 1; }  // odd: a column's frames are in different banks
 // as many frames as leave two workgroups of 72 KB a CU: 128 (64, 32) consecutive bytes of every bin
 constexpr int FR_WIDTH_32 = 558, FR_WIDTH_16 = 1088;
@@ -423,7 +424,7 @@ __global__ __launch_bounds__(FR_THREADS) void norm_frames_kernel(NormParams P) {
   const int width = P.width, pitch = frames_pitch(width), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const long long tiles = (P.T + FRAMES - 1) / FRAMES;
   const float inv = 1.f / (float)width;
-  const long long at = tile_of(blockIdx.x, gridDim.x), b = at / tiles, t0 = (at % tiles) * FRAMES;
+  const long long at = P.first_tile + tile_of(blockIdx.x, gridDim.x), b = at / tiles, t0 = (at % tiles) * FRAMES;
   const int frames = (int)(P.T - t0 < FRAMES ? P.T - t0 : FRAMES);
   float read[N];
   read_tile<FRAMES, PAIRS>(static_cast<const float*>(P.x) + b * width * P.T + t0, P.T, width, frames, read);
@@ -673,7 +674,10 @@ hipError_t launch_norm(const NormParams& P, int x_type, int y_type, bool frames,
       return by_frame(P.width, [&](auto f, auto pairs) {
         constexpr int F = f.value, C = pairs.value;
         const size_t lds = frames_lds(P.width, F);
-        hipLaunchKernelGGL((norm_frames_kernel<decltype(y), F, C>), dim3((unsigned)(P.batch * ((P.T + F - 1) / F))), dim3(FR_THREADS), lds, stream, P);
+        const long long tiles = P.batch * ((P.T + F - 1) / F);
+        NormParams Q = P;
+        for (Q.first_tile = 0; Q.first_tile < tiles; Q.first_tile += MAX_TILES)
+          hipLaunchKernelGGL((norm_frames_kernel<decltype(y), F, C>), dim3((unsigned)std::min(tiles - Q.first_tile, MAX_TILES)), dim3(FR_THREADS), lds, stream, Q);
         return hipGetLastError();
       });
     });

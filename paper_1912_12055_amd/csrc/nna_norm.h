@@ -15,6 +15,7 @@ struct NormParams {
   const void* gout;
   long long rows, row_stride;  // elements between rows of x
   long long batch, T;          // frames only: rows = batch * T
+  long long first_tile;        // frames, forward: of this launch
   int width;
   float eps;
   const float* weight;  // or NULL: ones

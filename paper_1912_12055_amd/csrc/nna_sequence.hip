@@ -85,8 +85,8 @@ nna_status check_heads(int type, long long B, long long T, long long H, long lon
   if (type == NNA_F16) return fail(NNA_ERR_UNSUPPORTED, "float16 has no range for the weights: float32 or bfloat16");
   if (B < 0 || T < 0 || H < 1 || dk < 1 || dv < 1) return fail(NNA_ERR_SHAPE, "B and T must not be negative, H, dk and dv at least 1");
   if (dk > DECAY_HEAD_MAX || dv > DECAY_HEAD_MAX) return fail(NNA_ERR_UNSUPPORTED, "heads of more than " + std::to_string(DECAY_HEAD_MAX) + " values");
-  // a workgroup for each (sequence, head), its segments and its blocks of 1,024 values of a state
-  if (H > 65536 || B > (1LL << 24) / H) return fail(NNA_ERR_SHAPE, "H or B H is too large");
+  // (sequence, head)s times the lanes of their workgroups, up to four of 256 or one of 1,024, are less than 2^32 in a launch
+  if (H > 65536 || B > (1LL << 21) / H) return fail(NNA_ERR_SHAPE, "H or B H is too large");
   if (T > INT_MAX - 4 * DECAY_CHUNK) return fail(NNA_ERR_SHAPE, "T is too large");
   return NNA_OK;
 }

@@ -51,7 +51,7 @@ def step(q=P, state=P, type=F32, H=8, dk=8, scale=1.0):
     (lambda: back(ws=P + 4), ARG), (lambda: back(gx=P), ARG), (lambda: back(gt=F16, xt=BF16), ARG), (lambda: back(width=0), SHAPE),
     (lambda: attend(q=None), ARG), (lambda: attend(out=None), ARG), (lambda: attend(qs=None), ARG), (lambda: attend(decay=None), ARG), (lambda: attend(scale=0.0), ARG),
     (lambda: attend(scale=float("inf")), ARG), (lambda: attend(type=F16), UNSUPPORTED), (lambda: attend(type=7), ARG), (lambda: attend(dk=129), UNSUPPORTED),
-    (lambda: attend(dv=0), SHAPE), (lambda: attend(H=0), SHAPE), (lambda: attend(T=-1), SHAPE), (lambda: attend(B=1 << 40), SHAPE),
+    (lambda: attend(dv=0), SHAPE), (lambda: attend(H=0), SHAPE), (lambda: attend(T=-1), SHAPE), (lambda: attend(B=1 << 40), SHAPE), (lambda: attend(B=1 << 19), SHAPE),
     (lambda: attend(qs=strides(0, (1 << 24) + 1, 8)), SHAPE), (lambda: attend(qs=strides(0, -8, 8)), SHAPE), (lambda: attend(T=20000, ws=None, size=0), ARG),
     (lambda: attend(T=20000, size=256), ARG), (lambda: attend(T=20000, ws=P + 16), ARG),
     (lambda: attend_back(g=None), ARG), (lambda: attend_back(gk=None), ARG), (lambda: attend_back(gv=None), ARG), (lambda: attend_back(type=F16), UNSUPPORTED),
