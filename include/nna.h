@@ -636,8 +636,8 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
  *   first_dev, last_dev  [B, H, dk, dv] float32 or NULL: the state before the first frame (NULL: 0), and after the last.  They may be the same
  *   out_dev      [B, T, H, dv] of `type`, contiguous
  *   workspace_dev  256-byte aligned, nna_decay_attention_workspace bytes (0: may be NULL)
- * States are float32, and sums of products of inputs are exact to float32; for NNA_BF16 the weights l^(t-s) (q . k) and the state are rounded to
- * bfloat16 where they are multiplied with v and q (an error like that of the rounded output).  A value of v that is not finite makes the
+ * States are float32, and sums of products of inputs are exact to float32; for NNA_BF16 the weights l^(t-s) (q . k) and the state are held to 2^-17
+ * where they are multiplied with v and q, some 2^-9 of what the output's own rounding takes.  A value of v that is not finite makes the
  * outputs of its head NaN from its frame on, and the last state; one of k likewise by the rules of arithmetic; one of q its own frame's.
  *
  * nna_decay_attention_backward: given gout_dev [B, T, H, dv] (contiguous) and glast_dev (or NULL: 0), the gradients of a loss with respect to out and

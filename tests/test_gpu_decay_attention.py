@@ -376,3 +376,32 @@ def test_gradients_of_keys_and_values_alone(nb, dtype, T, d):
     assert status == nb.NNA_OK
     for a, b in zip(alone, (gk, gv, gfirst)):
         assert torch.equal(a, b)
+
+
+SIZES = [(2, 200, 2, 64, 64), (1, 431, 2, 128, 128), (2, 150, 2, 100, 33), (1, 3000, 2, 64, 64), (1, 2111, 2, 128, 64)]
+
+
+def _all_of(nb, q, k, v, go, decay, first, glast):
+    o, last = nb.nna_decay_attention(q, k, v, decay, state=first, want_state=True)
+    gq, gk, gv, gfirst = nb.nna_decay_attention_backward(go, q, k, v, decay, state=first, gstate=glast, want_gstate=True)
+    return dict(o=o, gq=gq, gk=gk, gv=gv, last=last, gfirst=gfirst)
+
+
+@pytest.mark.parametrize("given", [True, False])
+@pytest.mark.parametrize("B,T,H,dk,dv", SIZES)
+def test_bfloat16_results_are_off_by_their_own_rounding_alone(nb, B, T, H, dk, dv, given):
+    """A float32 sum that is an operand again (weights, state) is held to 2^-17 at least, so what comes before the last rounding is off by some units of
+    2^-17 of the result's norm (roundings of either sign add as squares), a 64th of the 2^-9 that the rounding takes or less; a rounding of a value that is off by e
+    is off by at most 2 e more than that of the value: 1 + 2 / 64 of the exact result's own rounding, and 1.05 is allowed."""
+    _say("own rounding", B, T, H, dk, dv, given)
+    q, k, v, go, decay, first, glast = _inputs(B, T, H, dk, dv, torch.bfloat16, seed=T + 1)
+    e = _exact(q, k, v, decay, first, None, go, glast)
+    if given:
+        got = _all_of(nb, q, k, v, go, decay, first, glast)
+    else:  # no state is given back
+        gq, gk, gv, _ = nb.nna_decay_attention_backward(go, q, k, v, decay, state=first, gstate=glast)
+        got = dict(o=nb.nna_decay_attention(q, k, v, decay, state=first), gq=gq, gk=gk, gv=gv)
+    for name in ("o", "gq", "gk", "gv"):
+        ref = e[name][0]
+        own = (ref.bfloat16().double() - ref).norm()
+        assert (got[name].double() - ref).norm() <= 1.05 * own, (name, float((got[name].double() - ref).norm() / own))
