@@ -405,3 +405,18 @@ def test_bfloat16_results_are_off_by_their_own_rounding_alone(nb, B, T, H, dk, d
         ref = e[name][0]
         own = (ref.bfloat16().double() - ref).norm()
         assert (got[name].double() - ref).norm() <= 1.05 * own, (name, float((got[name].double() - ref).norm() / own))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,T,H,dk,dv", SIZES)
+def test_float32_results_hold_float32(nb, B, T, H, dk, dv, dtype):
+    """Roundings of either sign add as squares: a product of planes leaves out or rounds off some 2^-24, its power of the decay two of them, and the sums some ten
+    roundings of partial sums: 16 units, 1e-6 of the norm.  Operands of two planes alone would be off by 2^-17 / sqrt(3) = 4.4e-6 each."""
+    _say("float32", B, T, H, dk, dv, dtype)
+    args = _inputs(B, T, H, dk, dv, dtype, seed=T + 2)
+    q, k, v, go, decay, first, glast = args
+    e = _exact(q, k, v, decay, first, None, go, glast)
+    for name, x in _all_of(nb, *args).items():
+        if x.dtype == torch.float32:
+            ref = e[name][0]
+            assert (x.double() - ref).norm() <= 1e-6 * ref.norm(), (name, float((x.double() - ref).norm() / ref.norm()))
