@@ -47,12 +47,24 @@ __device__ __forceinline__ f32x4 mma(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB
 }
 __device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
+// What a first plane is rounded from: the last 2^-9 of float32's range would round to an infinity, so it is bfloat16's largest there and the next planes hold the rest;
+// an infinity or a NaN stays one in them.  Beside bfloat16 values (T), none of which is larger, it is left out (16,384 frames, 64 heads of 128, both directions: 1,429 us
+// with it, 1,395 without): a state or weight that near to float32's end is then an infinity to the frames it meets.
+template <typename T>
+__device__ __forceinline__ float in_range(float v) { return sizeof(T) == 4 ? __builtin_amdgcn_fmed3f(v, -0x1.fep127f, 0x1.fep127f) : v; }
+template <typename T, typename V>
+__device__ __forceinline__ V all_in_range(V v) {
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(V) / sizeof(float)); ++i) v[i] = in_range<T>(v[i]);
+  return v;
+}
+
 // two accumulators (k and 16 + k) as an operand of N planes
-template <int N>
+template <typename T, int N>
 __device__ __forceinline__ void split(f32x4 v, f32x4 w, bf16x8 (&o)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const bf16x4 a = __builtin_convertvector(v, bf16x4), b = __builtin_convertvector(w, bf16x4);
+    const bf16x4 a = __builtin_convertvector(i ? v : all_in_range<T>(v), bf16x4), b = __builtin_convertvector(i ? w : all_in_range<T>(w), bf16x4);
     o[i] = join(a, b);
     if (i + 1 < N) {
       v -= __builtin_convertvector(a, f32x4);
@@ -142,7 +154,7 @@ struct Kind<float> {
     f32x8 left = v;
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      const bf16x8 w = __builtin_convertvector(left, bf16x8);
+      const bf16x8 w = __builtin_convertvector(i ? left : all_in_range<float>(left), bf16x8);
       *reinterpret_cast<bf16x8*>(p + i * plane) = w;
       if (i < 2) left -= __builtin_convertvector(w, f32x8);
     }
@@ -150,7 +162,7 @@ struct Kind<float> {
   static __device__ __forceinline__ void put1(bf16* p, int plane, float v) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      p[i * plane] = (bf16)v;
+      p[i * plane] = (bf16)(i ? v : in_range<float>(v));
       v -= (float)p[i * plane];
     }
   }
@@ -466,7 +478,7 @@ __device__ __forceinline__ void mix_chunks(const DecayMix& P, const int workgrou
           }
 #pragma unroll
           for (int p = 0; p < SUMS; ++p) {
-            const bf16x4 w = __builtin_convertvector(s, bf16x4);
+            const bf16x4 w = __builtin_convertvector(p ? s : all_in_range<T>(s), bf16x4);
             weights[(block * SUMS + p) * 64 + lane] = w;
             s -= __builtin_convertvector(w, f32x4);
           }
@@ -481,7 +493,7 @@ __device__ __forceinline__ void mix_chunks(const DecayMix& P, const int workgrou
       for (int r = 0; r < RB; r += 2) {
         bf16x8 vs[CB][SUMS];
 #pragma unroll
-        for (int m = 0; m < CB; ++m) split(state[r][m], state[r + 1][m], vs[m]);
+        for (int m = 0; m < CB; ++m) split<T>(state[r][m], state[r + 1][m], vs[m]);
 #pragma unroll
         for (int i = 0; i < IB; ++i) {
           bf16x8 va[NP];
@@ -541,7 +553,7 @@ __device__ __forceinline__ void mix_chunks(const DecayMix& P, const int workgrou
         f32x8 v = __builtin_convertvector(vc[m][NP - 1], f32x8);
 #pragma unroll
         for (int p = NP - 2; p >= 0; --p) v += __builtin_convertvector(vc[m][p], f32x8);
-        split(__builtin_shufflevector(v, v, 0, 1, 2, 3) * weight[0], __builtin_shufflevector(v, v, 4, 5, 6, 7) * weight[1], vs[m]);
+        split<T>(__builtin_shufflevector(v, v, 0, 1, 2, 3) * weight[0], __builtin_shufflevector(v, v, 4, 5, 6, 7) * weight[1], vs[m]);
       }
 #pragma unroll
       for (int r = 0; r < RB; ++r) {

@@ -420,3 +420,62 @@ def test_float32_results_hold_float32(nb, B, T, H, dk, dv, dtype):
         if x.dtype == torch.float32:
             ref = e[name][0]
             assert (x.double() - ref).norm() <= 1e-6 * ref.norm(), (name, float((x.double() - ref).norm() / ref.norm()))
+
+
+def _of_head(name, x, h):
+    return x[:, h] if name in ("last", "gfirst") else x[:, :, h]
+
+
+@pytest.mark.parametrize("T,dk,dv", [(100, 64, 64), (1500, 64, 64), (100, 128, 128), (100, 65, 63), (100, 7, 100)])
+def test_the_largest_float32_values_are_values(nb, T, dk, dv):
+    """float32's largest is above bfloat16's: what it enters is what it would be times 1 (powers of two throughout), and no frame before it knows it."""
+    _say("largest", T, dk, dv)
+    most, at = torch.finfo(torch.float32).max, 77
+    q, k, v, go, decay, first, glast = _inputs(1, T, 2, dk, dv, torch.float32, seed=T + dk, state=False)
+    clean = _all_of(nb, q, k, v, go, decay, None, None)
+    for name, x in (("v", v), ("k", k), ("q", q), ("go", go)):
+        for last in (False, True):
+            keep, d = x.clone(), x.shape[-1] - 1 if last else 0
+            x[0, at, 0, d] = most
+            got = _all_of(nb, q, k, v, go, decay, None, None)
+            for out in ("o", "gq") if name != "go" else ("o",):
+                assert torch.equal(got[out][0, :at], clean[out][0, :at]), (name, out)
+            for out in ("gk", "gv") if name in ("go", "q") else ():
+                assert torch.equal(got[out][0, at + 1:], clean[out][0, at + 1:]), (name, out)
+            for out in got:
+                assert torch.equal(_of_head(out, got[out], 1), _of_head(out, clean[out], 1)), (name, out)
+            x.copy_(keep)
+    # one value through a state and weights: 2^-7 of it everywhere
+    q, k, v = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    q[..., 0], k[0, at, 0, 0], v[0, at, 0, dv - 1] = 2.0**-7, 1.0, most
+    one = torch.ones_like(decay)
+    o, state = nb.nna_decay_attention(q, k, v, one, scale=1.0, want_state=True)
+    assert (o[0, at:, 0, dv - 1] == most * 2.0**-7).all() and not o[0, :at].any() and not o[0, :, :, :dv - 1].any()
+    assert state[0, 0, 0, dv - 1] == most and int((state != 0).sum()) == 1
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,dk,dv", [(100, 128, 128), (1500, 128, 128), (100, 65, 63), (1500, 33, 100), (40, 5, 3)])
+def test_a_value_that_is_not_finite_in_heads_of_other_sizes(nb, dtype, T, dk, dv):
+    """no output before it, no gradient of keys and values after a go or q that has one, no other head; in the first column and in the last"""
+    _say("not finite", T, dk, dv, dtype)
+    q, k, v, go, decay, first, glast = _inputs(2, T, 2, dk, dv, dtype, seed=dk)
+    clean, at = _all_of(nb, q, k, v, go, decay, first, glast), 35
+    for name, x in (("v", v), ("k", k), ("q", q), ("go", go)):
+        for value in (float("nan"), float("inf")):
+            for d in (0, x.shape[-1] - 1):
+                keep = x.clone()
+                x[1, at, 0, d] = value
+                got = _all_of(nb, q, k, v, go, decay, first, glast)
+                before = ("o", "gq") if name != "go" else ("o",)
+                after = ("gk", "gv") if name in ("go", "q") else ()
+                for out in got:
+                    a, b = got[out], clean[out]
+                    assert torch.equal(a[0], b[0]), (name, out)
+                    assert torch.equal(_of_head(out, a, 1), _of_head(out, b, 1)), (name, out)
+                    if out in before:
+                        assert torch.equal(a[1, :at], b[1, :at]), (name, out)
+                    if out in after:
+                        assert torch.equal(a[1, at + 1:], b[1, at + 1:]), (name, out)
+                assert not torch.isfinite(torch.cat([t[1].flatten() for t in got.values()])).all()
+                x.copy_(keep)
