@@ -780,7 +780,7 @@ def nna_forward_keep(plan: Plan, x, stream=None, size=None, kept=None):
 
     if size is None:
         size = nna_kept_bytes(plan, *x.shape)
-    spec = None
+    spec, given = None, kept
     if kept is None:
         kept = torch.empty(size, dtype=torch.uint8, device=x.device)
     elif not (kept.is_cuda and kept.is_contiguous() and kept.device == x.device and kept.numel() * kept.element_size() >= size):
@@ -792,7 +792,10 @@ def nna_forward_keep(plan: Plan, x, stream=None, size=None, kept=None):
     def fn(handle, xp, B, L, op, st):
         return lib().nna_forward_keep(handle, xp, B, L, op, None if spec is None else spec.data_ptr(), kept.data_ptr(), size, st)
 
-    return _run(fn, plan, x, None, stream), kept
+    out = _run(fn, plan, x, None, stream)
+    if given is not None:
+        _written(given)
+    return out, kept
 
 
 def nna_backward_kept(plan: Plan, x, gout, kept, want_gmelw=False, want_gw=True, want_gx=True, stream=None):
@@ -866,6 +869,16 @@ def _vector(t, name, shape, device, none=False):
     return t.data_ptr()
 
 
+def _written(*tensors):
+    """Tells autograd of tensors of the caller's that a call has written through their pointers, as torch's own in-place operations do: a graph that
+    holds one of them for its backward pass then refuses to run on the new values.  (0.3 us a tensor.)"""
+    from torch.autograd.graph import increment_version
+
+    for t in tensors:
+        if t is not None:
+            increment_version(t)
+
+
 def _row_stride(x):
     """Elements between the rows of x[..., width] if its rows are at one distance from each other, or None."""
     shape, strides = x.shape, x.stride()
@@ -929,7 +942,7 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
     if keep not in (0, 8, 32):
         raise ValueError("keep: 0, 8 or 32")
     shape, width, device = x.shape, x.shape[-1], x.device
-    out_dtype = x.dtype if out_dtype is None else out_dtype
+    out_dtype, given = x.dtype if out_dtype is None else out_dtype, out
     if out is None:
         out = torch.empty_like(x, dtype=out_dtype, memory_format=torch.contiguous_format)
     elif not (isinstance(out, torch.Tensor) and out.device == device and out.dtype == out_dtype and out.is_contiguous() and out.shape == shape):
@@ -957,6 +970,8 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
         _check(lib().nna_layer_norm_frames(x.data_ptr(), shape[0], width, shape[1], w, b, eps, out.data_ptr(), yt, sp, device.index, st))
     else:
         raise TypeError("x must be rows at one distance from each other, or the transpose of a contiguous float32 [B, bins, T]")
+    if given is not None:
+        _written(given)
     return (out, kept) if keep else out
 
 
@@ -1025,7 +1040,7 @@ def nna_unpack8(codes, scales, dtype=None, out=None, stream=None):
     if not (isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dtype == torch.int8 and codes.is_contiguous() and codes.dim()):
         raise TypeError("codes must be a contiguous int8 CUDA tensor")
     width = codes.shape[-1]
-    sp = _vector(scales, "scales", (*codes.shape[:-1], -(-width // NNA_BLOCK8)), codes.device)
+    sp, given = _vector(scales, "scales", (*codes.shape[:-1], -(-width // NNA_BLOCK8)), codes.device), out
     if out is None:
         out = torch.empty_like(codes, dtype=torch.float32 if dtype is None else dtype)
     elif not (out.is_contiguous() and out.shape == codes.shape and out.device == codes.device and dtype in (None, out.dtype)):
@@ -1033,6 +1048,8 @@ def nna_unpack8(codes, scales, dtype=None, out=None, stream=None):
     ot = _type_of(out, "out")
     _check(lib().nna_unpack8(codes.data_ptr(), sp, codes.numel() // width if width else 0, width, out.data_ptr(), ot, codes.device.index,
                              _stream_on(codes.device, stream)))
+    if given is not None:
+        _written(given)
     return out
 
 
@@ -1089,6 +1106,7 @@ def nna_decay_attention(q, k, v, decay, scale=None, state=None, lengths=None, wa
     t, (B, T, H, dk, dv), args = _heads(q, k, v, 4)
     device = q.device
     dp, sp, lp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device, none=True), _lengths(lengths, B, device)
+    given = out
     if out is None:
         out = q.new_empty((B, T, H, dv))
     elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == (B, T, H, dv) and out.device == device):
@@ -1101,6 +1119,8 @@ def nna_decay_attention(q, k, v, decay, scale=None, state=None, lengths=None, wa
         ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     _check(lib().nna_decay_attention(*args, t, B, T, H, dk, dv, dp, dk**-0.5 if scale is None else scale, lp, sp, last.data_ptr() if want_state else None,
                                      out.data_ptr(), *ws, device.index, _stream_on(device, stream)))
+    if given is not None:
+        _written(given)
     return (out, last) if want_state else out
 
 
@@ -1135,10 +1155,12 @@ def nna_decay_attention_step(q, k, v, decay, state, scale=None, out=None, stream
     t, (B, H, dk, dv), args = _heads(q, k, v, 3)
     device = q.device
     dp, sp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device)
+    given = out
     if out is None:
         out = q.new_empty((B, H, dv))
     elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == (B, H, dv) and out.device == device):
         raise TypeError(f"out must be a contiguous {q.dtype} tensor of shape {(B, H, dv)}")
     _check(lib().nna_decay_attention_step(*args, t, B, H, dk, dv, dp, dk**-0.5 if scale is None else scale, sp, out.data_ptr(), device.index,
                                           _stream_on(device, stream)))
+    _written(state, given)
     return out

@@ -182,3 +182,37 @@ def test_the_example_learns_and_streams(layers):
     assert torch.isfinite(state).all()
     # bfloat16 weights and states in one, float32 states in the other: a few roundings of 2^-9 between them
     assert (example.stream(model, tokens, prompt=17) - whole).norm() <= 0.02 * whole.norm()
+
+
+def test_what_the_calls_write_in_place_is_noticed(layers):
+    """A tensor that a recorded call holds for its backward pass, written by a later call through its pointer: a state by `step`, outputs that are given."""
+    from paper_1912_12055_amd import binding as nb
+    g = _gen(8)
+    q = torch.randn(2, 6, 2, 16, device=DEV, generator=g).requires_grad_()
+    mix, state = layers.DecayAttention(2), torch.randn(2, 2, 16, 16, device=DEV, generator=g)
+    o = mix(q, q, q, state=state)
+    with torch.no_grad():
+        mix.step(q[:, 0], q[:, 0], q[:, 0], state)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        o.sum().backward()
+    for inference in (False, True):  # nothing else changes
+        with torch.inference_mode(inference):
+            s = torch.zeros(2, 2, 16, 16, device=DEV)
+            mix.step(q[:, 0].detach(), q[:, 0].detach(), q[:, 0].detach(), s)
+            assert s.any()
+
+    x = torch.randn(5, 16, device=DEV, generator=g).requires_grad_()
+    codes, scales = nb.nna_pack8(x.detach())
+    for write in (lambda out: nb.nna_layer_norm(x.detach(), out=out), lambda out: nb.nna_unpack8(codes, scales, out=out),
+                  lambda out: nb.nna_decay_attention(*3 * [out.new_ones(1, 5, 1, 16)], mix.decay[:1], out=out.view(1, 5, 1, 16)),
+                  lambda out: nb.nna_decay_attention_step(*3 * [out.new_ones(5, 1, 16)], mix.decay[:1], out.new_zeros(5, 1, 16, 16), out=out.view(5, 1, 16))):
+        held = torch.randn(5, 16, device=DEV, generator=g)
+        y = (x * held).sum()
+        write(held)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    layer = layers.STFT(n_fft=512, hop_length=128, trainable=True, output_format="Power")
+    wave = torch.randn(2, 4000, device=DEV, generator=g)
+    kept = torch.zeros(nb.nna_kept_bytes(layer.plan, 2, 4000), dtype=torch.uint8, device=DEV)
+    nb.nna_forward_keep(layer.plan, wave, kept=kept)
+    assert kept._version == 1
