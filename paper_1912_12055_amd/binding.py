@@ -879,6 +879,19 @@ def _written(*tensors):
             increment_version(t)
 
 
+def _bytes_of(t):
+    """The addresses from a tensor's first element to its last."""
+    if not t.numel():
+        return 0, 0
+    at = t.data_ptr()
+    return at, at + (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size()
+
+
+def _overlap(a, b):
+    (a0, a1), (b0, b1) = _bytes_of(a), _bytes_of(b)
+    return a0 < b1 and b0 < a1
+
+
 def _row_stride(x):
     """Elements between the rows of x[..., width] if its rows are at one distance from each other, or None."""
     shape, strides = x.shape, x.stride()
@@ -933,7 +946,7 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
     also of `out_dtype` bfloat16 or float16).  x's rows lie at one distance from each other, or x is frames as the transforms write
     them, ``spec.transpose(1, 2)`` of a contiguous float32 spec[B, bins, T].  weight, bias: float32 [width].
     keep: 0, or what is kept for nna_layer_norm_backward, returned behind y as a NormKept: 32 the input as it is, 8 the input in 8 bits
-    (nna_pack8's; rows only, y of x's type)."""
+    (nna_pack8's; rows only, y of x's type).  `out` may be x itself, of contiguous rows and x's type, unless x is what is kept."""
     import torch
 
     xt = _type_of(x, "x")
@@ -947,6 +960,8 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
         out = torch.empty_like(x, dtype=out_dtype, memory_format=torch.contiguous_format)
     elif not (isinstance(out, torch.Tensor) and out.device == device and out.dtype == out_dtype and out.is_contiguous() and out.shape == shape):
         raise TypeError(f"out must be a contiguous {out_dtype} CUDA tensor of shape {tuple(shape)}")
+    if given is not None and keep == 32 and _overlap(out, x):
+        raise ValueError("keep=32 keeps x itself: out must not share its memory")
     yt = _type_of(out, "out")
     w, b = _vector(weight, "weight", (width,), device, none=True), _vector(bias, "bias", (width,), device, none=True)
     rows = x.numel() // width if width else 0

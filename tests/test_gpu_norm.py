@@ -338,3 +338,29 @@ def test_on_another_stream_and_in_a_graph(nb):
         torch.cuda.synchronize()
         got = [t.clone() for t in out]
         assert all(torch.equal(a, c) for a, c in zip(step(), got)), k
+
+
+def test_rows_normalised_in_place(nb):
+    """y over x is right where x is not what is kept, and refused where it is: the gradients would be those of y."""
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        for width in (40, 640, 5000):
+            _say("in place", dtype, width)
+            x, w, b, g = _inputs((37, width), dtype, seed=width)
+            g = g.to(dtype)
+            y, kept = nb.nna_layer_norm(x, w, b, keep=8)
+            ref = nb.nna_layer_norm_backward(g, kept, w)
+            z = x.clone()
+            assert nb.nna_layer_norm(z, w, b, out=z) is z and torch.equal(z, y)
+            z = x.clone()
+            z, kept = nb.nna_layer_norm(z, w, b, keep=8, out=z)
+            assert torch.equal(z, y) and all(torch.equal(a, c) for a, c in zip(nb.nna_layer_norm_backward(g, kept, w), ref))
+            z = x.clone()
+            for out in (z, z.view(-1)[:x.numel()].view(x.shape)):
+                with pytest.raises(ValueError):
+                    nb.nna_layer_norm(z, w, b, keep=32, out=out)
+            two = torch.cat([x, x])
+            with pytest.raises(ValueError):
+                nb.nna_layer_norm(two[:37], w, b, keep=32, out=two[36:73])
+            assert torch.equal(two, torch.cat([x, x]))
+            out, kept = nb.nna_layer_norm(two[:37], w, b, keep=32, out=two[37:])  # beside it: nothing is shared
+            assert torch.equal(two[37:], y) and torch.equal(kept.x, x)
