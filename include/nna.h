@@ -577,7 +577,7 @@ typedef enum { NNA_F32 = 0, NNA_BF16 = 1, NNA_F16 = 2 } nna_dtype;
  * Layer norm of `rows` rows of `width` values (1..16384):  y = h w + b,  h = (x - m) r,  m the row's mean, r = 1 / sqrt(mean((x - m)^2) + eps).
  *   x_dev        of x_type, consecutive values of a row next to each other, rows row_stride elements apart (0: all the same row)
  *   weight_dev, bias_dev  [width] float32, or NULL: ones, zeros
- *   y_dev        [rows, width] of y_type: x_type, or NNA_BF16 / NNA_F16 where x_type is NNA_F32.  May be x_dev where the types and strides are equal.
+ *   y_dev        [rows, width] of y_type: x_type, or NNA_BF16 / NNA_F16 where x_type is NNA_F32.  May be x_dev where the types are equal and row_stride is width (not of frames).
  *   stats_dev    NULL, or [rows, 2] float32 for the backward call: m and r
  *   codes_dev, scales_dev  both NULL, or x in 8 bits for the backward call (y_type = x_type): as nna_pack8 writes it
  * nna_layer_norm_frames normalises the frames of the library's own outputs: x_dev[B, width, T] float32, T fastest (width 1..2112);
@@ -594,7 +594,7 @@ nna_status nna_layer_norm_frames(const float* x_dev, long long B, long long widt
  * Gradients of a layer norm, from gout_dev[rows, width] ([B, T, width]) = dLoss/dy of y's type:
  *   gx = r (g - mean(g) - h mean(g h)), g = gout w;   gw = sum over rows of gout h;   gb = sum over rows of gout.
  * x comes as it went into the forward call, or as the codes and scales that call wrote (x_dev NULL); stats_dev from that call.
- *   gx_dev       [rows, width] of x_type ([B, width, T] float32 for frames), or NULL; not x_dev
+ *   gx_dev       [rows, width] of x_type ([B, width, T] float32 for frames), or NULL; not x_dev, and gout_dev only of rows of one type
  *   gw_dev, gb_dev  [width] float32, or NULL
  *   workspace_dev  16-byte aligned, nna_layer_norm_backward_workspace bytes (for frames with B and T; rows B = 0); not read where gw_dev and gb_dev are NULL.
  * The sums over rows are taken in an order that depends on the shape alone: the same inputs give the same bits.
@@ -634,7 +634,7 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
  *   lengths_dev  [B] int32 in device memory, or NULL: T.  Frames from a sequence's length on (below 0: 0, above T: T) take no part: their values are not
  *                used, their outputs and gradients are 0, and the last state is that after the length
  *   first_dev, last_dev  [B, H, dk, dv] float32 or NULL: the state before the first frame (NULL: 0), and after the last.  They may be the same
- *   out_dev      [B, T, H, dv] of `type`, contiguous
+ *   out_dev      [B, T, H, dv] of `type`, contiguous; none of the inputs
  *   workspace_dev  256-byte aligned, nna_decay_attention_workspace bytes (0: may be NULL)
  * States are float32, and sums of products of inputs are exact to float32; for NNA_BF16 the weights l^(t-s) (q . k) and the state are held to 2^-17
  * where they are multiplied with v and q, some 2^-9 of what the output's own rounding takes.  A value of v that is not finite makes the
@@ -642,7 +642,7 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
  *
  * nna_decay_attention_backward: given gout_dev [B, T, H, dv] (contiguous) and glast_dev (or NULL: 0), the gradients of a loss with respect to out and
  * the last state: gq_dev [B, T, H, dk] (or NULL), gk_dev [B, T, H, dk], gv_dev [B, T, H, dv] (contiguous, of `type`) and gfirst_dev [B, H, dk, dv]
- * (or NULL; not glast_dev), in nna_decay_attention_backward_workspace bytes.  The same inputs give the same bits.
+ * (or NULL), none of them an input of the call, in nna_decay_attention_backward_workspace bytes.  The same inputs give the same bits.
  * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_UNSUPPORTED (type, dk or dv above 128), NNA_ERR_SHAPE.  T = 0 or B = 0 is no error.
  */
 nna_status nna_decay_attention_workspace(long long B, long long T, long long H, long long dk, long long dv, size_t* bytes);
@@ -657,7 +657,7 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
                                         const int* lengths_dev, const float* first_dev, const float* glast_dev, void* gq_dev, void* gk_dev,
                                         void* gv_dev, float* gfirst_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream);
 /* One new frame of B sequences: q_dev, k_dev [B, H, dk], v_dev [B, H, dv] (strides[2]: batches, heads), state_dev [B, H, dk, dv] updated in place,
- * out_dev [B, H, dv] of `type`, contiguous: scale q S with the updated S. */
+ * out_dev [B, H, dv] of `type`, contiguous, none of the inputs: scale q S with the updated S. */
 nna_status nna_decay_attention_step(const void* q_dev, const long long* q_strides, const void* k_dev, const long long* k_strides, const void* v_dev,
                                     const long long* v_strides, nna_dtype type, long long B, long long H, long long dk, long long dv,
                                     const float* decay_dev, double scale, float* state_dev, void* out_dev, int device, void* hip_stream);

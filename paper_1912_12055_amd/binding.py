@@ -892,6 +892,13 @@ def _overlap(a, b):
     return a0 < b1 and b0 < a1
 
 
+def _refuse_overlap(out, *inputs):
+    """A given output is written while other workgroups still read the inputs."""
+    for t in inputs:
+        if t is not None and _overlap(out, t):
+            raise ValueError("out must not share memory with an input")
+
+
 def _row_stride(x):
     """Elements between the rows of x[..., width] if its rows are at one distance from each other, or None."""
     shape, strides = x.shape, x.stride()
@@ -962,6 +969,8 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
         raise TypeError(f"out must be a contiguous {out_dtype} CUDA tensor of shape {tuple(shape)}")
     if given is not None and keep == 32 and _overlap(out, x):
         raise ValueError("keep=32 keeps x itself: out must not share its memory")
+    if given is not None:  # (over x only where every row is written where it was read, by the lanes that read it)
+        _refuse_overlap(out, weight, bias, None if x.is_contiguous() and x.dtype == out_dtype and x.data_ptr() == out.data_ptr() else x)
     yt = _type_of(out, "out")
     w, b = _vector(weight, "weight", (width,), device, none=True), _vector(bias, "bias", (width,), device, none=True)
     rows = x.numel() // width if width else 0
@@ -1061,6 +1070,8 @@ def nna_unpack8(codes, scales, dtype=None, out=None, stream=None):
     elif not (out.is_contiguous() and out.shape == codes.shape and out.device == codes.device and dtype in (None, out.dtype)):
         raise TypeError(f"out must be a contiguous CUDA tensor of shape {tuple(codes.shape)}")
     ot = _type_of(out, "out")
+    if given is not None:
+        _refuse_overlap(out, codes, scales)
     _check(lib().nna_unpack8(codes.data_ptr(), sp, codes.numel() // width if width else 0, width, out.data_ptr(), ot, codes.device.index,
                              _stream_on(codes.device, stream)))
     if given is not None:
@@ -1126,6 +1137,8 @@ def nna_decay_attention(q, k, v, decay, scale=None, state=None, lengths=None, wa
         out = q.new_empty((B, T, H, dv))
     elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == (B, T, H, dv) and out.device == device):
         raise TypeError(f"out must be a contiguous {q.dtype} tensor of shape {(B, T, H, dv)}")
+    else:
+        _refuse_overlap(out, q, k, v, decay, state, lengths)
     last = decay.new_empty((B, H, dk, dv)) if want_state else None
     need = nna_decay_attention_workspace(B, T, H, dk, dv)
     ws = (None, 0)
@@ -1175,6 +1188,8 @@ def nna_decay_attention_step(q, k, v, decay, state, scale=None, out=None, stream
         out = q.new_empty((B, H, dv))
     elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.is_contiguous() and tuple(out.shape) == (B, H, dv) and out.device == device):
         raise TypeError(f"out must be a contiguous {q.dtype} tensor of shape {(B, H, dv)}")
+    else:
+        _refuse_overlap(out, q, k, v, decay, state)
     _check(lib().nna_decay_attention_step(*args, t, B, H, dk, dv, dp, dk**-0.5 if scale is None else scale, sp, out.data_ptr(), device.index,
                                           _stream_on(device, stream)))
     _written(state, given)

@@ -17,6 +17,14 @@ nna_status enter_device(DeviceGuard& guard, int device) {
   return e == hipSuccess ? NNA_OK : fail_hip(e, "kernel set-up");
 }
 
+// An output over an input is written while other workgroups still read: refused where the pointers are equal (what overlaps otherwise is the caller's to see to).
+nna_status refuse_same(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+  for (const void* o : outputs)
+    for (const void* i : inputs)
+      if (o && o == i) return fail(NNA_ERR_INVALID_ARG, "an output must not be an input of the call");
+  return NNA_OK;
+}
+
 bool known_type(int t) { return t == NNA_F32 || t == NNA_BF16 || t == NNA_F16; }
 
 // rows (B x T frames) of `width` values
@@ -51,6 +59,8 @@ nna_status run_norm(NormParams& P, int x_type, int y_type, double eps, bool fram
   P.eps = (float)eps;
   DeviceGuard guard;
   nna_status s = enter_device(guard, device);
+  // (every row where it was read, by the lanes that read it: y may be x)
+  if (s == NNA_OK && (frames || x_type != y_type || (P.rows > 1 && P.row_stride != P.width))) s = refuse_same({P.y}, {P.x});
   if (s != NNA_OK || !P.rows) return s;
   const hipError_t e = launch_norm(P, x_type, y_type, frames, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? NNA_OK : fail_hip(e, "layer norm");
@@ -70,6 +80,7 @@ nna_status run_norm_backward(NormParams& P, int x_type, int g_type, bool frames,
   }
   DeviceGuard guard;
   nna_status s = enter_device(guard, device);
+  if (s == NNA_OK && (frames || x_type != g_type)) s = refuse_same({P.gx}, {P.gout});
   if (s != NNA_OK || (!P.rows && !P.partial)) return s;
   const hipError_t e = launch_norm_backward(P, x_type, g_type, frames, gw, gb, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? NNA_OK : fail_hip(e, "layer norm, backward");
@@ -305,6 +316,7 @@ nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, co
   P.H = (int)H;
   DeviceGuard guard;
   s = enter_device(guard, device);
+  if (s == NNA_OK) s = refuse_same({out_dev}, {q_dev, k_dev, v_dev, first_dev});
   if (s != NNA_OK || !B) return s;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const hipError_t e = launch_decay(P, type, stream);
@@ -339,6 +351,7 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
   P.H = (int)H;
   DeviceGuard guard;
   s = enter_device(guard, device);
+  if (s == NNA_OK) s = refuse_same({gq_dev, gk_dev, gv_dev, gfirst_dev}, {gout_dev, q_dev, k_dev, v_dev, first_dev, glast_dev});
   if (s != NNA_OK || !B) return s;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   DecayMix states = P, gq = P, pair = P;
@@ -393,6 +406,7 @@ nna_status nna_decay_attention_step(const void* q_dev, const long long* q_stride
   P.dv = (int)dv;
   DeviceGuard guard;
   s = enter_device(guard, device);
+  if (s == NNA_OK) s = refuse_same({out_dev}, {q_dev, k_dev, v_dev, state_dev});
   if (s != NNA_OK || !B) return s;
   const hipError_t e = launch_decay_step(P, type, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? NNA_OK : fail_hip(e, "linear attention, one frame");

@@ -479,3 +479,31 @@ def test_a_value_that_is_not_finite_in_heads_of_other_sizes(nb, dtype, T, dk, dv
                         assert torch.equal(a[1, at + 1:], b[1, at + 1:]), (name, out)
                 assert not torch.isfinite(torch.cat([t[1].flatten() for t in got.values()])).all()
                 x.copy_(keep)
+
+
+def test_outputs_over_inputs_are_refused(nb):
+    from ctypes import c_longlong
+
+    q, k, v, go, decay, first, glast = _inputs(2, 10, 3, 16, 16, torch.float32)
+    one = [x[:, 0].contiguous() for x in (q, k, v)]
+    for x in (q, k, v):
+        with pytest.raises(ValueError):
+            nb.nna_decay_attention(q, k, v, decay, out=x)
+    for x in one:
+        with pytest.raises(ValueError):
+            nb.nna_decay_attention_step(*one, decay, first, out=x)
+    with pytest.raises(ValueError):
+        nb.nna_decay_attention_step(*one, decay, first, out=first.view(-1)[:96].view(2, 3, 16))
+    both = torch.zeros(21 * 48, device=DEV)
+    with pytest.raises(ValueError):
+        nb.nna_decay_attention(both[:960].view(2, 10, 3, 16), k, v, decay, out=both[48:].view(2, 10, 3, 16))
+    s, s2, st = (c_longlong * 3)(480, 48, 16), (c_longlong * 2)(48, 16), torch.cuda.current_stream().cuda_stream
+    P = [x.data_ptr() for x in (q, k, v)]
+    new = [torch.zeros_like(x).data_ptr() for x in (q, k, v)]
+    qkv, step = (P[0], s, P[1], s, P[2], s, nb.NNA_F32, 2, 10, 3, 16, 16, decay.data_ptr(), 1.0), (P[0], s2, P[1], s2, P[2], s2, nb.NNA_F32, 2, 3, 16, 16, decay.data_ptr(), 1.0)
+    for p in P:
+        assert nb.lib().nna_decay_attention(*qkv, None, None, None, p, None, 0, 0, st) == nb.NNA_ERR_INVALID_ARG
+        assert nb.lib().nna_decay_attention_step(*step, first.data_ptr(), p, 0, st) == nb.NNA_ERR_INVALID_ARG
+    g, f, l = go.data_ptr(), first.data_ptr(), glast.data_ptr()
+    for outs in ((P[0], new[1], new[2], None), (new[0], P[1], new[2], None), (new[0], new[1], g, None), (*new, f), (*new, l)):
+        assert nb.lib().nna_decay_attention_backward(g, *qkv, None, f, l, *outs, None, 0, 0, st) == nb.NNA_ERR_INVALID_ARG

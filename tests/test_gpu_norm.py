@@ -364,3 +364,34 @@ def test_rows_normalised_in_place(nb):
             assert torch.equal(two, torch.cat([x, x]))
             out, kept = nb.nna_layer_norm(two[:37], w, b, keep=32, out=two[37:])  # beside it: nothing is shared
             assert torch.equal(two[37:], y) and torch.equal(kept.x, x)
+
+
+def test_outputs_over_inputs_are_refused(nb):
+    """Where other workgroups still read what one writes: frames in place, other strides or types, part of the input, the weights."""
+    buf = torch.zeros(40 * 64, device=DEV)
+    x, w = buf[:1280].view(20, 64), torch.ones(64, device=DEV)
+    frames = buf[:1280].view(1, 64, 20).transpose(1, 2)
+    wide = buf.view(20, 128)[:, :64]
+    scales = torch.ones(20, 1, device=DEV)
+    for bad in (lambda: nb.nna_layer_norm(frames, out=buf[:1280].view(1, 20, 64)), lambda: nb.nna_layer_norm(wide, out=buf[:1280].view(20, 64)),
+                lambda: nb.nna_layer_norm(x, out=buf[64:1344].view(20, 64)), lambda: nb.nna_layer_norm(x[:1].expand(20, 64), out=x),
+                lambda: nb.nna_layer_norm(x, out_dtype=torch.bfloat16, out=buf.view(torch.bfloat16)[:1280].view(20, 64)),
+                lambda: nb.nna_layer_norm(torch.ones(1, 64, device=DEV), w, out=w[None]), lambda: nb.nna_layer_norm(torch.ones(1, 64, device=DEV), None, w, out=w[None]),
+                lambda: nb.nna_unpack8(buf.view(torch.int8)[-1280:].view(20, 64), scales, out=buf[-1280:].view(20, 64))):
+        with pytest.raises(ValueError):
+            bad()
+    p, st = buf.data_ptr(), torch.cuda.current_stream().cuda_stream
+    stats, ws = torch.zeros(64, device=DEV), torch.zeros(1 << 16, dtype=torch.uint8, device=DEV)
+    norm, back = nb.lib().nna_layer_norm, nb.lib().nna_layer_norm_backward
+    for status in (nb.lib().nna_layer_norm_frames(p, 1, 64, 20, None, None, 1e-5, p, nb.NNA_F32, None, 0, st),
+                   norm(p, nb.NNA_F32, 20, 64, 128, None, None, 1e-5, p, nb.NNA_F32, None, None, None, 0, st),
+                   norm(p, nb.NNA_F32, 20, 64, 64, None, None, 1e-5, p, nb.NNA_BF16, None, None, None, 0, st),
+                   nb.lib().nna_layer_norm_frames_backward(p, nb.NNA_F32, p + 5120, 1, 64, 20, stats.data_ptr(), None, p, None, None, None, 0, 0, st),
+                   back(p, nb.NNA_BF16, p + 5120, nb.NNA_F32, 20, 64, 64, None, None, stats.data_ptr(), None, p, None, None, None, 0, 0, st)):
+        assert status == nb.NNA_ERR_INVALID_ARG
+    # over gout where nothing else is read of it: allowed, and right
+    x, w, b, g = _inputs((300, 640), torch.float32)
+    kept = nb.nna_layer_norm(x, w, b, keep=32)[1]
+    gx = nb.nna_layer_norm_backward(g, kept, w, want_gw=False)[0]
+    assert back(g.data_ptr(), nb.NNA_F32, x.data_ptr(), nb.NNA_F32, 300, 640, 640, None, None, kept.stats.data_ptr(), w.data_ptr(), g.data_ptr(), None, None, None, 0, 0, st) == nb.NNA_OK
+    assert torch.equal(g, gx)
