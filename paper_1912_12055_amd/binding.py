@@ -844,6 +844,25 @@ def _stream_on(device, stream):
     return _current_stream(device.index)
 
 
+def _under(stream, device, call):
+    """call() with `stream` as torch's current one, or None where it is that already or none that torch has an allocator for: what the call allocates is then memory of
+    the stream it is written on, and what it returns is not handed out again before the stream that it is returned to has done with it, too."""
+    import torch
+
+    if not isinstance(stream, int) or stream in (1, 2):  # (HIP's names for the default stream and for every thread's own; a ctypes pointer)
+        return None
+    current = torch.cuda.current_stream(device)
+    if stream == current.cuda_stream:
+        return None
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)):
+        result = call()
+    for t in result if isinstance(result, tuple) else (result,):
+        for t in (t.stats, t.codes, t.scales) if isinstance(t, NormKept) else (t,):
+            if t is not None:
+                t.record_stream(current)
+    return result
+
+
 def _type_of(t, name, allowed=("float32", "bfloat16", "float16")):
     """The nna_dtype of a CUDA tensor, which is refused if it is none or of a type not `allowed`."""
     import torch
@@ -957,6 +976,8 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
     import torch
 
     xt = _type_of(x, "x")
+    if stream is not None and (done := _under(stream, x.device, lambda: nna_layer_norm(x, weight, bias, eps, out_dtype, keep, out))) is not None:
+        return done
     if x.dim() < 1:
         raise TypeError("x must have an axis to normalise")
     if keep not in (0, 8, 32):
@@ -1006,6 +1027,8 @@ def nna_layer_norm_backward(gout, kept, weight=None, want_gx=True, want_gw=True,
     import torch
 
     gt = _type_of(gout, "gout")
+    if stream is not None and (done := _under(stream, gout.device, lambda: nna_layer_norm_backward(gout, kept, weight, want_gx, want_gw, workspace))) is not None:
+        return done
     if gout.dtype != kept.out_dtype or gout.shape != kept.shape or not gout.is_contiguous() or gout.device != kept.stats.device:
         raise TypeError(f"gout must be a contiguous {kept.out_dtype} CUDA tensor of shape {tuple(kept.shape)}")
     shape, width, device, rows = kept.shape, kept.shape[-1], gout.device, kept.rows
@@ -1046,6 +1069,8 @@ def nna_pack8(x, stream=None):
     import torch
 
     xt = _type_of(x, "x")
+    if stream is not None and (done := _under(stream, x.device, lambda: nna_pack8(x))) is not None:
+        return done
     step = _row_stride(x) if x.dim() else None
     if step is None:
         raise TypeError("x must be rows at one distance from each other")
@@ -1063,6 +1088,8 @@ def nna_unpack8(codes, scales, dtype=None, out=None, stream=None):
 
     if not (isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dtype == torch.int8 and codes.is_contiguous() and codes.dim()):
         raise TypeError("codes must be a contiguous int8 CUDA tensor")
+    if stream is not None and (done := _under(stream, codes.device, lambda: nna_unpack8(codes, scales, dtype, out))) is not None:
+        return done
     width = codes.shape[-1]
     sp, given = _vector(scales, "scales", (*codes.shape[:-1], -(-width // NNA_BLOCK8)), codes.device), out
     if out is None:
@@ -1131,6 +1158,8 @@ def nna_decay_attention(q, k, v, decay, scale=None, state=None, lengths=None, wa
 
     t, (B, T, H, dk, dv), args = _heads(q, k, v, 4)
     device = q.device
+    if stream is not None and (done := _under(stream, device, lambda: nna_decay_attention(q, k, v, decay, scale, state, lengths, want_state, out, workspace))) is not None:
+        return done
     dp, sp, lp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device, none=True), _lengths(lengths, B, device)
     given = out
     if out is None:
@@ -1159,6 +1188,9 @@ def nna_decay_attention_backward(gout, q, k, v, decay, scale=None, state=None, l
 
     t, (B, T, H, dk, dv), args = _heads(q, k, v, 4)
     device = q.device
+    if stream is not None and (done := _under(stream, device, lambda: nna_decay_attention_backward(gout, q, k, v, decay, scale, state, lengths, gstate, want_gstate,
+                                                                                                   workspace))) is not None:
+        return done
     dp, sp, lp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device, none=True), _lengths(lengths, B, device)
     lastp = _vector(gstate, "gstate", (B, H, dk, dv), device, none=True)
     if not (isinstance(gout, torch.Tensor) and gout.dtype == q.dtype and gout.is_contiguous() and tuple(gout.shape) == (B, T, H, dv) and gout.device == device):
@@ -1182,6 +1214,8 @@ def nna_decay_attention_step(q, k, v, decay, state, scale=None, out=None, stream
 
     t, (B, H, dk, dv), args = _heads(q, k, v, 3)
     device = q.device
+    if stream is not None and (done := _under(stream, device, lambda: nna_decay_attention_step(q, k, v, decay, state, scale, out))) is not None:
+        return done
     dp, sp = _vector(decay, "decay", (H,), device), _vector(state, "state", (B, H, dk, dv), device)
     given = out
     if out is None:

@@ -216,3 +216,52 @@ def test_what_the_calls_write_in_place_is_noticed(layers):
     kept = torch.zeros(nb.nna_kept_bytes(layer.plan, 2, 4000), dtype=torch.uint8, device=DEV)
     nb.nna_forward_keep(layer.plan, wave, kept=kept)
     assert kept._version == 1
+
+
+def test_results_are_memory_of_the_stream_they_are_written_on(layers):
+    """With a stream's handle: what a call allocates is that stream's (memory that torch's current stream has freed and may still read is not written), and is
+    not handed out again while the current stream, which gets it, is still at work."""
+    from paper_1912_12055_amd import binding as nb
+    g = _gen(9)
+    x, w = torch.randn(4096, 512, device=DEV, generator=g), torch.ones(512, device=DEV)
+    spec = torch.randn(2, 64, 300, device=DEV, generator=g)
+    q = torch.randn(2, 3000, 4, 64, device=DEV, generator=g)
+    decay, first = torch.full((4,), 0.9, device=DEV), torch.randn(2, 4, 64, 64, device=DEV, generator=g)
+    side = torch.cuda.Stream()
+
+    def calls(stream, state):
+        y, kept = nb.nna_layer_norm(x, w, keep=8, stream=stream)
+        f, kf = nb.nna_layer_norm(spec.transpose(1, 2), keep=32, stream=stream)
+        out = [y, kept.stats, kept.codes, kept.scales, f, kf.stats, *nb.nna_layer_norm_backward(x, kept, w, stream=stream), *nb.nna_layer_norm_backward(f, kf, stream=stream)]
+        codes, scales = nb.nna_pack8(x, stream=stream)
+        out += [codes, scales, nb.nna_unpack8(codes, scales, stream=stream)]
+        out += nb.nna_decay_attention(q, q, q, decay, state=first, want_state=True, stream=stream)
+        out += nb.nna_decay_attention_backward(q, q, q, q, decay, state=first, gstate=first, want_gstate=True, stream=stream)
+        return out + [nb.nna_decay_attention_step(q[:, 0], q[:, 0], q[:, 0], decay, state, stream=stream)]
+
+    states = first.clone(), first.clone()
+    ref = [t.clone() for t in calls(None, states[0])]
+    torch.cuda.synchronize()
+    out = calls(side.cuda_stream, states[1])
+    torch.cuda.synchronize()
+    segments = torch.cuda.memory_snapshot()
+    for k, (a, b) in enumerate(zip(out, ref)):
+        assert torch.equal(a, b), k
+        owner = [s["stream"] for s in segments if s["address"] <= a.data_ptr() < s["address"] + s["total_size"]]
+        assert owner == [side.cuda_stream], k
+    assert torch.equal(*states)
+    y = nb.nna_layer_norm(x, w, stream=side.cuda_stream)
+    at, size = y.data_ptr(), y.numel()
+    torch.cuda.current_stream().wait_stream(side)
+    a = torch.randn(8192, 8192, device=DEV, generator=g)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        a = a @ a  # the current stream is busy, and has y to read after it
+    z = y.sum()
+    del y
+    with torch.cuda.stream(side):
+        again = torch.empty(size, device=DEV)
+    busy = not torch.cuda.current_stream().query()
+    assert not busy or again.data_ptr() != at
+    torch.cuda.synchronize()
+    assert torch.isfinite(z)
