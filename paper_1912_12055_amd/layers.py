@@ -17,6 +17,8 @@ codes stand for, off by up to 1/254 of the largest of 128 neighbouring products.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import binding as nb
@@ -96,6 +98,40 @@ def _saved(ctx):
     return x, kept[0] if len(kept) == 1 else nb.nna_unpack8(*kept)
 
 
+class _OneDerivative(torch.autograd.Function):
+    """A gradient as it is, whose own derivative the library does not have."""
+
+    @staticmethod
+    def forward(ctx, g):
+        return g.view_as(g)
+
+    @staticmethod
+    def backward(ctx, gg):
+        raise RuntimeError("the library's calls have no second derivative: their gradients can't be differentiated (create_graph=True)")
+
+
+def _one_derivative(depends):
+    """A backward method whose gradients raise an error where they are differentiated, in place of being constants without a word.  `depends(ctx)`: for each
+    input with a gradient, the inputs that gradient depends on, besides what comes from the loss; one that depends on nothing asked for is a constant."""
+    def decorate(backward):
+        @functools.wraps(backward)
+        def run(ctx, *gouts):
+            with torch.no_grad():
+                grads = backward(ctx, *gouts)
+            if not torch.is_grad_enabled():
+                return grads
+            of_loss, on = any(g is not None and g.requires_grad for g in gouts), depends(ctx)
+            return tuple(g if g is None or not (of_loss or any(ctx.needs_input_grad[j] for j in on[i])) else _OneDerivative.apply(g.detach().requires_grad_())
+                         for i, g in enumerate(grads))
+        return run
+    return decorate
+
+
+def _kernel_gradients(ctx):
+    """of waveform and kernels: products with the other one where the outputs are the products themselves"""
+    return ((1,), (0,)) if ctx.layer.linear else ((0, 1), (0, 1))
+
+
 class _StftFn(torch.autograd.Function):
     """nna_stft with nna_stft_backward as its derivative (kernels W and waveform x)."""
 
@@ -105,6 +141,7 @@ class _StftFn(torch.autograd.Function):
         return _forward(ctx, layer.plan, x, keep, nb.nna_stft)
 
     @staticmethod
+    @_one_derivative(_kernel_gradients)
     def backward(ctx, gout):
         x, kept = _saved(ctx)
         need_x, need_w = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
@@ -138,6 +175,7 @@ class _MelFn(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_one_derivative(lambda ctx: ((0, 1, 2), (0, 1, 2), (0, 1)))
     def backward(ctx, gout):
         x, kept = _saved(ctx)
         need_x, need_w, need_m = ctx.needs_input_grad[:3]
@@ -153,6 +191,7 @@ class _Trainable(torch.nn.Module):
     """Keeps the library's copy of a parameter in step with the ``nn.Parameter`` an optimiser updates."""
 
     kept_bits = 32
+    linear = False  # the outputs are the kernels' products with the waveform themselves
 
     def _make_trainable(self, kept_bits=32):
         if kept_bits not in (8, 32):
@@ -201,6 +240,7 @@ class STFT(_Trainable):
         self.trainable = bool(trainable)
         if self.trainable:
             self._make_trainable(kept_bits)
+            self.linear = fmt == nb.NNA_OUT_COMPLEX
             self.wsin_wcos = torch.nn.Parameter(nb.nna_plan_get_bank(self.plan))
 
     def forward(self, x):
@@ -264,6 +304,7 @@ class _CqtFn(torch.autograd.Function):
         return _forward(ctx, layer.plan, x, keep, nb.nna_cqt)
 
     @staticmethod
+    @_one_derivative(_kernel_gradients)
     def backward(ctx, gout):
         x, kept = _saved(ctx)
         need_x, need_w = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
@@ -300,6 +341,7 @@ class CQT1992v2(_Cqt):
         self.trainable = bool(trainable)
         if self.trainable:
             self._make_trainable(kept_bits)
+            self.linear = _format(output_format) == nb.NNA_OUT_COMPLEX
             self.cqt_kernels = torch.nn.Parameter(nb.nna_plan_get_bank(self.plan))
 
     def forward(self, x):
@@ -383,6 +425,7 @@ class _NormFn(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_one_derivative(lambda ctx: ((0, 1), (0,), ()))
     def backward(ctx, gout):
         weight, *tensors = ctx.saved_tensors
         kept = ctx.kept.with_tensors(tensors, ctx.bits)
@@ -429,6 +472,7 @@ class _DecayFn(torch.autograd.Function):
         return nb.nna_decay_attention(q, k, v, decay, scale=scale, state=state, lengths=lengths, want_state=want_state)
 
     @staticmethod
+    @_one_derivative(lambda ctx: ((1, 2, 3), (0, 2), (0, 1), (0,)))
     def backward(ctx, gout, gstate=None):
         q, k, v, state, decay, lengths = ctx.saved_tensors
         gout = torch.zeros((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device) if gout is None else gout.contiguous()

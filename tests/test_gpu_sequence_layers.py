@@ -265,3 +265,55 @@ def test_results_are_memory_of_the_stream_they_are_written_on(layers):
     assert not busy or again.data_ptr() != at
     torch.cuda.synchronize()
     assert torch.isfinite(z)
+
+
+def _penalty(call, x, weight):
+    """the gradient of a call behind a product with `weight`, differentiated"""
+    y = call(x * weight)
+    gx, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
+    return gx
+
+
+@pytest.mark.parametrize("kind", ["norm", "norm without weights", "attention", "state", "stft", "mel", "cqt", "complex"])
+def test_a_second_derivative_is_refused(layers, kind):
+    """Not left out: the gradients themselves are right under create_graph, and differentiating them raises."""
+    g = _gen(10)
+    mix = layers.DecayAttention(2)
+    zeros = torch.zeros(2, 2, 16, 16, device=DEV)
+    call, shape = {
+        "norm": (layers.LayerNorm(16), (4, 16)), "norm without weights": (layers.LayerNorm(16, affine=False), (4, 16)),
+        "attention": (lambda h: mix(h, h, h), (2, 6, 2, 16)), "state": (lambda h: mix(h.detach(), h.detach(), h.detach(), state=zeros + h.sum()), (2, 6, 2, 16)),
+        "stft": (layers.STFT(n_fft=512, hop_length=128, trainable=True, output_format="Power"), (1, 2000)),
+        "mel": (layers.MelSpectrogram(sr=16000, n_fft=512, hop_length=128, n_mels=40, trainable_STFT=True), (1, 2000)),
+        "cqt": (layers.CQT1992v2(sr=16000, hop_length=128, fmin=440.0, n_bins=12, trainable=True), (1, 4000)),
+        "complex": (layers.STFT(n_fft=512, hop_length=128, trainable=True, output_format="Complex"), (1, 2000))}[kind]
+    _say("second derivative", kind)
+    x = torch.randn(shape, device=DEV, generator=g).requires_grad_()
+    weight = torch.ones((), device=DEV).requires_grad_()
+    gx = _penalty(call, x, weight)
+    y = call(x * weight)
+    first, = torch.autograd.grad(y.square().sum(), x)
+    assert (gx.detach() - first).norm() <= 1e-5 * first.norm()  # (the transforms' sums in another order: some units of 2^-24)
+    with pytest.raises(RuntimeError, match="no second derivative"):
+        gx.square().sum().backward()
+
+
+def test_gradients_that_are_constants_stay_constants(layers):
+    """A gradient that depends on nothing with a gradient of its own has no second derivative to leave out."""
+    g = _gen(11)
+    q, k, v = (torch.randn(2, 6, 2, 16, device=DEV, generator=g) for _ in range(3))
+    first, w = torch.randn(2, 2, 16, 16, device=DEV, generator=g), torch.full((), 3.0, device=DEV).requires_grad_()
+    mix, norm = layers.DecayAttention(2), layers.LayerNorm(16)
+    stft = layers.STFT(n_fft=512, hop_length=128, trainable=True, output_format="Complex")
+    stft.wsin_wcos.requires_grad_(False)
+    wave = torch.randn(1, 2000, device=DEV, generator=g)
+    for call, x in ((lambda t: mix(q, k, t, state=first), v), (lambda t: mix(t, k, v), q), (lambda t: mix(q, t, v), k), (stft, wave)):
+        x = x.clone().requires_grad_()
+        gx, = torch.autograd.grad(call(x * w).sum(), x, create_graph=True)  # w times a constant
+        plain = x.detach().requires_grad_()
+        c, = torch.autograd.grad(call(plain).sum(), plain)
+        gw, = torch.autograd.grad(gx.sum(), w)
+        assert torch.allclose(gw, c.sum(), rtol=1e-5, atol=1e-5 * float(c.abs().sum()))
+    y = norm(q)
+    grads = torch.autograd.grad(y.sum(), (norm.weight, norm.bias), create_graph=True)
+    assert not any(t.requires_grad for t in grads)
