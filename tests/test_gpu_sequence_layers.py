@@ -317,3 +317,23 @@ def test_gradients_that_are_constants_stay_constants(layers):
     y = norm(q)
     grads = torch.autograd.grad(y.sum(), (norm.weight, norm.bias), create_graph=True)
     assert not any(t.requires_grad for t in grads)
+
+
+def test_forward_mode_is_refused(layers):
+    """a dual tensor's tangent is not dropped"""
+    from torch.autograd import forward_ad
+    g = _gen(12)
+    q = torch.randn(2, 6, 2, 16, device=DEV, generator=g)
+    state = torch.zeros(2, 2, 16, 16, device=DEV)
+    mix, norm, bare = layers.DecayAttention(2), layers.LayerNorm(16), layers.LayerNorm(16, affine=False)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(q, torch.ones_like(q))
+        dual_state = forward_ad.make_dual(state, torch.ones_like(state))
+        for call in (lambda: bare(dual), lambda: norm(dual), lambda: mix(dual, q, q), lambda: mix(q, q, dual), lambda: mix(q, q, q, state=dual_state),
+                     lambda: mix.step(dual[:, 0], q[:, 0], q[:, 0], state), lambda: mix.step(q[:, 0], q[:, 0], q[:, 0], dual_state)):
+            for grad in (True, False):
+                with torch.set_grad_enabled(grad), pytest.raises((NotImplementedError, RuntimeError)):
+                    call()
+        assert not state.any()
+        with torch.no_grad():  # others are as ever
+            assert mix(q, q, q).shape == norm(q).shape == q.shape
