@@ -827,6 +827,7 @@ def nna_backward_kept(plan: Plan, x, gout, kept, want_gmelw=False, want_gw=True,
 # ---- operators of networks on the transforms' frames ------------------------------------------------------------------
 NNA_F32, NNA_BF16, NNA_F16 = 0, 1, 2
 NNA_BLOCK8 = 128
+NNA_FRAMES_WIDTH = 2112  # bins of the frames that nna_layer_norm reads as the transforms write them
 _types = {}
 _current_stream = None
 

@@ -447,7 +447,7 @@ class LayerNorm(torch.nn.Module):
     """Layer norm over the last axis, of `width` values; ``weight`` and ``bias`` are float32 parameters.
 
     Input: rows ``x[..., width]`` of float32, bfloat16 or float16, or frames as the transforms write them, ``spec.transpose(1, 2)`` of
-    ``spec[B, bins, T]``, read as they lie and returned as tokens ``[B, T, bins]``.  ``out_dtype``: the tokens' type (float32 input; its own if None).
+    ``spec[B, bins, T]``, read as they lie (up to 2,112 bins; more are copied to rows) and returned as tokens ``[B, T, bins]``.  At most 16,384 values.  ``out_dtype``: the tokens' type (float32 input; its own if None).
     ``kept_bits=8`` keeps the input for the backward pass in 8 bits (rows)."""
 
     def __init__(self, width, eps=1e-5, affine=True, bias=True, out_dtype=None, kept_bits=32, device="cuda:0"):
@@ -462,7 +462,7 @@ class LayerNorm(torch.nn.Module):
     def forward(self, x):
         if x.shape[-1] != self.width:
             raise ValueError(f"x must have {self.width} values along its last axis")
-        frames = x.dim() == 3 and x.dtype == torch.float32 and x.transpose(1, 2).is_contiguous()
+        frames = x.dim() == 3 and x.dtype == torch.float32 and x.transpose(1, 2).is_contiguous() and self.width <= nb.NNA_FRAMES_WIDTH
         if nb._row_stride(x) is None and (not frames or self.kept_bits == 8):
             x = x.contiguous()
         if _differentiates(x, self.weight, self.bias):

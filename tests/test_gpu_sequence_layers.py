@@ -337,3 +337,27 @@ def test_forward_mode_is_refused(layers):
         assert not state.any()
         with torch.no_grad():  # others are as ever
             assert mix(q, q, q).shape == norm(q).shape == q.shape
+
+
+@pytest.mark.parametrize("bins", [2112, 2113, 4097])
+def test_layer_norm_layer_on_wide_frames(layers, bins):
+    """More bins than are read as frames (an STFT of 8,192 samples has 4,097): rows are made of them; values and gradients as of rows, and against 64 bits."""
+    _say("wide frames", bins)
+    g = _gen(13)
+    layer = layers.LayerNorm(bins)
+    with torch.no_grad():
+        layer.weight.add_(0.3 * torch.randn(bins, device=DEV, generator=g))
+    spec = torch.randn(2, bins, 21, device=DEV, generator=g).requires_grad_()
+    y = layer(spec.transpose(1, 2))
+    gout = torch.randn(y.shape, device=DEV, generator=g)
+    y.backward(gout)
+    x, w = spec.detach().double().transpose(1, 2).requires_grad_(), layer.weight.detach().double().requires_grad_()
+    d = x - x.mean(-1, keepdim=True)
+    ref = d / (d.square().mean(-1, keepdim=True) + layer.eps).sqrt() * w
+    ref.backward(gout.double())
+    for got, want in ((y, ref.detach()), (spec.grad, x.grad.transpose(1, 2)), (layer.weight.grad, w.grad)):
+        _near(got, want, 1e-5)
+    with torch.no_grad():
+        assert torch.equal(layer(spec.transpose(1, 2)), y)
+        if bins > 2112:
+            assert torch.equal(layer(spec.transpose(1, 2).contiguous()), y)
