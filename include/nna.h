@@ -390,7 +390,8 @@ nna_status nna_cqt_backward(const nna_plan* plan, const float* x_dev, long long 
  * A training step whose backward pass need not compute C = W x again: the forward pass writes it to kept_dev beside its output.
  * For plans from nna_plan_stft (power format), nna_plan_mel (power 2) and nna_plan_cqt (every format but NNA_OUT_COMPLEX) made
  * trainable; results are those of nna_stft / nna_mel_with_stft / nna_cqt and their backward calls.
- *   nna_kept_bytes     size of kept_dev (bank rows padded to 128 x padded frames x 4); 0: this plan's calls keep nothing.
+ *   nna_kept_bytes     size of kept_dev: float32 [frames / 32][rows][32], the B T frames of all waveforms in one count and the bank's rows each padded to 128;
+ *                      0: this plan's calls keep nothing.
  *   nna_forward_keep   as nna_stft, nna_cqt or (spec_dev not NULL, Mel plans only) nna_mel_with_stft, and kept_dev (256-byte aligned).
  *   nna_backward_kept  as the plan's backward call with the same workspace; kept_dev from the forward pass of the same x_dev and
  *                      bank (a bank set since makes the kernels' and the waveform's gradient a mixture of both), unchanged by the call.  gmelw_dev: Mel plans only.

@@ -10,8 +10,9 @@ Input ``x``: float32 CUDA tensor ``[B, L]`` (or ``[L]``); output ``[B, bins, T]`
 Memory: a call of a trainable ``MelSpectrogram`` (power 2), ``STFT`` (``output_format='Power'``) or ``CQT1992v2`` (every format but
 ``'Complex'``) that autograd records holds, until its backward pass, the kernels' products with the waveform besides ``x``: bank rows
 rounded up to 128 times frames times 4 bytes, at most 1 GiB a call.  Larger batches hold ``x`` alone and compute the products again.
-``kept_bits=8`` on these layers holds the products in 8 bits (``nna_pack8``), about a quarter of that; gradients are then those of the values the
-codes stand for, off by up to 1/254 of the largest of 128 neighbouring products.
+``kept_bits=8`` on these layers holds the products in 8 bits (``nna_pack8``), about a quarter of that (clips of at least 16 frames); gradients are then those
+of the values the codes stand for, off by up to 1/254 of the largest of 128 neighbouring frames of a clip and kernel.  A product that is not finite makes those of
+its 128 NaN, of no other clip or kernel.
 
 ``LayerNorm`` and ``DecayAttention`` are what a network on the transforms' frames is built of.
 """
@@ -73,15 +74,42 @@ def _no_grad_input(x):
 _KEPT_BYTES = 1 << 30  # what a forward pass holds for its backward pass, at most; a larger batch's computes it again
 
 
+_FRAMES8 = 16  # of a clip: fewer are kept in 32 bits, their blocks' scales would be the larger part of 8
+
+
+def _padded_rows(kept, frames):
+    """Rows of what nna_forward_keep writes: [frame / 32][rows][frame % 32], all clips' frames in one count, padded to a multiple of 128."""
+    return kept.numel() // (-(-frames // 128) * 128)
+
+
+def _copy_products(products, kept, back):
+    """products[kernel row, frame] (a clip's frames next to each other) from what nna_forward_keep wrote, or (`back`) to where nna_backward_kept reads them."""
+    rows, frames = products.shape
+    blocks, whole = kept.view(-1, _padded_rows(kept, frames), 32), frames // 32
+    parts = [(products[:, :whole * 32].unflatten(1, (whole, 32)), blocks[:whole, :rows].transpose(0, 1))] if whole else []
+    if frames % 32:
+        parts.append((products[:, whole * 32:], blocks[whole, :rows, :frames % 32]))
+    for a, b in parts:
+        if back:
+            b.copy_(a)
+        else:
+            a.copy_(b)
+
+
 def _forward(ctx, plan, x, keep, run):
     """run(plan, x), or what is worth keeping for the backward pass with it (`keep`: there will be one)."""
     if keep and x.is_cuda and x.dim() == 2 and x.shape[1] >= 4:
         size = nb.nna_kept_bytes(plan, *x.shape)
         if 0 < size <= _KEPT_BYTES:
-            if ctx.layer.kept_bits == 8:  # (places between the products share their blocks: zeros, which change no scale)
+            frames = nb.nna_out_shape(plan, *x.shape)[1]
+            if ctx.layer.kept_bits == 8 and frames >= _FRAMES8:
                 kept = torch.zeros(size // 4, dtype=torch.float32, device=x.device)
                 out, _ = nb.nna_forward_keep(plan, x, size=size, kept=kept)
-                ctx.save_for_backward(x, *nb.nna_pack8(kept))
+                products = kept.new_empty((min(plan.constants()[1], _padded_rows(kept, x.shape[0] * frames)), x.shape[0] * frames))
+                _copy_products(products, kept, False)
+                del kept
+                ctx.save_for_backward(x, *nb.nna_pack8(products.view(-1, frames)))
+                ctx.kept_size = size // 4
             else:
                 out, kept = nb.nna_forward_keep(plan, x, size=size)
                 ctx.save_for_backward(x, kept)
@@ -96,7 +124,12 @@ def _saved(ctx):
     x, *kept = ctx.saved_tensors
     if not kept or ctx.bank_sets != ctx.layer.plan.bank_sets:
         return x, None
-    return x, kept[0] if len(kept) == 1 else nb.nna_unpack8(*kept)
+    if len(kept) == 1:
+        return x, kept[0]
+    frames = x.shape[0] * kept[0].shape[1]
+    full = kept[1].new_empty(ctx.kept_size)  # (what stands for no frame or no kernel is not read)
+    _copy_products(nb.nna_unpack8(*kept).view(-1, frames), full, True)
+    return x, full
 
 
 class _OneDerivative(torch.autograd.Function):

@@ -361,3 +361,61 @@ def test_layer_norm_layer_on_wide_frames(layers, bins):
         assert torch.equal(layer(spec.transpose(1, 2)), y)
         if bins > 2112:
             assert torch.equal(layer(spec.transpose(1, 2).contiguous()), y)
+
+
+LAYERS8 = {"stft": lambda L, b: L.STFT(n_fft=512, hop_length=128, trainable=True, output_format="Power", kept_bits=b),
+           "mel": lambda L, b: L.MelSpectrogram(sr=16000, n_fft=512, hop_length=128, n_mels=40, trainable_mel=True, trainable_STFT=True, kept_bits=b),
+           "cqt": lambda L, b: L.CQT1992v2(sr=16000, hop_length=128, fmin=220.0, n_bins=24, trainable=True, output_format="Power", kept_bits=b)}
+
+
+@pytest.mark.parametrize("kind", sorted(LAYERS8))
+@pytest.mark.parametrize("length", [9001, 6000, 16384])
+def test_products_in_8_bits_of_a_clip_know_no_other_clip(layers, kind, length):
+    """A clip between two others that is NaN in one sample, or a million times as loud: the others' gradients are those of 8 bits by themselves, off by at most
+    sqrt(128) / 254 < 0.045 of a block's norm (whatever its neighbour)."""
+    _say("clips in 8 bits", kind, length)
+    g = _gen(14)
+    clean = 0.3 * torch.randn(3, length, device=DEV, generator=g)
+    gout = None
+    grads = {}
+    for bits in (32, 8):
+        layer = LAYERS8[kind](layers, bits)
+        for what in ("clean", "nan", "loud"):
+            x = clean.clone()
+            if what == "nan":
+                x[1, length // 2] = float("nan")
+            elif what == "loud":
+                x[1] *= 1e3  # its powers a million times
+            x.requires_grad_()
+            y = layer(x)
+            gout = torch.randn(y.shape, device=DEV, generator=_gen(15)) if gout is None else gout
+            y.backward(gout)
+            grads[bits, what] = x.grad
+    for what in ("nan", "loud"):
+        for b in (0, 2):
+            full, small, alone = grads[32, "clean"][b], grads[8, what][b], grads[8, "clean"][b]
+            assert torch.isfinite(small).all(), what
+            assert (small - full).norm() <= 0.045 * full.norm(), what
+            assert (small - alone).norm() <= 1e-5 * alone.norm(), what
+    assert not torch.isfinite(grads[8, "nan"][1]).all()
+
+
+@pytest.mark.parametrize("kind", sorted(LAYERS8))
+@pytest.mark.parametrize("batch,frames", [(1, 15), (40, 15), (1, 16), (5, 16), (2, 32), (3, 33), (1, 64), (4, 128), (2, 129)])
+def test_products_in_8_bits_of_any_number_of_frames(layers, kind, batch, frames):
+    _say("frames in 8 bits", kind, batch, frames)
+    if kind == "cqt":  # one second at least: its longest kernel
+        frames += 25
+    x = (0.3 * torch.randn(batch, 128 * (frames - 1), device=DEV, generator=_gen(16))).requires_grad_()
+    grads = []
+    for bits in (32, 8):
+        layer = LAYERS8[kind](layers, bits)
+        x.grad = None
+        y = layer(x)
+        assert y.shape[-1] == frames
+        held = [t for t in y.grad_fn.saved_tensors if t is not x]
+        assert len(held) == (2 if bits == 8 and frames >= 16 else 1)
+        y.backward(torch.randn(y.shape, device=DEV, generator=_gen(17)))
+        grads.append([x.grad.clone()] + [p.grad.clone() for p in layer.parameters()])
+    for a, b in zip(*grads):
+        assert torch.isfinite(b).all() and (a - b).norm() <= 0.045 * a.norm()
