@@ -1,8 +1,6 @@
 // Running a plan: shape checks, launch parameters and the transform calls of the C ABI, the per-device
 // set-up, and the library's static workspace with the entry point that uses it.
-#include "nna_decay.h"
 #include "nna_host.h"
-#include "nna_norm.h"
 
 // Workspace of nna_cqt2010v2_static: the downsampled waveforms of two consecutive octaves live here instead
 // of in caller memory.  Every device the library's code is loaded on holds its own copy of the array, at its
@@ -30,8 +28,6 @@ hipError_t ensure_kernels_init(int device) {
     if (e == hipSuccess) e = nna::cql_kernels_init();
     if (e == hipSuccess) e = nna::short_kernels_init();
     if (e == hipSuccess) e = nna::fft_kernels_init();
-    if (e == hipSuccess) e = nna::norm_kernels_init();
-    if (e == hipSuccess) e = nna::decay_kernels_init();
     if (e != hipSuccess) return e;
     void* ptr = nullptr;
     e = hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch));

@@ -8,13 +8,28 @@ using namespace nna::host;
 
 namespace {
 
-// enters the device for a call without a plan, its kernels set up
-nna_status enter_device(DeviceGuard& guard, int device) {
+// Kernels' set-up, once per device and at the first call that needs it: the transforms' users do not wait for it, nor those of one operator for the other's.
+struct Setup {
+  hipError_t (*const init)();
+  std::mutex mutex;
+  std::vector<char> done;
+};
+Setup norm_setup{nna::norm_kernels_init}, decay_setup{nna::decay_kernels_init};
+
+// enters the device for a call without a plan, its kernels set up (pack and unpack: there is nothing to)
+nna_status enter_device(DeviceGuard& guard, int device, Setup* setup) {
   if (device < 0) return fail(NNA_ERR_INVALID_ARG, "device must be the HIP device of the arrays");
   hipError_t e = guard.enter(device);  // (refuses a device that there is not)
   if (e != hipSuccess) return fail_hip(e, "hipSetDevice");
-  e = ensure_kernels_init(device);
-  return e == hipSuccess ? NNA_OK : fail_hip(e, "kernel set-up");
+  if (!setup) return NNA_OK;
+  std::lock_guard<std::mutex> lock(setup->mutex);
+  if ((int)setup->done.size() <= device) setup->done.resize(device + 1, 0);
+  if (!setup->done[device]) {
+    e = setup->init();
+    if (e != hipSuccess) return fail_hip(e, "kernel set-up");
+    setup->done[device] = 1;
+  }
+  return NNA_OK;
 }
 
 // An output over an input is written while other workgroups still read: refused where the pointers are equal (what overlaps otherwise is the caller's to see to).
@@ -58,7 +73,7 @@ nna_status run_norm(NormParams& P, int x_type, int y_type, double eps, bool fram
   if (P.codes && x_type != y_type) return fail(NNA_ERR_UNSUPPORTED, "8-bit codes need outputs of the inputs' type");
   P.eps = (float)eps;
   DeviceGuard guard;
-  nna_status s = enter_device(guard, device);
+  nna_status s = enter_device(guard, device, &norm_setup);
   // (every row where it was read, by the lanes that read it: y may be x)
   if (s == NNA_OK && (frames || x_type != y_type || (P.rows > 1 && P.row_stride != P.width))) s = refuse_same({P.y}, {P.x});
   if (s != NNA_OK || !P.rows) return s;
@@ -79,7 +94,7 @@ nna_status run_norm_backward(NormParams& P, int x_type, int g_type, bool frames,
     P.partial = static_cast<float*>(workspace);
   }
   DeviceGuard guard;
-  nna_status s = enter_device(guard, device);
+  nna_status s = enter_device(guard, device, &norm_setup);
   if (s == NNA_OK && (frames || x_type != g_type)) s = refuse_same({P.gx}, {P.gout});
   if (s != NNA_OK || (!P.rows && !P.partial)) return s;
   const hipError_t e = launch_norm_backward(P, x_type, g_type, frames, gw, gb, static_cast<hipStream_t>(stream));
@@ -259,7 +274,7 @@ nna_status nna_pack8(const void* x_dev, nna_dtype type, long long rows, long lon
   if (s != NNA_OK) return s;
   if (rows && (!x_dev || !codes_dev || !scales_dev)) return fail(NNA_ERR_INVALID_ARG, "x_dev / codes_dev / scales_dev is NULL");
   DeviceGuard guard;
-  s = enter_device(guard, device);
+  s = enter_device(guard, device, nullptr);
   if (s != NNA_OK || !rows) return s;
   const hipError_t e = launch_pack8(x_dev, type, rows, width, row_stride, codes_dev, scales_dev, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_pack8");
@@ -271,7 +286,7 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
   if (s != NNA_OK) return s;
   if (rows && (!out_dev || !codes_dev || !scales_dev)) return fail(NNA_ERR_INVALID_ARG, "out_dev / codes_dev / scales_dev is NULL");
   DeviceGuard guard;
-  s = enter_device(guard, device);
+  s = enter_device(guard, device, nullptr);
   if (s != NNA_OK || !rows) return s;
   const hipError_t e = launch_unpack8(codes_dev, scales_dev, rows, width, out_dev, type, static_cast<hipStream_t>(hip_stream));
   return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_unpack8");
@@ -315,7 +330,7 @@ nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, co
   P.T = (int)T;
   P.H = (int)H;
   DeviceGuard guard;
-  s = enter_device(guard, device);
+  s = enter_device(guard, device, &decay_setup);
   if (s == NNA_OK) s = refuse_same({out_dev}, {q_dev, k_dev, v_dev, first_dev});
   if (s != NNA_OK || !B) return s;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -350,7 +365,7 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
   P.T = (int)T;
   P.H = (int)H;
   DeviceGuard guard;
-  s = enter_device(guard, device);
+  s = enter_device(guard, device, &decay_setup);
   if (s == NNA_OK) s = refuse_same({gq_dev, gk_dev, gv_dev, gfirst_dev}, {gout_dev, q_dev, k_dev, v_dev, first_dev, glast_dev});
   if (s != NNA_OK || !B) return s;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -405,7 +420,7 @@ nna_status nna_decay_attention_step(const void* q_dev, const long long* q_stride
   P.dk = (int)dk;
   P.dv = (int)dv;
   DeviceGuard guard;
-  s = enter_device(guard, device);
+  s = enter_device(guard, device, &decay_setup);
   if (s == NNA_OK) s = refuse_same({out_dev}, {q_dev, k_dev, v_dev, state_dev});
   if (s != NNA_OK || !B) return s;
   const hipError_t e = launch_decay_step(P, type, static_cast<hipStream_t>(hip_stream));

@@ -419,3 +419,43 @@ def test_products_in_8_bits_of_any_number_of_frames(layers, kind, batch, frames)
         grads.append([x.grad.clone()] + [p.grad.clone() for p in layer.parameters()])
     for a, b in zip(*grads):
         assert torch.isfinite(b).all() and (a - b).norm() <= 0.045 * a.norm()
+
+
+FIRST_CALLS = """
+import sys
+import torch
+from paper_1912_12055_amd import binding as nb
+g = torch.Generator(device="cuda:0").manual_seed(1)
+x, w = torch.randn(64, 200, device="cuda:0", generator=g), torch.ones(200, device="cuda:0")
+spec, q = torch.randn(2, 50, 40, device="cuda:0", generator=g), torch.randn(1, 900, 2, 64, device="cuda:0", generator=g)
+decay, state = torch.full((2,), 0.9, device="cuda:0"), torch.zeros(1, 2, 64, 64, device="cuda:0")
+
+def step():
+    y, kept = nb.nna_layer_norm(x, w, keep=8)
+    f, kf = nb.nna_layer_norm(spec.transpose(1, 2), keep=32)
+    o, last = nb.nna_decay_attention(q, q, q, decay, state=state, want_state=True)
+    return [y, *nb.nna_layer_norm_backward(x, kept, w), f, *nb.nna_layer_norm_backward(f, kf), o, last, *nb.nna_decay_attention_backward(o, q, q, q, decay)[:3],
+            nb.nna_unpack8(*nb.nna_pack8(x))]
+
+torch.mm(x, x.T)  # (torch's own set-up)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = step()
+for k in range(3):
+    x.copy_(torch.randn_like(x)), q.copy_(torch.randn_like(q))
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in out]
+    assert all(torch.equal(a, b) for a, b in zip(got, step())), k
+print("the same")
+"""
+
+
+def test_first_calls_of_a_process_inside_a_graph(layers):
+    """The kernels' set-up is done at the first call that needs it, also where that call is recorded."""
+    import subprocess
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=100)
+    assert done.returncode == 0 and "the same" in done.stdout, done.stderr[-2000:]
