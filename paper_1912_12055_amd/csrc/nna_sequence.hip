@@ -138,9 +138,10 @@ nna_status check_decay_args(const void* decay, double scale, const void* workspa
   return NNA_OK;
 }
 
-nna_status check_strides(const long long* const (&strides)[3]) {
+nna_status check_strides(const long long* const (&strides)[3], long long T) {
   for (const long long* s : strides) {
     if (!s) return fail(NNA_ERR_INVALID_ARG, "strides are NULL");
+    if (T <= 1) continue;  // (of one frame there is no next: the step is not taken, whatever it is)
     if (s[1] < 0 || s[1] > DECAY_STEP_MAX) return fail(NNA_ERR_SHAPE, "more than " + std::to_string(DECAY_STEP_MAX) + " elements from one frame to the next");
   }
   return NNA_OK;
@@ -152,7 +153,7 @@ struct Heads {
   long long strides[3];
   int width;
 };
-Heads heads_of(const void* at, const long long* strides, long long width) { return {at, {strides[0], strides[1], strides[2]}, (int)width}; }
+Heads heads_of(const void* at, const long long* strides, long long width, long long T) { return {at, {strides[0], T > 1 ? strides[1] : 0, strides[2]}, (int)width}; }
 
 void set_mix(DecayMix& P, const Heads& a, const Heads& b, const Heads& c) {
   P.a = a.at;
@@ -308,7 +309,7 @@ nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, co
                                void* out_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream) {
   nna_status s = check_heads(type, B, T, H, dk, dv);
   if (s != NNA_OK) return s;
-  s = check_strides({q_strides, k_strides, v_strides});
+  s = check_strides({q_strides, k_strides, v_strides}, T);
   if (s != NNA_OK) return s;
   if (B && T && (!q_dev || !k_dev || !v_dev || !out_dev)) return fail(NNA_ERR_INVALID_ARG, "q_dev / k_dev / v_dev / out_dev is NULL");
   DecayMix P = {};
@@ -317,7 +318,7 @@ nna_status nna_decay_attention(const void* q_dev, const long long* q_strides, co
   if (s == NNA_OK) s = check_decay_args(decay_dev, scale, workspace_dev, workspace_bytes, need);
   if (s != NNA_OK) return s;
   decay_segments(B, T, (int)H, (int)dk, (int)dv, type, false, &P.segments, &P.segment_chunks);
-  set_mix(P, heads_of(q_dev, q_strides, dk), heads_of(k_dev, k_strides, dk), heads_of(v_dev, v_strides, dv));
+  set_mix(P, heads_of(q_dev, q_strides, dk, T), heads_of(k_dev, k_strides, dk, T), heads_of(v_dev, v_strides, dv, T));
   P.out = out_dev;
   P.decay = decay_dev;
   P.lengths = lengths_dev;
@@ -345,7 +346,7 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
                                         void* gv_dev, float* gfirst_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream) {
   nna_status s = check_heads(type, B, T, H, dk, dv);
   if (s != NNA_OK) return s;
-  s = check_strides({q_strides, k_strides, v_strides});
+  s = check_strides({q_strides, k_strides, v_strides}, T);
   if (s != NNA_OK) return s;
   if (B && T && (!gout_dev || !q_dev || !k_dev || !v_dev)) return fail(NNA_ERR_INVALID_ARG, "gout_dev / q_dev / k_dev / v_dev is NULL");
   if (B && T && (!gk_dev || !gv_dev)) return fail(NNA_ERR_INVALID_ARG, "gk_dev / gv_dev is NULL");
@@ -356,7 +357,7 @@ nna_status nna_decay_attention_backward(const void* gout_dev, const void* q_dev,
   if (s != NNA_OK) return s;
   decay_segments(B, T, (int)H, (int)dk, (int)dv, type, true, &P.segments, &P.segment_chunks);
   const long long packed[3] = {T * H * dv, H * dv, dv};
-  const Heads q = heads_of(q_dev, q_strides, dk), k = heads_of(k_dev, k_strides, dk), v = heads_of(v_dev, v_strides, dv), g = heads_of(gout_dev, packed, dv);
+  const Heads q = heads_of(q_dev, q_strides, dk, T), k = heads_of(k_dev, k_strides, dk, T), v = heads_of(v_dev, v_strides, dv, T), g = heads_of(gout_dev, packed, dv, T);
   P.decay = decay_dev;
   P.lengths = lengths_dev;
   P.parts = static_cast<float*>(workspace_dev);

@@ -507,3 +507,12 @@ def test_outputs_over_inputs_are_refused(nb):
     g, f, l = go.data_ptr(), first.data_ptr(), glast.data_ptr()
     for outs in ((P[0], new[1], new[2], None), (new[0], P[1], new[2], None), (new[0], new[1], g, None), (*new, f), (*new, l)):
         assert nb.lib().nna_decay_attention_backward(g, *qkv, None, f, l, *outs, None, 0, 0, st) == nb.NNA_ERR_INVALID_ARG
+
+
+def test_one_frame_from_memory_of_any_order(nb):
+    """of [T, B, H, d] in memory, the distance from one frame to the next is no matter where there is one frame"""
+    q, k, v, go, decay, first, glast = _inputs(3, 1, 2, 16, 24, torch.float32, seed=2)
+    want = _all_of(nb, q, k, v, go, decay, first, glast)
+    far = [torch.as_strided(x, x.shape, (x.stride(0), 1 << 40, x.stride(2), 1)) for x in (q, k, v)]
+    got = _all_of(nb, *far, go, decay, first, glast)
+    assert all(torch.equal(got[name], want[name]) for name in want)

@@ -83,3 +83,10 @@ def test_memory_of_linear_attention():
     assert nb.lib().nna_decay_attention_workspace(1, 10, 8, 64, 64, None) == ARG
     assert nb.lib().nna_decay_attention_backward_workspace(1, 10, 8, 64, 64, None) == ARG
     assert nb.lib().nna_layer_norm_backward_workspace(10, 0, 0, 0, byref(n)) == SHAPE
+
+
+def test_the_step_between_frames_is_checked_where_there_are_two():
+    for s in (strides(640, 1 << 40, 8), strides(640, -8, 8)):
+        assert attend(qs=s, T=2) == SHAPE
+        for T in (0, 1):
+            assert attend(qs=s, T=T) == ARG and "device" in nb.nna_last_error()
