@@ -22,14 +22,16 @@ nna_status enter_device(DeviceGuard& guard, int device, Setup* setup) {
   hipError_t e = guard.enter(device);  // (refuses a device that there is not)
   if (e != hipSuccess) return fail_hip(e, "hipSetDevice");
   if (!setup) return NNA_OK;
-  std::lock_guard<std::mutex> lock(setup->mutex);
-  if ((int)setup->done.size() <= device) setup->done.resize(device + 1, 0);
-  if (!setup->done[device]) {
+  try {
+    std::lock_guard<std::mutex> lock(setup->mutex);
+    if ((int)setup->done.size() <= device) setup->done.resize(device + 1, 0);
+    if (setup->done[device]) return NNA_OK;
     e = setup->init();
-    if (e != hipSuccess) return fail_hip(e, "kernel set-up");
-    setup->done[device] = 1;
+    setup->done[device] = e == hipSuccess;
+  } catch (const std::exception&) {
+    return fail(NNA_ERR_ALLOC, "out of host memory while setting kernels up");
   }
-  return NNA_OK;
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "kernel set-up");
 }
 
 // An output over an input is written while other workgroups still read: refused where the pointers are equal (what overlaps otherwise is the caller's to see to).
