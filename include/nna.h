@@ -627,7 +627,7 @@ nna_status nna_unpack8(const signed char* codes_dev, const float* scales_dev, lo
  * Linear attention with a decay l for each head (the state of a head is a matrix S[dk, dv]):
  *   S_t = l S_{t-1} + k_t^T v_t,   o_t = scale q_t S_t = scale (sum_{s <= t} l^(t-s) (q_t . k_s) v_s + l^(t+1) q_t S_first).
  * nna_decay_attention takes whole sequences, nna_decay_attention_step one new frame of each.
- *   q_dev, k_dev [B, T, H, dk], v_dev [B, T, H, dv]   of `type`, NNA_F32 or NNA_BF16 (float16 has no range for the weights l^(t-s) q . k); a head's
+ *   q_dev, k_dev [B, T, H, dk], v_dev [B, T, H, dv]   of `type`, NNA_F32 or NNA_BF16 (NNA_F16 is not implemented); a head's
  *                values next to each other, strides[3] = elements between batches, frames (0 to
  *                2^24; not read where T = 1), heads (0 where they are shared).  dk, dv 1..128, B H at most 2^21
  *   decay_dev    [H] float32, in [0, 1]: a constant of the head (no gradient is taken)

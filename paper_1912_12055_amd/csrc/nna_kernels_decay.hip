@@ -5,14 +5,14 @@
 // The gradients are the same mix of other arrays: gq = mix(go, v, k) with S^T, and, with time reversed and the state's gradient G in
 // S's place, gk = mix(v, go, q) with G^T, gv = mix(k, q, go) with G.  One kernel runs them all: out = mix(a, b, c).
 //
-// A workgroup of four waves goes through the chunks of a (sequence, head), or of a segment of one where there are too few of them to
-// fill the card (the segments' own states are then summed in a launch before, and joined in order).  Its state stays in registers, float32,
-// a quarter of the columns to a wave; the chunk's a, b and c are in LDS.
+// A workgroup of four waves (float32 heads of 128: eight; gradients in pairs: sixteen) goes through the chunks of a (sequence, head), or of a segment of one where
+// there are too few of them to fill the card (the segments' own states are then summed in a launch before, and joined in order).  Its state stays in registers,
+// float32, some of the columns to a wave; the chunk's a, b and c are in LDS.  Where values are float32 a chunk is 32 frames (Shape).
 //
-// 4 sequences of 16 heads of 128, 16,384 frames, bfloat16: states 129 us (4.2 TB/s), joined in 11, the mix 250 to 275 (4.1 TB/s; a copy as large reaches 5.1), the
-// gradients' states 230, joined in 21, three mixes 775.  Memory is the largest part; the conversions and scalings around the products (670 vector instructions a
-// wave and chunk beside 118 matrix instructions) and the barriers between a chunk's steps keep it from its rate.  Few heads (8 of 64, 15,504 frames): 12, 8 and
-// 20 us, latencies of a segment's chunks one after the other.  float32, 16 sequences of 431 frames, 8 heads of 64: 42 and 56 us, half of the CUs, one wave a SIMD.
+// 4 sequences of 16 heads of 128, 16,384 frames, bfloat16: states 126 us (4.3 TB/s), joined in 11, the mix 305 to 320 (3.4 TB/s; a copy as large reaches 5.1), the
+// gradients' states 223, joined in 21, three mixes 855 to 930.  The conversions and scalings around the products (830 vector instructions a wave and chunk beside 162
+// matrix instructions) and the barriers between a chunk's steps keep it from memory's rate.  Few heads (8 of 64, 15,504 frames): 13, 8 and 25 us, latencies of a
+// segment's chunks one after the other.  float32, 16 sequences of 431 frames, 8 heads of 64: 43 and 60 us, half of the CUs, one wave a SIMD.
 #include "nna_decay.h"
 
 namespace nna {
@@ -263,8 +263,8 @@ constexpr int sums_of() { return sizeof(T) == 4 ? 3 : 2; }
 enum { MIX, STATE, PAIR };
 constexpr int XCDS = 8;  // workgroups go to them in turn
 
-// Frames of a chunk: 64; of three planes 32, so that heads of 64 leave room for two workgroups on a CU (64 clips of 431 frames, 8 heads of 64, float32: 61 us forward
-// and 153 backward, 87 and 208 with 64; one workgroup a CU: the same) and heads of 128 for one.  Columns of the state to a wave: 32 where a state of 128 x 32 and
+// Frames of a chunk: 64; of three planes 32, so that heads of 64 leave room for two workgroups on a CU (64 clips of 431 frames, 8 heads of 64, float32: 64 us forward
+// and 165 backward, 90 and 262 with 64) and heads of 128 for one.  Columns of the state to a wave: 32 where a state of 128 x 32 and
 // the rest fit 256 registers, so that what is read from LDS meets two products; else 16.
 template <typename T, int DA, int DC>
 struct Shape {
@@ -653,8 +653,8 @@ __global__ __launch_bounds__((Shape<T, D, D>::threads(PAIR)), 2) void decay_grad
 
 // The gradients as mixes of their own, all in one launch: gv, gk and (if wanted) gq of a segment in workgroups of one XCD, begun together, so that what two of them
 // read comes from its cache the second time.  Two such workgroups fit a CU and one's products run beside the other's loads and barriers; a pair reads a third less but
-// has the CU for itself (bfloat16, 64 heads of 128, 16,384 frames: 820 us, gq and then the pair 863; float32, 32 clips of 431 frames, 8 heads of 64: 80 and 102).
-// Heads of 128 in float32 fill a CU either way: there the pair is ahead (16 clips of 431 frames, 8 heads: 119 us, 150 as mixes).
+// has the CU for itself (bfloat16, 64 heads of 128, 16,384 frames: 1,045 us with the states before, gq and then the pair 1,080; float32, 32 clips of 431 frames, 8 heads of 64: 87 and 105).
+// Heads of 128 in float32 fill a CU either way: there the pair is ahead (16 clips of 431 frames, 8 heads: a quarter faster than as mixes, 126 us).
 template <typename T, int DK, int DV, int PLANES, bool FULL>
 __global__ __launch_bounds__((Shape<T, DK, DV>::THREADS), 2) void decay_mixes_kernel(DecayMix V, DecayMix K, DecayMix Q, int workgroups, int mixes) {
   extern __shared__ __align__(16) unsigned char lds[];
@@ -957,15 +957,18 @@ hipError_t decay_kernels_init() {
 // Segments cost half as much again (their states) and a launch that joins them, so there are some only where the heads alone leave the card idle, and then as many as
 // its workgroups: 512 forward (256 in float32 with heads of 128: one a CU), 256 backward, of three mixes each.  Forward / backward in us, the number of segments before
 // the colon:
-//   float32, heads of 64    8 heads, 2,048 frames      1: 174/182  8: 45/49    32: 27/37
-//                           64 heads, 1,024 frames     1: 89/96    4: 48/76    8: 41/79
-//                           128 heads, 1,024 frames    1: 89/123   4: 63/128
-//   bfloat16, heads of 64   8 heads, 512 frames        1: 23/25    4: 25/28            (float32: 1: 47/50  4: 31/32)
-//                           128 heads, 16,384 frames   1: 600/775  4: 355/841
-//                           256 heads, 2,048 frames    1: 79/170   2: 85/201
-//   bfloat16, heads of 128  64 heads, 1,024 frames     1: 69/73    4: 50/92
-//                           64 heads, 16,384 frames    1: 1088/1117  4: 419/939  8: 397/938
-//   float32, heads of 128   128 heads, 2,048 frames    1: 334/556  2: 270/626  4: 283/669
+//   float32, heads of 64    8 heads, 2,048 frames      1: 185/189  8: 47/51    32: 27/40
+//                           64 heads, 1,024 frames     1: 96/103   4: 51/82    8: 44/82
+//                           128 heads, 1,024 frames    1: 96/137   4: 67/135
+//   bfloat16, heads of 64   8 heads, 512 frames        1: 26/27    4: 22/24            (float32: 1: 49/51  4: 28/31)
+//                           128 heads, 16,384 frames   1: 719/896  4: 343/865
+//                           256 heads, 2,048 frames    1: 94/180   2: 94/211
+//   bfloat16, heads of 128  64 heads, 1,024 frames     1: 86/88    4: 54/97
+//                           64 heads, 16,384 frames    1: 1370/1388  4: 491/1036  8: 398/1020
+//   float32, heads of 128   128 heads, 2,048 frames    1: 348/550  2: 270/617  4: 274/663
+// Between them: bfloat16, heads of 64, 96 heads, 1,024 frames 1: 49/60  5: 34/59, 8,192 frames 1: 355/447  5: 135/329 (backward one is taken: the rule is the short one's);
+// heads of 128 1: 86/115  5: 65/132; 200 heads forward, where one each leaves a quarter of the card idle: 2,048 frames 1: 92  2: 87, heads of 128 1: 179  2: 188, float32
+// 1,024 frames 1: 95  2: 104.
 size_t decay_segments(long long B, long long T, int H, int dk, int dv, int type, bool backward, int* segments, int* chunks) {
   const long long all = std::max(1LL, (T + CHUNK - 1) / CHUNK), heads = std::max(1LL, B * H);
   const bool wide = dk > 64 || dv > 64;
@@ -1021,7 +1024,7 @@ hipError_t launch_decay_gradients(DecayMix states, DecayMix gq, DecayMix pair, i
     if (e != hipSuccess) return e;
   }
   if (!in_pairs(type, pair.da, pair.dc)) return launch_mixes(gq, pair, type, given, workgroups, stream);
-  // a workgroup a CU at most: together (16 clips of up to 431 frames, 8 heads of 64, float32: 63 us, 48 and 60 in two launches); more than that, the waves that
+  // a workgroup a CU at most: together (16 clips of 431 frames, 8 heads of 128, float32: 126 us, 195 in two launches); more than that, the waves that
   // only wait would hold registers that a second workgroup runs in
   if (gq.out && 2 * workgroups <= 256) return launch_both(gq, pair, type, given, workgroups, true, stream);
   if (gq.out) {

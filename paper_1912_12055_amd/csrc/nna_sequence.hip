@@ -110,7 +110,7 @@ nna_status check_pack(int type, long long rows, long long width) {
 
 nna_status check_heads(int type, long long B, long long T, long long H, long long dk, long long dv) {
   if (!known_type(type)) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
-  if (type == NNA_F16) return fail(NNA_ERR_UNSUPPORTED, "float16 has no range for the weights: float32 or bfloat16");
+  if (type == NNA_F16) return fail(NNA_ERR_UNSUPPORTED, "float16 is not implemented here: float32 or bfloat16");
   if (B < 0 || T < 0 || H < 1 || dk < 1 || dv < 1) return fail(NNA_ERR_SHAPE, "B and T must not be negative, H, dk and dv at least 1");
   if (dk > DECAY_HEAD_MAX || dv > DECAY_HEAD_MAX) return fail(NNA_ERR_UNSUPPORTED, "heads of more than " + std::to_string(DECAY_HEAD_MAX) + " values");
   // (sequence, head)s times the lanes of their workgroups, up to four of 256 or one of 1,024, are less than 2^32 in a launch
