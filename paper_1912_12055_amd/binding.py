@@ -991,10 +991,10 @@ def nna_layer_norm(x, weight=None, bias=None, eps=1e-5, out_dtype=None, keep=0, 
         raise TypeError(f"out must be a contiguous {out_dtype} CUDA tensor of shape {tuple(shape)}")
     if given is not None and keep == 32 and _overlap(out, x):
         raise ValueError("keep=32 keeps x itself: out must not share its memory")
-    if given is not None:  # (over x only where every row is written where it was read, by the lanes that read it)
-        _refuse_overlap(out, weight, bias, None if x.is_contiguous() and x.dtype == out_dtype and x.data_ptr() == out.data_ptr() else x)
     yt = _type_of(out, "out")
     w, b = _vector(weight, "weight", (width,), device, none=True), _vector(bias, "bias", (width,), device, none=True)
+    if given is not None:  # (over x only where every row is written where it was read, by the lanes that read it)
+        _refuse_overlap(out, weight, bias, None if x.is_contiguous() and x.dtype == out_dtype and x.data_ptr() == out.data_ptr() else x)
     rows = x.numel() // width if width else 0
     step = _row_stride(x)
     kept = stats = codes = scales = None

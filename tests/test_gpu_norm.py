@@ -395,3 +395,12 @@ def test_outputs_over_inputs_are_refused(nb):
     gx = nb.nna_layer_norm_backward(g, kept, w, want_gw=False)[0]
     assert back(g.data_ptr(), nb.NNA_F32, x.data_ptr(), nb.NNA_F32, 300, 640, 640, None, None, kept.stats.data_ptr(), w.data_ptr(), g.data_ptr(), None, None, None, 0, 0, st) == nb.NNA_OK
     assert torch.equal(g, gx)
+
+
+def test_weights_that_are_no_tensors_are_refused_with_a_given_output_too(nb):
+    x = torch.ones(3, 8, device=DEV)
+    for bad in ([1.0] * 8, np.ones(8, np.float32)):
+        for kw in (dict(weight=bad), dict(bias=bad)):
+            for out in (None, torch.empty_like(x)):
+                with pytest.raises(TypeError):
+                    nb.nna_layer_norm(x, out=out, **kw)
