@@ -830,6 +830,7 @@ NNA_BLOCK8 = 128
 NNA_FRAMES_WIDTH = 2112  # bins of the frames that nna_layer_norm reads as the transforms write them
 _types = {}
 _current_stream = None
+_increment_version = None
 
 
 def _stream_on(device, stream):
@@ -892,11 +893,12 @@ def _vector(t, name, shape, device, none=False):
 def _written(*tensors):
     """Tells autograd of tensors of the caller's that a call has written through their pointers, as torch's own in-place operations do: a graph that
     holds one of them for its backward pass then refuses to run on the new values.  (0.3 us a tensor.)"""
-    from torch.autograd.graph import increment_version
-
+    global _increment_version
+    if _increment_version is None:
+        from torch.autograd.graph import increment_version as _increment_version
     for t in tensors:
         if t is not None:
-            increment_version(t)
+            _increment_version(t)
 
 
 def _bytes_of(t):
