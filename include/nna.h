@@ -663,6 +663,88 @@ nna_status nna_decay_attention_step(const void* q_dev, const long long* q_stride
                                     const long long* v_strides, nna_dtype type, long long B, long long H, long long dk, long long dv,
                                     const float* decay_dev, double scale, float* state_dev, void* out_dev, int device, void* hip_stream);
 
+/*
+ * Queries and keys of T frames: each head normalised, and its pairs rotated by the frame's position, in one pass:
+ *   h = x r w,  r = 1 / sqrt(mean(x^2) + eps)  (norm != 0; h = x without);   a pair (a, b) of h becomes (a cos - b sin, a sin + b cos) of the angle p f.
+ *   q_dev [B, T, q_heads, width], k_dev [B, T, k_heads, width]   of `type`, a head's values (1..256) next to each other, strides[3] = elements between batches,
+ *                frames, heads.  k_heads may be 0 (no keys), and differ from q_heads
+ *   freqs_dev    [pairs] float64 in device memory: radians a position.  The first 2 pairs values of a head are rotated: pair j is (j, j + pairs), or with `interleaved`
+ *                (2 j, 2 j + 1); those behind are normalised alone.  Angles are products of 64 bits: positions of millions of frames keep theirs
+ *   positions_dev  int32 in device memory, positions_strides[2] = elements between batches, frames; or NULL: frame t is at offset + t
+ *   q_weight_dev, k_weight_dev  [width] float32, or NULL: ones (only with norm)
+ *   q_out_dev, k_out_dev  [B, T, heads, width] of `type`, contiguous; none of the inputs
+ * nna_rotate_heads_backward: from gq_out_dev, gk_out_dev (contiguous, as the outputs) the gradients gq_dev, gk_dev (contiguous, of `type`) of q and k, and those of the
+ * weights (float32 [width], or NULL) by way of workspace_dev (16-byte aligned, nna_rotate_heads_backward_workspace bytes; not read where both are NULL).  Without
+ * norm q_dev and k_dev are not read.  Sums are float32 in an order that goes with the shape alone.
+ * A value that is not finite reaches its own head's outputs of its own frame, and the weights' gradients.
+ * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_UNSUPPORTED (heads of more than 256 values), NNA_ERR_SHAPE.  B = 0 or T = 0 is no error.
+ */
+nna_status nna_rotate_heads(const void* q_dev, const long long* q_strides, long long q_heads, const void* k_dev, const long long* k_strides, long long k_heads,
+                            nna_dtype type, long long B, long long T, long long width, const double* freqs_dev, long long pairs, int interleaved,
+                            const int* positions_dev, const long long* positions_strides, long long offset, int norm, double eps, const float* q_weight_dev,
+                            const float* k_weight_dev, void* q_out_dev, void* k_out_dev, int device, void* hip_stream);
+nna_status nna_rotate_heads_backward_workspace(long long B, long long T, long long width, size_t* bytes);
+nna_status nna_rotate_heads_backward(const void* gq_out_dev, const void* gk_out_dev, const void* q_dev, const long long* q_strides, long long q_heads, const void* k_dev,
+                                     const long long* k_strides, long long k_heads, nna_dtype type, long long B, long long T, long long width, const double* freqs_dev,
+                                     long long pairs, int interleaved, const int* positions_dev, const long long* positions_strides, long long offset, int norm,
+                                     double eps, const float* q_weight_dev, const float* k_weight_dev, void* gq_dev, void* gk_dev, float* gq_weight_dev,
+                                     float* gk_weight_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream);
+
+/*
+ * Gated linear recurrence of C channels:  h_t = a_t h_{t-1} + u_t x_t,  a = sigmoid(forget),  u = sigmoid(input), or 1 - a where input_dev is NULL.
+ * nna_gated_scan takes whole sequences, nna_gated_scan_step one new frame of each.
+ *   x_dev, forget_dev, input_dev  [B, T, C] of `type`, a frame's channels next to each other, strides[2] = elements between batches, frames (not read where T is 1)
+ *   lengths_dev  [B] int32 in device memory, or NULL: T.  Frames from a sequence's length on (below 0: 0, above T: T) take no part: their values are not
+ *                used, their outputs and gradients are 0, and the last state is that after the length
+ *   first_dev, last_dev  [B, C] float32 or NULL: the state before the first frame (NULL: 0), and after the last; not the same
+ *   out_dev      [B, T, C] of `type`, contiguous: h
+ *   kept_dev     NULL, or [B, ceil(T / NNA_SCAN_KEPT), C] float32 for the backward call: the states before every NNA_SCAN_KEPT-th frame
+ *   workspace_dev  256-byte aligned, nna_gated_scan_workspace bytes (0: may be NULL), of either call
+ * States are float32, and 1 - a is computed as sigmoid(-forget): channels that remember for thousands of frames keep their decay to float32's precision.  A value that is not
+ * finite leaves its channel's outputs not finite from its frame on.
+ *
+ * nna_gated_scan_backward: from gout_dev [B, T, C] (contiguous), glast_dev [B, C] (or NULL: 0) and kept_dev the gradients gx_dev, gforget_dev, ginput_dev (with input_dev)
+ * [B, T, C] (contiguous, of `type`) and gfirst_dev [B, C] (float32, or NULL).  Outputs are none of the inputs.  The same inputs give the same bits.
+ * nna_gated_scan_step: x_dev, forget_dev, input_dev [B, C] with their stride between batches; state_dev [B, C] updated in place; out_dev [B, C], contiguous.
+ * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_SHAPE (B times C, in 64s, above 2^22).  T = 0 or B = 0 is no error.
+ */
+#define NNA_SCAN_KEPT 64
+nna_status nna_gated_scan_workspace(long long B, long long T, long long C, size_t* bytes);
+nna_status nna_gated_scan(const void* x_dev, const long long* x_strides, const void* forget_dev, const long long* forget_strides, const void* input_dev,
+                          const long long* input_strides, nna_dtype type, long long B, long long T, long long C, const int* lengths_dev, const float* first_dev,
+                          float* last_dev, void* out_dev, float* kept_dev, void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream);
+nna_status nna_gated_scan_backward(const void* gout_dev, const float* kept_dev, const void* x_dev, const long long* x_strides, const void* forget_dev,
+                                   const long long* forget_strides, const void* input_dev, const long long* input_strides, nna_dtype type, long long B, long long T,
+                                   long long C, const int* lengths_dev, const float* glast_dev, void* gx_dev, void* gforget_dev, void* ginput_dev, float* gfirst_dev,
+                                   void* workspace_dev, size_t workspace_bytes, int device, void* hip_stream);
+nna_status nna_gated_scan_step(const void* x_dev, long long x_stride, const void* forget_dev, long long forget_stride, const void* input_dev, long long input_stride,
+                               nna_dtype type, long long B, long long C, float* state_dev, void* out_dev, int device, void* hip_stream);
+
+/*
+ * One AdamW step over `count` tensors:  m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,  p <- (1 - lr wd) p - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps).
+ *   tensors      [count] in host memory (read during the call): n values p_dev, updated, and their gradient g_dev, of `type`, contiguous; n may be 0.  Their states begin at value
+ *                `at` of m and v: multiples of 128, in the tensors' order, without overlap.  No two tensors may share memory
+ *   m_dev, v_dev [state_size] float32, m_scales_dev and v_scales_dev NULL; or int8 (m) and uint8 (v) codes with float32 scales [state_size / 128].  Zeros before the first step
+ *   master_dev   [state_size] float32 or NULL: the float32 copies that tensors of 16 bits are updated in and rounded from (float32 tensors have none)
+ *   step_dev, lr_dev  NULL, or the step's number (from 1) and lr in device memory in the place of step and lr: for steps recorded into a graph
+ * 8 bits: 128 neighbours share a scale s, their largest magnitude.  A code c of m stands for s (c / 127) |c / 127|, rounded to the nearest code; one of v for s (c / 255)^4, rounded
+ * down from (255 (v / s)^(1/4) + d), at least 1 where v > 0, d in [0, 1) the fraction (first 24 bits) of (at + index) 0x9E3779B9 + t 0xB504F333 over 2^32.  The update itself
+ * uses the moments before they are rounded; they are float64 until then, each product and sum rounded by itself.  A block with a value that is not finite stands for NaN throughout; one below 2^-126 for zero.
+ * nna_adamw_moment: out_dev [size] float32 = what the codes of m, or (second != 0) of v, stand for; size a multiple of 128.
+ * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_SHAPE, NNA_ERR_ALLOC.  A value that is not finite reaches its own weight (8 bits: its block's).
+ */
+typedef struct {
+  void* p_dev;
+  const void* g_dev;
+  long long n, at;
+  int type; /* nna_dtype */
+  int reserved;
+} nna_adamw_tensor;
+nna_status nna_adamw(const nna_adamw_tensor* tensors, long long count, void* m_dev, void* v_dev, float* m_scales_dev, float* v_scales_dev, float* master_dev,
+                     long long state_size, long long step, const long long* step_dev, double lr, const float* lr_dev, double beta1, double beta2, double eps,
+                     double weight_decay, int device, void* hip_stream);
+nna_status nna_adamw_moment(const void* codes_dev, int second, const float* scales_dev, long long size, float* out_dev, int device, void* hip_stream);
+
 void nna_plan_destroy(nna_plan* plan); /* NULL is allowed */
 
 const char* nna_status_str(nna_status s);

@@ -41,6 +41,9 @@ EXPORTS = [
     "nna_layer_norm", "nna_layer_norm_frames", "nna_layer_norm_backward_workspace", "nna_layer_norm_backward",
     "nna_layer_norm_frames_backward", "nna_pack8", "nna_unpack8",
     "nna_decay_attention_workspace", "nna_decay_attention_backward_workspace", "nna_decay_attention", "nna_decay_attention_backward", "nna_decay_attention_step",
+    "nna_rotate_heads", "nna_rotate_heads_backward_workspace", "nna_rotate_heads_backward",
+    "nna_gated_scan_workspace", "nna_gated_scan", "nna_gated_scan_backward", "nna_gated_scan_step",
+    "nna_adamw", "nna_adamw_moment",
 ]
 
 _c = ctypes
@@ -130,6 +133,18 @@ def lib():
         L.nna_decay_attention.argtypes = [*qkv, _I, *shape, _VP, _D, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
         L.nna_decay_attention_backward.argtypes = [_VP, *qkv, _I, *shape, _VP, _D, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
         L.nna_decay_attention_step.argtypes = [*qkv, _I, _LL, _LL, _LL, _LL, _VP, _D, _VP, _VP, _I, _VP]
+        _PLL = _c.POINTER(_LL)
+        heads, turns = 2 * [_VP, _PLL, _LL] + [_I, _LL, _LL, _LL], [_VP, _LL, _I, _VP, _PLL, _LL, _I, _D, _VP, _VP]
+        L.nna_rotate_heads.argtypes = [*heads, *turns, _VP, _VP, _I, _VP]
+        L.nna_rotate_heads_backward_workspace.argtypes = [_LL, _LL, _LL, _c.POINTER(_c.c_size_t)]
+        L.nna_rotate_heads_backward.argtypes = [_VP, _VP, *heads, *turns, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
+        gates, frames = 3 * [_VP, _PLL], [_I, _LL, _LL, _LL, _VP]
+        L.nna_gated_scan_workspace.argtypes = [_LL, _LL, _LL, _c.POINTER(_c.c_size_t)]
+        L.nna_gated_scan.argtypes = [*gates, *frames, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
+        L.nna_gated_scan_backward.argtypes = [_VP, _VP, *gates, *frames, _VP, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
+        L.nna_gated_scan_step.argtypes = [_VP, _LL, _VP, _LL, _VP, _LL, _I, _LL, _LL, _VP, _VP, _I, _VP]
+        L.nna_adamw.argtypes = [_VP, _LL, _VP, _VP, _VP, _VP, _VP, _LL, _LL, _VP, _D, _VP, _D, _D, _D, _D, _I, _VP]
+        L.nna_adamw_moment.argtypes = [_VP, _I, _VP, _LL, _VP, _I, _VP]
         L.nna_out_shape.argtypes = [_VP, _LL, _LL, _c.POINTER(_LL), _c.POINTER(_LL)]
         for name in ("nna_stft", "nna_mel", "nna_cqt", "nna_cqt1992", "nna_cqt2010v2_static"):
             getattr(L, name).argtypes = [_VP, _VP, _LL, _LL, _VP, _VP]
@@ -1230,4 +1245,315 @@ def nna_decay_attention_step(q, k, v, decay, state, scale=None, out=None, stream
     _check(lib().nna_decay_attention_step(*args, t, B, H, dk, dv, dp, dk**-0.5 if scale is None else scale, sp, out.data_ptr(), device.index,
                                           _stream_on(device, stream)))
     _written(state, given)
+    return out
+
+
+def nna_rotary_freqs(width, base=10000.0, scale=1.0, device=0):
+    """float64 [width // 2] on the GPU: radians a position for nna_rotate_heads, base^(-2 i / width) / scale, of heads whose first `width` values (even) are rotated.
+    `scale` above 1 stretches positions for contexts longer than those trained on; another `base` stretches the slow pairs alone.  Any other rule is its own tensor."""
+    import torch
+
+    width = int(width)
+    if width < 0 or width % 2:
+        raise ValueError("width must be even")
+    if not (base > 0 and scale > 0 and np.isfinite(base) and np.isfinite(scale)):
+        raise ValueError("base and scale must be positive")
+    return torch.from_numpy(float(base) ** (-np.arange(0, width, 2, dtype=np.float64) / max(1, width)) / float(scale)).to(device if device is not None else "cpu")
+
+
+def _turns(q, k, freqs, positions, offset, q_weight, k_weight, eps):
+    """(nna_dtype, (B, T, heads, key heads, width), [q, strides, heads, k, strides, heads], the arguments from freqs to the weights) of q, k [B, (T,) heads, width]."""
+    import torch
+
+    t, tensor, device = _type_of(q, "q"), torch.Tensor, q.device
+    shape, axes = q.shape, q.dim()
+    if axes not in (3, 4):
+        raise TypeError("q must be [B, T, heads, width], or [B, heads, width] of one frame")
+    if k is not None and not (isinstance(k, tensor) and k.dtype == q.dtype and k.device == device and k.dim() == axes and k.shape[:-2] == shape[:-2] and k.shape[-1] == shape[-1]):
+        raise TypeError("k must be of q's type, on its device and of its shape but for the number of heads")
+    B, T, H, width = shape if axes == 4 else (shape[0], 1, *shape[1:])
+    args = []
+    for x in (q, k):
+        if x is None:
+            args += [None, None, 0]
+            continue
+        *s, last = x.stride()
+        if width != 1 and last != 1:
+            raise TypeError("a head's values must lie next to each other")
+        args += [x.data_ptr(), _strides3(*s) if axes == 4 else _strides3(s[0], 0, s[1]), x.shape[-2]]
+    if not (isinstance(freqs, tensor) and freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous() and freqs.device == device):
+        raise TypeError(f"freqs must be a contiguous float64 tensor of one axis on {device}")
+    at, steps = None, None
+    if positions is not None:
+        if not (isinstance(positions, tensor) and positions.dtype == torch.int32 and positions.device == device and positions.shape == shape[: axes - 2]):
+            raise TypeError(f"positions must be an int32 tensor of shape {tuple(shape[: axes - 2])} on {device}")
+        if offset:
+            raise ValueError("offset is where positions are not given")
+        at, steps = positions.data_ptr(), _strides2(*positions.stride()) if axes == 4 else _strides2(positions.stride(0), 0)
+    if eps is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("weights are the norm's: give eps")
+    weights = (_vector(q_weight, "q_weight", (width,), device, none=True), _vector(k_weight, "k_weight", (width,), device, none=True))
+    return t, (B, T, H, args[5], width), args, (freqs.data_ptr(), freqs.shape[0], at, steps, int(offset), eps is not None, 0.0 if eps is None else eps, *weights)
+
+
+def nna_rotate_heads(q, k, freqs, positions=None, offset=0, q_weight=None, k_weight=None, eps=None, interleaved=False, out=None, stream=None):
+    """(q, k) with each head normalised by its root mean square (`eps` given; times q_weight, k_weight, float32 [width]) and the pairs of its first 2 len(freqs) values
+    rotated by position * freqs, contiguous.  q [B, T, heads, width], k [B, T, its own heads, width] or None; or [B, heads, width] of one frame: float32, bfloat16 or float16,
+    any strides but the last.  freqs: float64 (nna_rotary_freqs).  positions: int32 [B, T] ([B]) on the GPU; if None, frame t is at offset + t.  Pair j is (j, j + len(freqs)), or
+    `interleaved` (2 j, 2 j + 1).  out: (q, k) to write to, not over inputs."""
+    import torch
+
+    t, (B, T, _, heads, width), args, (freqs_p, pairs, *rest) = _turns(q, k, freqs, positions, offset, q_weight, k_weight, eps)
+    device = q.device
+    if stream is not None and (done := _under(stream, device, lambda: nna_rotate_heads(q, k, freqs, positions, offset, q_weight, k_weight, eps, interleaved, out))) is not None:
+        return done
+    if out is None:
+        yq, yk = torch.empty_like(q, memory_format=torch.contiguous_format), None if k is None else torch.empty_like(k, memory_format=torch.contiguous_format)
+    else:
+        yq, yk = out
+        for y, x in ((yq, q), (yk, k)):
+            if (y is None) != (x is None) or (y is not None and not (y.dtype == x.dtype and y.is_contiguous() and y.shape == x.shape and y.device == device)):
+                raise TypeError("out must be contiguous tensors of q's and k's shapes and type")
+            if y is not None:
+                _refuse_overlap(y, q, k, freqs, positions, q_weight, k_weight)
+        if yk is not None and _overlap(yq, yk):
+            raise ValueError("the outputs must not share memory")
+    _check(lib().nna_rotate_heads(*args, t, B, T, width, freqs_p, pairs, bool(interleaved), *rest, yq.data_ptr(), None if yk is None else yk.data_ptr(), device.index,
+                                  _stream_on(device, stream)))
+    if out is not None:
+        _written(yq, yk)
+    return yq, yk
+
+
+def nna_rotate_heads_backward_workspace(B: int, T: int, width: int) -> int:
+    n = _c.c_size_t()
+    _check(lib().nna_rotate_heads_backward_workspace(B, T, width, _c.byref(n)))
+    return n.value
+
+
+def nna_rotate_heads_backward(gq, gk, q, k, freqs, positions=None, offset=0, q_weight=None, k_weight=None, eps=None, interleaved=False, want_weights=True,
+                              workspace=None, stream=None):
+    """(gradient of q, of k, of q_weight, of k_weight; None where there is none or not wanted) of a loss through nna_rotate_heads, given gq, gk = dLoss/d(its outputs), contiguous.
+    The weights' are those of ones where they are not given.  `workspace`: nna_rotate_heads_backward_workspace bytes (taken here if None)."""
+    import torch
+
+    t, (B, T, _, heads, width), args, (freqs_p, pairs, *rest) = _turns(q, k, freqs, positions, offset, q_weight, k_weight, eps)
+    device = q.device
+    if stream is not None and (done := _under(stream, device, lambda: nna_rotate_heads_backward(gq, gk, q, k, freqs, positions, offset, q_weight, k_weight, eps, interleaved,
+                                                                                                want_weights, workspace))) is not None:
+        return done
+    for g, x in ((gq, q), (gk, k)):
+        if (g is None) != (x is None) or (g is not None and not (isinstance(g, torch.Tensor) and g.dtype == x.dtype and g.is_contiguous() and g.shape == x.shape
+                                                                 and g.device == device)):
+            raise TypeError("gq and gk must be contiguous tensors of q's and k's shapes and type")
+    hq, hk = torch.empty_like(gq), None if k is None else torch.empty_like(gk)
+    gqw = gkw = None
+    ws = (None, 0)
+    if want_weights and eps is not None:
+        gqw = torch.empty(width, dtype=torch.float32, device=device)
+        gkw = None if k is None else torch.empty(width, dtype=torch.float32, device=device)
+        need = nna_rotate_heads_backward_workspace(B, T, width)
+        workspace = _workspace_on(stream, need, workspace, device)
+        ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+    def at(x):
+        return None if x is None else x.data_ptr()
+
+    _check(lib().nna_rotate_heads_backward(gq.data_ptr(), at(gk), *args, t, B, T, width, freqs_p, pairs, bool(interleaved), *rest, hq.data_ptr(), at(hk), at(gqw), at(gkw),
+                                           *ws, device.index, _stream_on(device, stream)))
+    return hq, hk, gqw, gkw
+
+
+NNA_SCAN_KEPT = 64
+
+
+def _gates(x, forget, input, axes):
+    """(nna_dtype, x's shape, [x, strides, forget, strides, input, strides]) of [B, (T,) C] tensors."""
+    import torch
+
+    t = _type_of(x, "x")
+    if x.dim() != axes:
+        raise TypeError("x must be " + ("[B, T, C]" if axes == 3 else "[B, C]"))
+    args = []
+    for name, g in (("x", x), ("forget", forget), ("input", input)):
+        if g is None and name == "input":
+            args += [None, None if axes == 3 else 0]
+            continue
+        if not (isinstance(g, torch.Tensor) and g.dtype == x.dtype and g.device == x.device and g.shape == x.shape):
+            raise TypeError(f"{name} must be of x's type and shape, on its device")
+        *s, last = g.stride()
+        if last != 1 and x.shape[-1] != 1:
+            raise TypeError(f"{name}: a frame's channels must lie next to each other")
+        args += [g.data_ptr(), _strides2(*s) if axes == 3 else s[0]]
+    return t, x.shape, args
+
+
+def nna_gated_scan_workspace(B: int, T: int, C: int) -> int:
+    """Bytes that nna_gated_scan and nna_gated_scan_backward need; 0 where there are sequences and channels enough to fill the card."""
+    n = _c.c_size_t()
+    _check(lib().nna_gated_scan_workspace(B, T, C, _c.byref(n)))
+    return n.value
+
+
+def _scan_workspace(B, T, C, workspace, device, stream):
+    need = nna_gated_scan_workspace(B, T, C)
+    if not need:
+        return None, (None, 0)
+    workspace = _workspace_on(stream, need, workspace, device)
+    return workspace, (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def nna_gated_scan(x, forget, input=None, state=None, lengths=None, want_state=False, keep=False, out=None, workspace=None, stream=None):
+    """h[B, T, C] of the gated recurrence h_t = a_t h_{t-1} + u_t x_t, a = sigmoid(forget), u = sigmoid(input), or 1 - a where input is None; with `want_state` also the state after
+    the last frame, float32 [B, C], with `keep` also what nna_gated_scan_backward takes (the states before every 64th frame).  x, forget, input [B, T, C]: float32, bfloat16 or
+    float16, any strides but the last.  state: float32 [B, C] before the first frame (None: zero).  lengths: int32 [B] on the GPU; frames from there on take no part, and their
+    outputs are zero.  `workspace`: nna_gated_scan_workspace bytes, 256-byte aligned (taken here if None)."""
+    import torch
+
+    t, (B, T, C), args = _gates(x, forget, input, 3)
+    device = x.device
+    if stream is not None and (done := _under(stream, device, lambda: nna_gated_scan(x, forget, input, state, lengths, want_state, keep, out, workspace))) is not None:
+        return done
+    sp, lp = _vector(state, "state", (B, C), device, none=True), _lengths(lengths, B, device)
+    given = out
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    elif not (isinstance(out, torch.Tensor) and out.dtype == x.dtype and out.is_contiguous() and out.shape == x.shape and out.device == device):
+        raise TypeError(f"out must be a contiguous {x.dtype} tensor of shape {(B, T, C)}")
+    else:
+        _refuse_overlap(out, x, forget, input, state, lengths)
+    last = torch.empty((B, C), dtype=torch.float32, device=device) if want_state else None
+    kept = torch.empty((B, -(-T // NNA_SCAN_KEPT), C), dtype=torch.float32, device=device) if keep else None
+    workspace, ws = _scan_workspace(B, T, C, workspace, device, stream)
+    _check(lib().nna_gated_scan(*args, t, B, T, C, lp, sp, last.data_ptr() if want_state else None, out.data_ptr(), kept.data_ptr() if keep else None, *ws,
+                                device.index, _stream_on(device, stream)))
+    if given is not None:
+        _written(given)
+    result = (out, *((last,) if want_state else ()), *((kept,) if keep else ()))
+    return result if len(result) > 1 else out
+
+
+def nna_gated_scan_backward(gout, kept, x, forget, input=None, lengths=None, gstate=None, want_gstate=False, workspace=None, stream=None):
+    """(gx, gforget, ginput or None, gradient of the first state or None): the gradients of a loss through nna_gated_scan, given gout = dLoss/dh (contiguous), what that call
+    kept, and gstate = dLoss/d(last state) (None: zero).  `workspace`: nna_gated_scan_workspace bytes (taken here if None)."""
+    import torch
+
+    t, (B, T, C), args = _gates(x, forget, input, 3)
+    device = x.device
+    if stream is not None and (done := _under(stream, device, lambda: nna_gated_scan_backward(gout, kept, x, forget, input, lengths, gstate, want_gstate, workspace))) is not None:
+        return done
+    lp, gp = _lengths(lengths, B, device), _vector(gstate, "gstate", (B, C), device, none=True)
+    kp = _vector(kept, "kept", (B, -(-T // NNA_SCAN_KEPT), C), device)
+    if not (isinstance(gout, torch.Tensor) and gout.dtype == x.dtype and gout.is_contiguous() and gout.shape == x.shape and gout.device == device):
+        raise TypeError(f"gout must be a contiguous {x.dtype} tensor of shape {(B, T, C)}")
+    gx, gf, gi = torch.empty_like(gout), torch.empty_like(gout), None if input is None else torch.empty_like(gout)
+    first = torch.empty((B, C), dtype=torch.float32, device=device) if want_gstate else None
+    workspace, ws = _scan_workspace(B, T, C, workspace, device, stream)
+    _check(lib().nna_gated_scan_backward(gout.data_ptr(), kp, *args, t, B, T, C, lp, gp, gx.data_ptr(), gf.data_ptr(), None if gi is None else gi.data_ptr(),
+                                         first.data_ptr() if want_gstate else None, *ws, device.index, _stream_on(device, stream)))
+    return gx, gf, gi, first
+
+
+def nna_gated_scan_step(x, forget, state, input=None, out=None, stream=None):
+    """h[B, C] of one new frame x, forget(, input) [B, C] of each sequence; state float32 [B, C] is updated in place."""
+    import torch
+
+    t, (B, C), args = _gates(x, forget, input, 2)
+    device = x.device
+    if stream is not None and (done := _under(stream, device, lambda: nna_gated_scan_step(x, forget, state, input, out))) is not None:
+        return done
+    sp, given = _vector(state, "state", (B, C), device), out
+    if out is None:
+        out = x.new_empty((B, C))
+    elif not (isinstance(out, torch.Tensor) and out.dtype == x.dtype and out.is_contiguous() and out.shape == x.shape and out.device == device):
+        raise TypeError(f"out must be a contiguous {x.dtype} tensor of shape {(B, C)}")
+    else:
+        _refuse_overlap(out, x, forget, input, state)
+    for g in (x, forget, input):
+        if g is not None and g.dtype == torch.float32 and _overlap(state, g):
+            raise ValueError("state must not share memory with an input")
+    _check(lib().nna_gated_scan_step(*args, t, B, C, sp, out.data_ptr(), device.index, _stream_on(device, stream)))
+    _written(state, given)
+    return out
+
+
+_ADAMW_TABLE = np.dtype([("p", np.uint64), ("g", np.uint64), ("n", np.int64), ("at", np.int64), ("type", np.int32), ("reserved", np.int32)])
+
+
+def nna_adamw_places(sizes):
+    """(where each tensor's states begin, values of all of them together): multiples of 128, in the tensors' order, for tensors of `sizes` values."""
+    at = np.zeros(len(sizes) + 1, np.int64)
+    np.cumsum([-(-int(n) // NNA_BLOCK8) * NNA_BLOCK8 for n in sizes], out=at[1:])
+    return at[:-1], int(at[-1])
+
+
+def nna_adamw(params, grads, m, v, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, m_scales=None, v_scales=None, master=None, stream=None):
+    """One AdamW step over all of `params`, in place: lists of contiguous float32, bfloat16 or float16 CUDA tensors and their gradients, of their types (None: that tensor and its
+    states are left alone).  m, v: the moments, flat, a tensor's beginning at nna_adamw_places' multiple of 128: float32, or int8 (m) and uint8 (v) codes with float32
+    m_scales, v_scales [values / 128]; zeros before the first step.  master: flat float32 copies of the 16-bit tensors, likewise, which are updated and rounded from.
+    step: the step's number, from 1; step and lr may be CUDA tensors of one value, int64 and float32, read when the step runs (so that a graph can record it)."""
+    import torch
+
+    tensor, f32 = torch.Tensor, torch.float32
+    if not _types:
+        _types.update({torch.float32: (NNA_F32, "float32"), torch.bfloat16: (NNA_BF16, "bfloat16"), torch.float16: (NNA_F16, "float16")})
+    params, grads = list(params), list(grads)
+    if len(params) != len(grads):
+        raise ValueError("params and grads must be as many")
+    if not (isinstance(m, tensor) and m.is_cuda):
+        raise TypeError("m must be a CUDA tensor")
+    device = m.device
+    for p, g in zip(params, grads):
+        if not (isinstance(p, tensor) and p.device == device and p.dtype in _types and p.is_contiguous()):
+            raise TypeError(f"params must be contiguous tensors of float32, bfloat16 or float16 on {device}")
+        if g is not None and not (isinstance(g, tensor) and g.dtype == p.dtype and g.device == device and g.shape == p.shape and g.layout == p.layout and g.is_contiguous()):
+            raise TypeError("a gradient must be a contiguous tensor of its parameter's type and shape, on its device")
+    sizes = [p.numel() for p in params]
+    at, size = nna_adamw_places(sizes)
+    codes = m_scales is not None or v_scales is not None
+    for name, t, dtype, n in (("m", m, torch.int8 if codes else f32, size), ("v", v, torch.uint8 if codes else f32, size),
+                              ("m_scales", m_scales, f32, size // NNA_BLOCK8), ("v_scales", v_scales, f32, size // NNA_BLOCK8), ("master", master, f32, size)):
+        if t is None and (name == "master" or (name.endswith("scales") and not codes)):
+            continue
+        if not (isinstance(t, tensor) and t.dtype == dtype and t.device == device and t.is_contiguous() and t.numel() == n):
+            raise TypeError(f"{name} must be a contiguous {dtype} tensor of {n} values on {device}")
+    step_p = lr_p = None
+    if isinstance(step, tensor):
+        if not (step.dtype == torch.int64 and step.device == device and step.numel() == 1):
+            raise TypeError(f"step must be a whole number, or one int64 value on {device}")
+        step_p, step = step.data_ptr(), 0
+    if isinstance(lr, tensor):
+        if not (lr.dtype == f32 and lr.device == device and lr.numel() == 1):
+            raise TypeError(f"lr must be a number, or one float32 value on {device}")
+        lr_p, lr = lr.data_ptr(), 0.0
+    table = np.zeros(len(params), _ADAMW_TABLE)
+    table["p"] = [p.data_ptr() for p in params]
+    table["g"] = [0 if g is None else g.data_ptr() for g in grads]
+    table["n"] = [0 if g is None else n for g, n in zip(grads, sizes)]
+    table["at"] = at
+    table["type"] = [_types[p.dtype][0] for p in params]
+    _check(lib().nna_adamw(table.ctypes.data, len(params), m.data_ptr(), v.data_ptr(), *(None if t is None else t.data_ptr() for t in (m_scales, v_scales, master)), size,
+                           int(step), step_p, float(lr), lr_p, float(betas[0]), float(betas[1]), float(eps), float(weight_decay), device.index,
+                           _stream_on(device, stream)))
+    _written(*(p for p, g in zip(params, grads) if g is not None), m, v, m_scales, v_scales, master)
+
+
+def nna_adamw_moment(codes, scales, out=None, stream=None):
+    """The float32 values that nna_adamw's 8-bit moments stand for: codes int8 (m) or uint8 (v), flat."""
+    import torch
+
+    if not (isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dtype in (torch.int8, torch.uint8) and codes.is_contiguous() and codes.numel() % NNA_BLOCK8 == 0):
+        raise TypeError("codes must be a contiguous int8 or uint8 CUDA tensor of blocks of 128")
+    if stream is not None and (done := _under(stream, codes.device, lambda: nna_adamw_moment(codes, scales, out))) is not None:
+        return done
+    sp, given = _vector(scales, "scales", (codes.numel() // NNA_BLOCK8,), codes.device), out
+    if out is None:
+        out = torch.empty_like(codes, dtype=torch.float32)
+    elif not (isinstance(out, torch.Tensor) and out.dtype == torch.float32 and out.is_contiguous() and out.shape == codes.shape and out.device == codes.device):
+        raise TypeError(f"out must be a contiguous float32 CUDA tensor of shape {tuple(codes.shape)}")
+    else:
+        _refuse_overlap(out, codes, scales)
+    _check(lib().nna_adamw_moment(codes.data_ptr(), codes.dtype == torch.uint8, sp, codes.numel(), out.data_ptr(), codes.device.index, _stream_on(codes.device, stream)))
+    if given is not None:
+        _written(given)
     return out

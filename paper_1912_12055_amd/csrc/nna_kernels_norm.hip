@@ -668,6 +668,11 @@ int norm_backward_groups(long long rows, int width, bool frames, long long batch
   return (int)std::max(1LL, std::min(n, MAX_GROUPS));
 }
 
+hipError_t launch_norm_join(const float* partial, int groups, int width, float* gw, float* gb, hipStream_t stream) {
+  hipLaunchKernelGGL(norm_join_kernel, dim3((2 * width + JOIN_COLUMNS - 1) / JOIN_COLUMNS), dim3(JOIN_COLUMNS * JOIN_RUNS), 0, stream, partial, groups, width, gw, gb);
+  return hipGetLastError();
+}
+
 hipError_t launch_norm(const NormParams& P, int x_type, int y_type, bool frames, hipStream_t stream) {
   if (frames)
     return by_type(y_type, [&](auto y) {
@@ -724,8 +729,7 @@ hipError_t launch_norm_backward(const NormParams& P, int x_type, int g_type, boo
       });
     });
   if (e != hipSuccess || !P.partial) return e;
-  hipLaunchKernelGGL(norm_join_kernel, dim3((2 * P.width + JOIN_COLUMNS - 1) / JOIN_COLUMNS), dim3(JOIN_COLUMNS * JOIN_RUNS), 0, stream, P.partial, grid, P.width, gw, gb);
-  return hipGetLastError();
+  return launch_norm_join(P.partial, grid, P.width, gw, gb, stream);
 }
 
 // rows whose blocks follow one another without a gap are one row: the kernel's quotients are then none

@@ -33,6 +33,8 @@ hipError_t norm_kernels_init();  // per device, before the first launch
 int norm_backward_groups(long long rows, int width, bool frames, long long batch, long long T);
 hipError_t launch_norm(const NormParams& P, int x_type, int y_type, bool frames, hipStream_t stream);
 hipError_t launch_norm_backward(const NormParams& P, int x_type, int g_type, bool frames, float* gw, float* gb, hipStream_t stream);
+// gw, gb [width] (or NULL): the sums over `groups` of partial[groups][2][width], in a fixed order
+hipError_t launch_norm_join(const float* partial, int groups, int width, float* gw, float* gb, hipStream_t stream);
 hipError_t launch_pack8(const void* x, int type, long long rows, long long width, long long row_stride, signed char* codes, float* scales, hipStream_t stream);
 hipError_t launch_unpack8(const signed char* codes, const float* scales, long long rows, long long width, void* out, int type, hipStream_t stream);
 

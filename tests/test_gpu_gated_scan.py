@@ -1,0 +1,316 @@
+"""The gated recurrence against its definition in 64 bits (frame by frame), forward, backward and one frame at a time.
+
+Tolerances.  The definition's sums with every term's magnitude in its place give M >= |value|.  A gate is off by at most 6 half units of 2^-24 (the exponential 3, its sum, the reciprocal and
+the product 1 each), a frame's step rounds three times more, and a gate's error meets the state once in a frame: over T frames (and the exchange of a round's eight runs,
+which is one more step for each) at most 10 (T + 10) 2^-24 M, twice that for gradients, where the states' and the gradients' own errors meet.  A 16-bit result is rounded
+once more, by half a step of its value (fp16: of its smallest normal value below that).  float32 has no normal value below 2^-126: a gate or a product there may be zero, which is
+off by 2^-126 of what it meets.
+"""
+import sys
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0**-24
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def nb():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU (there is no CPU fallback)")
+    from paper_1912_12055_amd import binding
+    binding.lib()
+    return binding
+
+
+def _say(*a):
+    print("[case]", *a, file=sys.stderr, flush=True)
+
+
+def inputs(B, T, C, dtype, gated, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+
+    def normal(*s):
+        return torch.randn(*s, device=DEV, generator=g)
+
+    x, go = normal(B, T, C).to(dtype), normal(B, T, C).to(dtype)
+    f = (normal(B, T, C) + 6 * torch.rand(C, device=DEV, generator=g)).to(dtype)
+    i = normal(B, T, C).to(dtype) if gated else None
+    return x, f, i, go, normal(B, C), normal(B, C)
+
+
+def exact(x, f, i, go=None, first=None, glast=None, lengths=None):
+    """{name: (value, magnitude)} in 64 bits on the CPU"""
+    B, T, C = x.shape
+    x, f, go, first, glast, i = (None if t is None else t.double().cpu() for t in (x, f, go, first, glast, i))
+    n = torch.tensor([T] * B if lengths is None else [min(max(int(v), 0), T) for v in lengths])
+    zero = torch.zeros(B, C, dtype=torch.float64)
+    a, u = torch.sigmoid(f), torch.sigmoid(-f if i is None else i)
+    na, nu = torch.sigmoid(-f), torch.sigmoid(f if i is None else -i)
+    out = {}
+    values, sizes = [], []
+    for to, fn in ((values, lambda v: v), (sizes, torch.abs)):
+        h = fn(first) if first is not None else zero
+        hs, before = torch.zeros(B, T, C, dtype=torch.float64), torch.zeros(B, T, C, dtype=torch.float64)
+        for t in range(T):
+            here = (t < n)[:, None]
+            before[:, t] = h
+            h = torch.where(here, a[:, t] * h + u[:, t] * fn(x[:, t]), h)
+            hs[:, t] = torch.where(here, h, 0)
+        to += [hs, h, before]
+    out["h"], out["last"] = (values[0], sizes[0]), (values[1], sizes[1])
+    if go is None:
+        return out
+    grads = []
+    for fn, before, sign in ((lambda v: v, values[2], -1), (torch.abs, sizes[2], 1)):
+        e = fn(glast) if glast is not None else zero
+        gx, gf, gi = (torch.zeros(B, T, C, dtype=torch.float64) for _ in range(3))
+        for t in reversed(range(T)):
+            here = (t < n)[:, None]
+            e = torch.where(here, e + fn(go[:, t]), e)
+            gx[:, t] = torch.where(here, u[:, t] * e, 0)
+            gf[:, t] = torch.where(here, a[:, t] * na[:, t] * e * (before[:, t] + (sign * fn(x[:, t]) if i is None else 0)), 0)
+            gi[:, t] = torch.where(here, u[:, t] * nu[:, t] * e * fn(x[:, t]), 0)
+            e = torch.where(here, a[:, t] * e, e)
+        grads.append(dict(gx=gx, gf=gf, gi=gi, gfirst=e))
+    return out | {name: (grads[0][name], grads[1][name]) for name in grads[0]}
+
+
+def near(name, got, want, T, times=1):
+    value, size = want
+    got = got.cpu()
+    tolerance = times * 10 * (T + 10) * (U * size + 2.0**-126 * (1 + (float(size.max()) if size.numel() else 0.0)))
+    if got.dtype != torch.float32:
+        least = torch.finfo(got.dtype).tiny
+        tolerance = tolerance + torch.finfo(got.dtype).eps / 2 * torch.clamp(value.abs() + tolerance, min=least)
+    off = (got.double() - value).abs()
+    worst = float((off / tolerance.clamp(min=1e-300)).max()) if off.numel() else 0.0
+    assert worst <= 1, (name, worst)
+
+
+def check(nb, x, f, i, go, first, glast, lengths=None):
+    B, T, C = x.shape
+    want = exact(x, f, i, go, first, glast, lengths)
+    h, last, kept = nb.nna_gated_scan(x, f, i, state=first, lengths=lengths, want_state=True, keep=True)
+    near("h", h, want["h"], T)
+    near("last", last, want["last"], T)
+    gx, gf, gi, gfirst = nb.nna_gated_scan_backward(go, kept, x, f, i, lengths=lengths, gstate=glast, want_gstate=True)
+    near("gx", gx, want["gx"], T, 2)
+    near("gf", gf, want["gf"], T, 2)
+    near("gfirst", gfirst, want["gfirst"], T, 2)
+    if i is not None:
+        near("gi", gi, want["gi"], T, 2)
+    else:
+        assert gi is None
+    return h, last, kept, gx, gf, gi, gfirst
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("B,T,C", [(1, 1, 1), (2, 1, 130), (3, 2, 2), (1, 7, 3), (2, 63, 64), (1, 64, 65), (2, 65, 127), (1, 130, 129), (3, 200, 257), (1, 129, 40), (2, 5, 1)])
+def test_sizes(nb, B, T, C, gated, dtype):
+    _say(B, T, C, gated, dtype)
+    x, f, i, go, first, glast = inputs(B, T, C, dtype, gated, seed=T * 1000 + C)
+    check(nb, x, f, i, go, first, glast)
+    if T > 1:
+        check(nb, x, f, i, go, None, None)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gated", [False, True])
+def test_lengths(nb, gated, dtype):
+    """Frames behind a length take no part, whatever is there; lengths of zero, below it, and above T."""
+    lengths = torch.tensor([0, 1, 64, 65, 150, 200, -3, 63], dtype=torch.int32, device=DEV)
+    x, f, i, go, first, glast = inputs(8, 150, 70, dtype, gated, seed=3)
+    want = check(nb, x, f, i, go, first, glast, lengths)
+    behind = torch.arange(150, device=DEV)[:, None] >= lengths[:, None, None]
+    for value in (float("nan"), float("inf"), torch.finfo(dtype).min):
+        spoilt = [None if t is None else torch.where(behind, value, t).to(dtype) for t in (x, f, i, go)]
+        h, last, kept = nb.nna_gated_scan(*spoilt[:3], state=first, lengths=lengths, want_state=True, keep=True)
+        got = (h, last, None, *nb.nna_gated_scan_backward(spoilt[3], kept, *spoilt[:3], lengths=lengths, gstate=glast, want_gstate=True))
+        for w, o in zip(want, got):
+            assert o is None or torch.equal(w, o)
+    assert torch.equal(want[1][[0, 6]], first[[0, 6]]) and torch.equal(want[6][[0, 6]], glast[[0, 6]])
+
+
+@pytest.mark.parametrize("B,T,C", [(1, 3000, 96), (2, 1100, 33), (1, 8192, 16), (5, 700, 128)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_long(nb, B, T, C, gated):
+    """Sequences that are cut into segments, with lengths that end anywhere in them."""
+    _say(B, T, C, gated)
+    for dtype in (torch.float32, torch.bfloat16):
+        x, f, i, go, first, glast = inputs(B, T, C, dtype, gated, seed=C)
+        check(nb, x, f, i, go, first, glast)
+        lengths = torch.tensor([(T * 7 // 10 + 331 * b) % (T + 1) for b in range(B)], dtype=torch.int32, device=DEV)
+        check(nb, x, f, i, go, first, glast, lengths)
+
+
+def test_slow_channels_keep_their_decay(nb):
+    """Gates within 2^-13 of one over 20,000 frames of a constant: float32's own 1 - a would be off by thousandths.  Each frame's step is off by three half units of the
+    state, which the channel remembers for 1 / (1 - a) frames, and its gate by six of the input: at most 9 2^13 2^-24 if all had one sign; they have not, and as a walk that is 9 2^6.5 2^-24."""
+    f = torch.full((1, 20000, 64), 9.0, device=DEV) + torch.linspace(-1, 0, 64, device=DEV)
+    x = torch.ones_like(f)
+    got = nb.nna_gated_scan(x, f, want_state=True)[1].double().cpu()
+    a = torch.sigmoid(f[0, 0].double().cpu())
+    assert float(((got - (1 - a**20000)) / (1 - a**20000)).abs().max()) <= 9 * 2**13 * U
+    assert float(((got - (1 - a**20000)) / (1 - a**20000)).abs().median()) <= 9 * 2**6.5 * U
+
+
+def test_gates_at_their_ends(nb):
+    """Gates of +-infinity and far from zero are 0 and 1 exactly, or as near as float32 has them."""
+    f = torch.tensor([float("inf"), -float("inf"), 200.0, -200.0, 60.0, -60.0, 0.0, -0.0], device=DEV).repeat(1, 70, 1)
+    x = torch.randn(1, 70, 8, device=DEV)
+    go = torch.randn(1, 70, 8, device=DEV)
+    first = torch.randn(1, 8, device=DEV)
+    for i in (None, f.flip(-1).contiguous()):
+        check(nb, x, f, i, go, first, first)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_what_is_not_finite_stays_in_its_channel_and_behind_its_frame(nb, value):
+    x, f, _, go, first, _ = inputs(2, 300, 70, torch.float32, False, seed=5)
+    clean, last = nb.nna_gated_scan(x, f, state=first, want_state=True)
+    x[1, 100, 33] = value
+    h, spoilt = nb.nna_gated_scan(x, f, state=first, want_state=True)
+    touched = torch.zeros_like(h, dtype=torch.bool)
+    touched[1, 100:, 33] = True
+    assert not h[touched].isfinite().any() and torch.equal(h[~touched], clean[~touched])
+    assert not spoilt[1, 33].isfinite()
+    spoilt[1, 33] = last[1, 33]
+    assert torch.equal(spoilt, last)
+
+
+def test_strides(nb):
+    """Slices of one projection, transposed batches and frames, frames shared by all sequences, misaligned starts."""
+    B, T, C = 3, 150, 67
+    for dtype in TYPES:
+        both = torch.randn(B, T, 3 * C + 1, device=DEV).to(dtype)
+        x, f, i = both[..., 1 : C + 1], both[..., C + 1 : 2 * C + 1], both[..., 2 * C + 1 :]
+        go = torch.randn(B, T, C, device=DEV).to(dtype)
+        want = check(nb, *(t.contiguous() for t in (x, f, i)), go, None, None)
+        got = check(nb, x, f, i, go, None, None)
+        turned = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (x, f, i)]
+        again = check(nb, *turned, go, None, None)
+        for a, b, c in zip(want, got, again):
+            assert a is None or (torch.equal(a, b) and torch.equal(a, c))
+        shared = f[:1].expand(B, T, C)
+        check(nb, x, shared, i[:, :1].expand(B, T, C), go, None, None)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gated", [False, True])
+def test_steps_go_on_where_a_sequence_ends(nb, gated, dtype):
+    for B, C in ((1, 1), (3, 5), (2, 64), (7, 130), (1, 515)):
+        x, f, i, _, first, _ = inputs(B, 90, C, dtype, gated, seed=C)
+        want = exact(x, f, i, first=first)
+        state = nb.nna_gated_scan(x[:, :80], f[:, :80], None if i is None else i[:, :80], state=first, want_state=True)[1]
+        for t in range(80, 90):
+            h = nb.nna_gated_scan_step(x[:, t], f[:, t], state, input=None if i is None else i[:, t])
+            near("step", h, (want["h"][0][:, t], want["h"][1][:, t]), t)
+        near("state", state, want["last"], 90)
+
+
+def test_gradients_against_differences(nb):
+    """The mean of both sides' differences in 64 bits of the definition, along random directions: off by h^2 / 6 of the third derivative (below 100 here: 2e-7) and 2^-20 of the terms."""
+    x, f, i, go, first, glast = inputs(2, 70, 10, torch.float32, True, seed=9)
+    _, _, kept = nb.nna_gated_scan(x, f, i, state=first, want_state=True, keep=True)
+    grads = nb.nna_gated_scan_backward(go, kept, x, f, i, gstate=glast, want_gstate=True)
+
+    def loss(x, f, i, first):
+        out = exact(x, f, i, first=first)
+        return float((out["h"][0] * go.double().cpu()).sum() + (out["last"][0] * glast.double().cpu()).sum())
+
+    leaves = [t.double() for t in (x, f, i, first)]
+    for k in range(4):
+        d = torch.randn_like(leaves[k])
+        up, down = ([t + s * 1e-4 * d if j == k else t for j, t in enumerate(leaves)] for s in (1, -1))
+        want = (loss(*up) - loss(*down)) / 2e-4
+        got = float((grads[k].double() * d).sum())
+        assert abs(got - want) <= 1e-5 * float((grads[k].double() * d).abs().sum()), k
+
+
+def test_empty(nb):
+    for B, T in ((0, 5), (2, 0), (0, 0)):
+        x = torch.empty(B, T, 6, device=DEV)
+        first = torch.randn(B, 6, device=DEV)
+        h, last, kept = nb.nna_gated_scan(x, x, state=first, want_state=True, keep=True)
+        assert h.shape == x.shape and torch.equal(last, first)
+        gx, gf, gi, gfirst = nb.nna_gated_scan_backward(x, kept, x, x, gstate=first, want_gstate=True)
+        assert gx.shape == x.shape and gi is None and torch.equal(gfirst, first)
+    state = torch.empty(0, 6, device=DEV)
+    assert nb.nna_gated_scan_step(torch.empty(0, 6, device=DEV), torch.empty(0, 6, device=DEV), state).shape == (0, 6)
+
+
+def test_refusals(nb):
+    x, f, i, go, first, _ = inputs(2, 10, 8, torch.float32, True)
+    _, kept = nb.nna_gated_scan(x, f, keep=True)
+    bad = [
+        lambda: nb.nna_gated_scan(x.cpu(), f), lambda: nb.nna_gated_scan(x, f.cpu()), lambda: nb.nna_gated_scan(x, f.bfloat16()), lambda: nb.nna_gated_scan(x, f[:, :9]),
+        lambda: nb.nna_gated_scan(x.double(), f.double()), lambda: nb.nna_gated_scan(x[0], f[0]), lambda: nb.nna_gated_scan(x, f, i[:1]),
+        lambda: nb.nna_gated_scan(x.transpose(1, 2), f.transpose(1, 2)), lambda: nb.nna_gated_scan(x, f, state=first.half()), lambda: nb.nna_gated_scan(x, f, state=first[0]),
+        lambda: nb.nna_gated_scan(x, f, lengths=torch.tensor([1, 2], device=DEV)), lambda: nb.nna_gated_scan(x, f, out=x), lambda: nb.nna_gated_scan(x, f, out=f),
+        lambda: nb.nna_gated_scan(x, f, out=torch.empty_like(x).half()), lambda: nb.nna_gated_scan_backward(go[:1], kept, x, f),
+        lambda: nb.nna_gated_scan_backward(go, kept[:1], x, f), lambda: nb.nna_gated_scan_backward(go.transpose(0, 1), kept, x, f),
+        lambda: nb.nna_gated_scan_step(x[:, 0], f[:, 0], first[:1]), lambda: nb.nna_gated_scan_step(x, f, first), lambda: nb.nna_gated_scan_step(first, f[:, 0], first),
+        lambda: nb.nna_gated_scan_step(x[:, 0], f[:, 0], first, out=first), lambda: nb.nna_gated_scan_step(x[:, 0], f[:, 0], first.bfloat16()),
+    ]
+    for k, call in enumerate(bad):
+        with pytest.raises((TypeError, ValueError, nb.NnaError)):
+            call()
+            pytest.fail(f"call {k} was not refused")
+
+
+def test_versions_count_up(nb):
+    x, f, _, _, first, _ = inputs(2, 10, 8, torch.float32, False)
+    out = torch.empty_like(x)
+    at = out._version, first._version
+    nb.nna_gated_scan(x, f, out=out)
+    nb.nna_gated_scan_step(x[:, 0], f[:, 0], first)
+    assert out._version > at[0] and first._version > at[1]
+
+
+def test_another_stream_and_a_graph(nb):
+    x, f, i, go, first, glast = inputs(2, 700, 96, torch.bfloat16, True, seed=2)
+    lengths = torch.tensor([700, 333], dtype=torch.int32, device=DEV)
+
+    def call():
+        h, last, kept = nb.nna_gated_scan(x, f, i, state=first, lengths=lengths, want_state=True, keep=True)
+        return (h, last, *nb.nna_gated_scan_backward(go, kept, x, f, i, lengths=lengths, gstate=glast, want_gstate=True))
+
+    want = call()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = nb.nna_gated_scan(x, f, i, state=first, lengths=lengths, want_state=True, keep=True, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for k in range(3):
+        x.copy_(torch.randn_like(x))
+        go.mul_(-1)
+        lengths.copy_(torch.tensor([650 - k, 64 * k], dtype=torch.int32))
+        graph.replay()
+        got = [t.clone() for t in out]
+        for a, b in zip(got, call()):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
+
+
+def test_far_apart(nb):
+    """Sequences whose elements' offsets pass 32 bits."""
+    B, T, C = 2, 70, 64
+    memory = torch.empty((1 << 32) + 8 * T * C, dtype=torch.bfloat16, device=DEV)
+    x = memory[: (1 << 32) + T * C].as_strided((B, T, C), (1 << 32, C, 1))
+    f = memory[T * C : (1 << 32) + 2 * T * C].as_strided((B, T, C), (1 << 32, C, 1))
+    vx, vf, _, go, _, _ = inputs(B, T, C, torch.bfloat16, False)
+    x.copy_(vx)
+    f.copy_(vf)
+    want, kept = nb.nna_gated_scan(vx, vf, keep=True)
+    got, kept2 = nb.nna_gated_scan(x, f, keep=True)
+    assert torch.equal(want, got)
+    for a, b in zip(nb.nna_gated_scan_backward(go, kept, vx, vf)[:2], nb.nna_gated_scan_backward(go, kept2, x, f)[:2]):
+        assert torch.equal(a, b)
