@@ -15,7 +15,7 @@ namespace nna {
 
 namespace {
 
-constexpr int WAVES = 8, FRAMES = SCAN_KEPT / WAVES, THREADS = WAVES * 64;
+constexpr int WAVES = 8, THREADS = WAVES * 64;
 
 // e^-|v|: the argument of the machine's 2^y rounded in two parts, since y's rounding alone is y 2^-24 of the result
 __device__ __forceinline__ float exp_down(float v) {
@@ -46,25 +46,26 @@ struct Stay {
   __device__ __forceinline__ float of(float h, float add) const { return __builtin_fmaf(a, h, __builtin_fmaf(rest, h, add)); }
 };
 
-// One wave's frames of a round, as they lie in memory.  Frames behind `count` are read from the last one that there is; they are masked later.
-template <typename T, int V>
+// A workgroup's lanes: CL neighbours along the channels, V channels each, 64 / CL runs of FRAMES frames in a wave, WAVES waves behind one another.
+template <int CL, int FRAMES>
+struct Shape {
+  static constexpr int RUNS = 64 / CL, WAVE = RUNS * FRAMES, ROUND = WAVES * WAVE;  // runs of a wave; frames of a wave, of a round
+  static constexpr int KEPT_WAVES = SCAN_KEPT / WAVE;                               // waves from one kept state to the next
+};
+
+// A lane's frames of a round, as they lie in memory
+template <typename T, int V, int FRAMES>
 struct Rows {
   typename Vec<T, V>::plain v[FRAMES];
-  __device__ __forceinline__ void load(const T* base, long long step, int t, int T_) {
+  // frames from t on; those behind the last one that there is are read from it, and masked later
+  template <bool FULL>
+  __device__ __forceinline__ void load(const T* base, long long step, int t, int last) {
+    const T* p = base + (FULL ? t : 0) * step;
 #pragma unroll
-    for (int k = 0; k < FRAMES; ++k) {
-      const int at = t + k < T_ ? t + k : T_ - 1;
-      v[k] = vec_load<V>(base + at * step);
-    }
+    for (int k = 0; k < FRAMES; ++k) v[k] = vec_load<V>(FULL ? p + k * step : base + (t + k < last ? t + k : last) * step);
   }
   __device__ __forceinline__ float at(int k, int c) const { return (float)vec_at<V>(v[k], c); }
 };
-
-template <int V>
-__device__ __forceinline__ void zero_rows(float* v) {
-#pragma unroll
-  for (int c = 0; c < V; ++c) v[c] = 0.f;
-}
 
 __device__ __forceinline__ int length_of(const int* lengths, long long b, int T) {
   if (!lengths) return T;
@@ -72,96 +73,182 @@ __device__ __forceinline__ int length_of(const int* lengths, long long b, int T)
   return n < 0 ? 0 : n < T ? n : T;
 }
 
-template <typename T, int V, bool INPUT>
-__global__ __launch_bounds__(THREADS) void scan_kernel(ScanParams P) {
-  __shared__ float2 sums[2][WAVES][V][64];
-  const int groups = (P.C + 64 * V - 1) / (64 * V);
-  const long long b = blockIdx.x / groups;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+// Which part of the work is a workgroup's.  Neighbouring channels' groups follow one another on one die (workgroups go round the eight of them), whose cache then serves both
+// halves of a line.
+struct Part {
+  long long b;
+  int segment, channel;
+  bool live;
+};
+template <int CL, int V>
+__device__ __forceinline__ Part part_of(const ScanParams& P) {
+  const int groups = (P.C + CL * V - 1) / (CL * V);
+  const unsigned all = gridDim.x, each = all / 8, id = blockIdx.x < each * 8 ? (blockIdx.x % 8) * each + blockIdx.x / 8 : blockIdx.x;
+  Part p;
+  const unsigned group = id % groups, rest = id / groups;
+  p.segment = (int)(rest % P.segments);
+  p.b = rest / P.segments;
   // lanes behind the last channel do its neighbours' work again and write nothing
-  const int mine = ((int)(blockIdx.x % groups) * 64 + lane) * V, channel = mine <= P.C - V ? mine : P.C - V;
-  const bool live = mine < P.C;
+  const int mine = ((int)group * CL + (int)(threadIdx.x % CL)) * V;
+  p.channel = mine <= P.C - V ? mine : P.C - V;
+  p.live = mine < P.C;
+  return p;
+}
+
+// In a wave: of (a, h) that make h = a h' + h of a run, those of all runs before this lane's (BEFORE) or behind it, and `all` of them together
+template <int CL, bool BEFORE>
+__device__ __forceinline__ void join_runs(float a, float h, float& a_to, float& h_to, float& a_all, float& h_all) {
+  if constexpr (CL == 64) {
+    a_to = 1.f, h_to = 0.f, a_all = a, h_all = h;
+  } else {
+    const int run = (threadIdx.x & 63) / CL;
+    constexpr int RUNS = 64 / CL;
+#pragma unroll
+    for (int d = 1; d < RUNS; d <<= 1) {
+      const float ao = BEFORE ? __shfl_up(a, d * CL) : __shfl_down(a, d * CL), ho = BEFORE ? __shfl_up(h, d * CL) : __shfl_down(h, d * CL);
+      if (BEFORE ? run >= d : run + d < RUNS) {
+        h = __builtin_fmaf(a, ho, h);
+        a *= ao;
+      }
+    }
+    const float ao = BEFORE ? __shfl_up(a, CL) : __shfl_down(a, CL), ho = BEFORE ? __shfl_up(h, CL) : __shfl_down(h, CL);
+    const bool none = BEFORE ? run == 0 : run == RUNS - 1;
+    a_to = none ? 1.f : ao;
+    h_to = none ? 0.f : ho;
+    a_all = a;  // (in the last run's lanes, or the first's)
+    h_all = h;
+  }
+}
+
+// Forward.  ENDS: no outputs, but what each segment makes of the state before it, P.parts[b][segment][a, h][C]; the mix composes those of the segments before its own.
+template <typename T, int V, int CL, int FRAMES, bool INPUT, bool ENDS>
+__global__ __launch_bounds__(THREADS) void scan_kernel(ScanParams P) {
+  typedef Shape<CL, FRAMES> S;
+  __shared__ float2 sums[2][WAVES][V][CL];
+  const Part part = part_of<CL, V>(P);
+  const long long b = part.b;
+  const int channel = part.channel, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = threadIdx.x % CL, run = (threadIdx.x & 63) / CL;
   const int n = length_of(P.lengths, b, P.T);
   const T* x = static_cast<const T*>(P.x) + b * P.x_b + channel;
   const T* f = static_cast<const T*>(P.f) + b * P.f_b + channel;
   const T* i = INPUT ? static_cast<const T*>(P.i) + b * P.i_b + channel : nullptr;
   T* out = static_cast<T*>(P.out) + b * P.T * P.C + channel;
-  float state[V];
+  const int begin = part.segment * P.segment_frames, end = begin + P.segment_frames < P.T ? begin + P.segment_frames : P.T;
+  const int used = n < end ? n : end;  // frames up to here are taken
+  const int kept_rows = (P.T + SCAN_KEPT - 1) / SCAN_KEPT;
+  float state[V], factor[V];
 #pragma unroll
-  for (int c = 0; c < V; ++c) state[c] = P.first ? P.first[b * P.C + channel + c] : 0.f;
-  const int rounds = (P.T + SCAN_KEPT - 1) / SCAN_KEPT, used = (n + SCAN_KEPT - 1) / SCAN_KEPT;
-  Rows<T, V> rx, rf, ri;
-  if (used) {
-    rx.load(x, P.x_t, wave * FRAMES, P.T);
-    rf.load(f, P.f_t, wave * FRAMES, P.T);
-    if (INPUT) ri.load(i, P.i_t, wave * FRAMES, P.T);
+  for (int c = 0; c < V; ++c) {
+    factor[c] = 1.f;
+    state[c] = !ENDS && P.first ? P.first[b * P.C + channel + c] : 0.f;
   }
-  for (int r = 0; r < used; ++r) {
-    const int t = r * SCAN_KEPT + wave * FRAMES;
-    float As[FRAMES][V], Hs[FRAMES][V], A[V], H[V];  // of the wave's frames up to each
+  if (!ENDS)
+    for (int s = 0; s < part.segment; ++s) {
+      const float* p = P.parts + (b * P.segments + s) * 2 * P.C + channel;
+#pragma unroll
+      for (int c = 0; c < V; ++c) state[c] = __builtin_fmaf(p[c], state[c], p[P.C + c]);
+    }
+  Rows<T, V, FRAMES> rx, rf, ri;
+  const auto load = [&](int t) {
+    if (t + S::ROUND <= P.T) {
+      const int at = t + wave * S::WAVE + run * FRAMES;
+      rx.template load<true>(x, P.x_t, at, 0);
+      rf.template load<true>(f, P.f_t, at, 0);
+      if (INPUT) ri.template load<true>(i, P.i_t, at, 0);
+    } else {
+      const int at = t + wave * S::WAVE + run * FRAMES;
+      rx.template load<false>(x, P.x_t, at, P.T - 1);
+      rf.template load<false>(f, P.f_t, at, P.T - 1);
+      if (INPUT) ri.template load<false>(i, P.i_t, at, P.T - 1);
+    }
+  };
+  const auto round = [&](int first, int turn, auto full) {
+    constexpr bool FULL = full.value;  // all frames of the round are taken
+    const int t = first + wave * S::WAVE + run * FRAMES;
+    float As[FRAMES][V], Hs[FRAMES][V], A[V], H[V];  // of the run's frames up to each
 #pragma unroll
     for (int c = 0; c < V; ++c) A[c] = 1.f, H[c] = 0.f;
 #pragma unroll
     for (int k = 0; k < FRAMES; ++k)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
+        const bool here = FULL || t + k < used;
         const Gate a = gate(rf.at(k, c));
         const float u = INPUT ? gate(ri.at(k, c)).on : a.off;
-        const Stay stay(a, t + k < n);
-        As[k][c] = A[c] = stay.of(A[c]);
-        Hs[k][c] = H[c] = stay.of(H[c], t + k < n ? u * rx.at(k, c) : 0.f);
+        const Stay stay(a, here);
+        A[c] = stay.of(A[c]);
+        H[c] = stay.of(H[c], here ? u * rx.at(k, c) : 0.f);
+        if (!ENDS) As[k][c] = A[c], Hs[k][c] = H[c];
       }
-    if (r + 1 < used) {
-      rx.load(x, P.x_t, t + SCAN_KEPT, P.T);
-      rf.load(f, P.f_t, t + SCAN_KEPT, P.T);
-      if (INPUT) ri.load(i, P.i_t, t + SCAN_KEPT, P.T);
-    }
+    if (first + S::ROUND < used) load(first + S::ROUND);
     // two buffers in turn: the next round's writes never meet a wave that still reads this one
+    float a_to[V], h_to[V];
 #pragma unroll
-    for (int c = 0; c < V; ++c) sums[r & 1][wave][c][lane] = make_float2(A[c], H[c]);
+    for (int c = 0; c < V; ++c) {
+      float a_all, h_all;
+      join_runs<CL, true>(A[c], H[c], a_to[c], h_to[c], a_all, h_all);
+      if (run == S::RUNS - 1) sums[turn][wave][c][column] = make_float2(a_all, h_all);
+    }
     __syncthreads();
-    if (P.kept && wave == 0 && live)
-#pragma unroll
-      for (int c = 0; c < V; ++c) P.kept[(b * rounds + r) * P.C + channel + c] = state[c];
     float h[V];
 #pragma unroll
     for (int w = 0; w < WAVES; ++w)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        if (w == wave) h[c] = state[c];
-        const float2 s = sums[r & 1][w][c][lane];
+        if (w == wave) h[c] = __builtin_fmaf(a_to[c], state[c], h_to[c]);
+        const float2 s = sums[turn][w][c][column];
         state[c] = __builtin_fmaf(s.x, state[c], s.y);
+        if (ENDS) factor[c] *= s.x;
       }
+    if (ENDS) return;
+    if (P.kept && t % SCAN_KEPT == 0 && t < used && part.live)
+#pragma unroll
+      for (int c = 0; c < V; ++c) P.kept[(b * kept_rows + t / SCAN_KEPT) * P.C + channel + c] = h[c];
 #pragma unroll
     for (int k = 0; k < FRAMES; ++k) {
       typename Vec<T, V>::plain o;
 #pragma unroll
       for (int c = 0; c < V; ++c) {
         const float now = __builtin_fmaf(As[k][c], h[c], Hs[k][c]);
-        vec_set<V>(o, c, (T)(t + k < n ? now : 0.f));
+        vec_set<V>(o, c, (T)(FULL || t + k < used ? now : 0.f));
       }
-      if (t + k < P.T && live) vec_store<V>(out + (long long)(t + k) * P.C, o);
+      if ((FULL || t + k < end) && part.live) vec_store<V>(out + (long long)(t + k) * P.C, o);
     }
+  };
+  if (begin < used) load(begin);
+  int turn = 0, t = begin;
+  for (; t < used; t += S::ROUND, turn ^= 1) {
+    if (t + S::ROUND <= used)
+      round(t, turn, std::true_type());
+    else
+      round(t, turn, std::false_type());
   }
-  if (live) {
-    if (P.last && wave == 0)
+  if (!part.live) return;
+  if (ENDS) {
+    if (threadIdx.x >= CL) return;
+    float* p = P.parts + (b * P.segments + part.segment) * 2 * P.C + channel;
 #pragma unroll
-      for (int c = 0; c < V; ++c) P.last[b * P.C + channel + c] = state[c];
-    typename Vec<T, V>::plain zero;
-#pragma unroll
-    for (int c = 0; c < V; ++c) vec_set<V>(zero, c, (T)0.f);
-    for (int t = used * SCAN_KEPT + wave; t < P.T; t += WAVES) vec_store<V>(out + (long long)t * P.C, zero);
+    for (int c = 0; c < V; ++c) p[c] = factor[c], p[P.C + c] = state[c];
+    return;
   }
+  if (P.last && part.segment == P.segments - 1 && threadIdx.x < CL)
+#pragma unroll
+    for (int c = 0; c < V; ++c) P.last[b * P.C + channel + c] = state[c];
+  typename Vec<T, V>::plain zero;
+#pragma unroll
+  for (int c = 0; c < V; ++c) vec_set<V>(zero, c, (T)0.f);
+  for (t += threadIdx.x / CL; t < end; t += THREADS / CL) vec_store<V>(out + (long long)t * P.C, zero);
 }
 
-template <typename T, int V, bool INPUT>
+// Backward, from the last frame to the first.  ENDS: what each segment makes of the carry behind it, P.parts[b][segment][a, e][C].
+template <typename T, int V, int CL, int FRAMES, bool INPUT, bool ENDS>
 __global__ __launch_bounds__(THREADS) void scan_backward_kernel(ScanParams P) {
-  __shared__ float sums[2][WAVES][3][V][64];
-  const int groups = (P.C + 64 * V - 1) / (64 * V);
-  const long long b = blockIdx.x / groups;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int mine = ((int)(blockIdx.x % groups) * 64 + lane) * V, channel = mine <= P.C - V ? mine : P.C - V;
-  const bool live = mine < P.C;
+  typedef Shape<CL, FRAMES> S;
+  __shared__ float2 sums[2][WAVES][V][CL];
+  __shared__ float carries[2][WAVES][V][CL];
+  const Part part = part_of<CL, V>(P);
+  const long long b = part.b;
+  const int channel = part.channel, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = threadIdx.x % CL, run = (threadIdx.x & 63) / CL;
   const int n = length_of(P.lengths, b, P.T);
   const T* x = static_cast<const T*>(P.x) + b * P.x_b + channel;
   const T* f = static_cast<const T*>(P.f) + b * P.f_b + channel;
@@ -169,54 +256,82 @@ __global__ __launch_bounds__(THREADS) void scan_backward_kernel(ScanParams P) {
   const long long packed = b * P.T * P.C + channel;
   const T* g = static_cast<const T*>(P.g) + packed;
   T *gx = static_cast<T*>(P.gx) + packed, *gf = static_cast<T*>(P.gf) + packed, *gi = INPUT ? static_cast<T*>(P.gi) + packed : nullptr;
-  float carry[V];  // a e of the frame behind
+  const int begin = part.segment * P.segment_frames, end = begin + P.segment_frames < P.T ? begin + P.segment_frames : P.T;
+  const int used = n < end ? n : end;
+  const int kept_rows = (P.T + SCAN_KEPT - 1) / SCAN_KEPT;
+  float carry[V], factor[V];  // a e of the frame behind
 #pragma unroll
-  for (int c = 0; c < V; ++c) carry[c] = P.glast ? P.glast[b * P.C + channel + c] : 0.f;
-  const int rounds = (P.T + SCAN_KEPT - 1) / SCAN_KEPT, used = (n + SCAN_KEPT - 1) / SCAN_KEPT;
-  if (live) {
+  for (int c = 0; c < V; ++c) {
+    factor[c] = 1.f;
+    carry[c] = !ENDS && P.glast ? P.glast[b * P.C + channel + c] : 0.f;
+  }
+  if (!ENDS)
+    for (int s = P.segments - 1; s > part.segment; --s) {
+      const float* p = P.parts + (b * P.segments + s) * 2 * P.C + channel;
+#pragma unroll
+      for (int c = 0; c < V; ++c) carry[c] = __builtin_fmaf(p[c], carry[c], p[P.C + c]);
+    }
+  const int rounds = used > begin ? (used - begin + S::ROUND - 1) / S::ROUND : 0;
+  if (!ENDS && part.live) {
     typename Vec<T, V>::plain zero;
 #pragma unroll
     for (int c = 0; c < V; ++c) vec_set<V>(zero, c, (T)0.f);
-    for (int t = used * SCAN_KEPT + wave; t < P.T; t += WAVES) {
+    for (int t = begin + rounds * S::ROUND + threadIdx.x / CL; t < end; t += THREADS / CL) {
       vec_store<V>(gx + (long long)t * P.C, zero);
       vec_store<V>(gf + (long long)t * P.C, zero);
       if (INPUT) vec_store<V>(gi + (long long)t * P.C, zero);
     }
   }
-  Rows<T, V> rx, rf, ri, rg;
-  if (used) {
-    const int t = (used - 1) * SCAN_KEPT + wave * FRAMES;
-    rx.load(x, P.x_t, t, P.T);
-    rf.load(f, P.f_t, t, P.T);
-    if (INPUT) ri.load(i, P.i_t, t, P.T);
-    rg.load(g, P.C, t, P.T);
-  }
-  for (int r = used - 1; r >= 0; --r) {
-    const int t = r * SCAN_KEPT + wave * FRAMES;
+  Rows<T, V, FRAMES> rx, rf, ri, rg;
+  const auto load = [&](int t) {
+    const int at = t + wave * S::WAVE + run * FRAMES;
+    if (t + S::ROUND <= P.T) {
+      rf.template load<true>(f, P.f_t, at, 0);
+      rg.template load<true>(g, P.C, at, 0);
+      if (!ENDS) rx.template load<true>(x, P.x_t, at, 0);
+      if (INPUT && !ENDS) ri.template load<true>(i, P.i_t, at, 0);
+    } else {
+      rf.template load<false>(f, P.f_t, at, P.T - 1);
+      rg.template load<false>(g, P.C, at, P.T - 1);
+      if (!ENDS) rx.template load<false>(x, P.x_t, at, P.T - 1);
+      if (INPUT && !ENDS) ri.template load<false>(i, P.i_t, at, P.T - 1);
+    }
+  };
+  const auto round = [&](int first, int turn, auto full) {
+    constexpr bool FULL = full.value;
+    const int t = first + wave * S::WAVE + run * FRAMES;
     Stay stay[FRAMES][V];
-    float slope[FRAMES][V], take[FRAMES][V], take_slope[FRAMES][V], in[FRAMES][V], go[FRAMES][V];
+    float off[FRAMES][V], take[FRAMES][V], take_slope[FRAMES][V], in[FRAMES][V], go[FRAMES][V], before[FRAMES][V];
     float A[V], H[V], E[V], h[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
       A[c] = 1.f, H[c] = 0.f, E[c] = 0.f;
-      h[c] = P.kept[(b * rounds + r) * P.C + channel + c];
+      if (!ENDS) {
+        const int row = (first + (wave - wave % S::KEPT_WAVES) * S::WAVE) / SCAN_KEPT;
+        h[c] = FULL || row < kept_rows ? P.kept[(b * kept_rows + row) * P.C + channel + c] : 0.f;
+      }
     }
 #pragma unroll
     for (int k = 0; k < FRAMES; ++k)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        const bool here = t + k < n;
+        const bool here = FULL || t + k < used;
         const Gate a = gate(rf.at(k, c));
         stay[k][c] = Stay(a, here);
-        slope[k][c] = here ? a.on * a.off : 0.f;
-        in[k][c] = here ? rx.at(k, c) : 0.f;
         go[k][c] = here ? rg.at(k, c) : 0.f;
+        if (ENDS) {
+          A[c] = stay[k][c].of(A[c]);
+          continue;
+        }
+        // (the slope a (1 - a) is made of these two where it is used)
+        off[k][c] = here ? a.off : 0.f;
+        in[k][c] = here ? rx.at(k, c) : 0.f;
         if (INPUT) {
           const Gate u = gate(ri.at(k, c));
           take[k][c] = here ? u.on : 0.f;
           take_slope[k][c] = here ? u.on * u.off : 0.f;
         } else {
-          take[k][c] = here ? a.off : 0.f;
+          take[k][c] = off[k][c];
         }
         A[c] = stay[k][c].of(A[c]);
         H[c] = stay[k][c].of(H[c], take[k][c] * in[k][c]);
@@ -224,36 +339,45 @@ __global__ __launch_bounds__(THREADS) void scan_backward_kernel(ScanParams P) {
 #pragma unroll
     for (int k = FRAMES - 1; k >= 0; --k)
 #pragma unroll
-      for (int c = 0; c < V; ++c) {
-        E[c] = stay[k][c].of(E[c] + go[k][c]);
-      }
-    if (r) {
-      rx.load(x, P.x_t, t - SCAN_KEPT, P.T);
-      rf.load(f, P.f_t, t - SCAN_KEPT, P.T);
-      if (INPUT) ri.load(i, P.i_t, t - SCAN_KEPT, P.T);
-      rg.load(g, P.C, t - SCAN_KEPT, P.T);
-    }
+      for (int c = 0; c < V; ++c) E[c] = stay[k][c].of(E[c] + go[k][c]);
+    if (first > begin) load(first - S::ROUND);
+    float a_to[V], h_to[V], a_from[V], e_from[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      sums[r & 1][wave][0][c][lane] = A[c];
-      sums[r & 1][wave][1][c][lane] = H[c];
-      sums[r & 1][wave][2][c][lane] = E[c];
+      float a_all, h_all, e_all;
+      if (!ENDS) {
+        join_runs<CL, true>(A[c], H[c], a_to[c], h_to[c], a_all, h_all);
+        if (run == S::RUNS - 1) sums[turn][wave][c][column] = make_float2(a_all, h_all);
+      }
+      join_runs<CL, false>(A[c], E[c], a_from[c], e_from[c], a_all, e_all);
+      if (run == 0) {
+        carries[turn][wave][c][column] = e_all;
+        if (ENDS) sums[turn][wave][c][column] = make_float2(a_all, 0.f);
+      }
     }
     __syncthreads();
     float e[V];
+    if (!ENDS)
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w)
-      if (w < wave)
+      for (int w = 0; w < WAVES; ++w)
+        if (w < wave && w >= wave - wave % S::KEPT_WAVES)
 #pragma unroll
-        for (int c = 0; c < V; ++c) h[c] = __builtin_fmaf(sums[r & 1][w][0][c][lane], h[c], sums[r & 1][w][1][c][lane]);
+          for (int c = 0; c < V; ++c) {
+            const float2 s = sums[turn][w][c][column];
+            h[c] = __builtin_fmaf(s.x, h[c], s.y);
+          }
 #pragma unroll
     for (int w = WAVES - 1; w >= 0; --w)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        if (w == wave) e[c] = carry[c];
-        carry[c] = __builtin_fmaf(sums[r & 1][w][0][c][lane], carry[c], sums[r & 1][w][2][c][lane]);
+        if (w == wave) e[c] = __builtin_fmaf(a_from[c], carry[c], e_from[c]);
+        const float a = sums[turn][w][c][column].x;
+        carry[c] = __builtin_fmaf(a, carry[c], carries[turn][w][c][column]);
+        if (ENDS) factor[c] *= a;
       }
-    float before[FRAMES][V];
+    if (ENDS) return;
+#pragma unroll
+    for (int c = 0; c < V; ++c) h[c] = __builtin_fmaf(a_to[c], h[c], h_to[c]);
 #pragma unroll
     for (int k = 0; k < FRAMES; ++k)
 #pragma unroll
@@ -267,21 +391,37 @@ __global__ __launch_bounds__(THREADS) void scan_backward_kernel(ScanParams P) {
 #pragma unroll
       for (int c = 0; c < V; ++c) {
         e[c] += go[k][c];
-        const bool here = t + k < n;
+        const bool here = FULL || t + k < used;
         vec_set<V>(ox, c, (T)(here ? take[k][c] * e[c] : 0.f));
-        vec_set<V>(of, c, (T)(here ? slope[k][c] * e[c] * (INPUT ? before[k][c] : before[k][c] - in[k][c]) : 0.f));
+        vec_set<V>(of, c, (T)(here ? stay[k][c].a * off[k][c] * e[c] * (INPUT ? before[k][c] : before[k][c] - in[k][c]) : 0.f));
         if (INPUT) vec_set<V>(oi, c, (T)(here ? take_slope[k][c] * e[c] * in[k][c] : 0.f));
         e[c] = stay[k][c].of(e[c]);
       }
-      if (t + k < P.T && live) {
+      if ((FULL || t + k < end) && part.live) {
         const long long at = (long long)(t + k) * P.C;
         vec_store<V>(gx + at, ox);
         vec_store<V>(gf + at, of);
         if (INPUT) vec_store<V>(gi + at, oi);
       }
     }
+  };
+  if (rounds) load(begin + (rounds - 1) * S::ROUND);
+  int turn = 0;
+  for (int r = rounds - 1; r >= 0; --r, turn ^= 1) {
+    const int t = begin + r * S::ROUND;
+    if (t + S::ROUND <= used)
+      round(t, turn, std::true_type());
+    else
+      round(t, turn, std::false_type());
   }
-  if (P.gfirst && live && wave == 0)
+  if (!part.live || threadIdx.x >= CL) return;
+  if (ENDS) {
+    float* p = P.parts + (b * P.segments + part.segment) * 2 * P.C + channel;
+#pragma unroll
+    for (int c = 0; c < V; ++c) p[c] = factor[c], p[P.C + c] = carry[c];
+    return;
+  }
+  if (P.gfirst && part.segment == 0)
 #pragma unroll
     for (int c = 0; c < V; ++c) P.gfirst[b * P.C + channel + c] = carry[c];
 }
@@ -325,6 +465,25 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStep P) {
   }
 }
 
+// How a call is cut up: whether a wave's lanes are 16 neighbouring channels' and four runs of frames, and segments.
+struct Cut {
+  bool runs;
+  int segments, frames;
+};
+constexpr int LANES_RUNS = 16, LANES_ONE = 64, LANES_BACK = 32;
+Cut cut_of(long long B, long long T, long long C, int channels /* of a lane */) {
+  Cut c;
+  c.runs = T > 128;
+  const int lanes = c.runs ? LANES_RUNS : LANES_ONE, round = c.runs ? 256 : 64;
+  const long long groups = B * ((C + lanes * channels - 1) / (lanes * channels)), rounds = (T + round - 1) / round;
+  const long long want = !c.runs || groups >= 192 ? 1 : std::min((512 + groups - 1) / groups, rounds);
+  const long long each = want > 1 ? (rounds + want - 1) / want : std::max(rounds, 1LL);
+  c.segments = (int)std::max(1LL, (rounds + each - 1) / each);
+  c.frames = (int)(each * round);
+  return c;
+}
+unsigned grid_of(const ScanParams& P, int lanes, int channels) { return (unsigned)(P.B * P.segments * ((P.C + lanes * channels - 1) / (lanes * channels))); }
+
 // channels of a lane: four bytes of them, where there are as many
 template <typename T, typename F>
 hipError_t by_lane(int C, F fn) {
@@ -333,37 +492,52 @@ hipError_t by_lane(int C, F fn) {
   return fn(std::integral_constant<int, 1>());
 }
 
-}  // namespace
-
-size_t scan_workspace(long long, long long, long long) { return 0; }
-
-hipError_t launch_scan(const ScanParams& P, int type, hipStream_t stream) {
+// fn(the type, channels of a lane, whether a wave has runs, whether there is a gate of the input's own)
+template <typename F>
+hipError_t by_cut(ScanParams& P, int type, F fn) {
   return by_element(type, [&](auto t) {
-    typedef decltype(t) T;
-    return by_lane<T>(P.C, [&](auto v) {
-      constexpr int V = v.value;
-      const unsigned grid = (unsigned)(P.B * ((P.C + 64 * V - 1) / (64 * V)));
-      if (P.i)
-        hipLaunchKernelGGL((scan_kernel<T, V, true>), dim3(grid), dim3(THREADS), 0, stream, P);
-      else
-        hipLaunchKernelGGL((scan_kernel<T, V, false>), dim3(grid), dim3(THREADS), 0, stream, P);
-      return hipGetLastError();
+    return by_lane<decltype(t)>(P.C, [&](auto v) {
+      const Cut c = cut_of(P.B, P.T, P.C, v.value);
+      P.segments = c.segments;
+      P.segment_frames = c.frames;
+      const auto gated = [&](auto runs) { return P.i ? fn(t, v, runs, std::true_type()) : fn(t, v, runs, std::false_type()); };
+      return c.runs ? gated(std::true_type()) : gated(std::false_type());
     });
   });
 }
 
-hipError_t launch_scan_backward(const ScanParams& P, int type, hipStream_t stream) {
-  return by_element(type, [&](auto t) {
+}  // namespace
+
+size_t scan_workspace(long long B, long long T, long long C) {
+  size_t most = 0;
+  for (int channels : {1, 2}) {
+    const Cut c = cut_of(B, T, C, channels);
+    if (c.segments > 1) most = std::max(most, (size_t)(B * c.segments * 2 * C) * sizeof(float));
+  }
+  return most;
+}
+
+hipError_t launch_scan(ScanParams P, int type, hipStream_t stream) {
+  return by_cut(P, type, [&](auto t, auto v, auto runs, auto gated) {
     typedef decltype(t) T;
-    return by_lane<T>(P.C, [&](auto v) {
-      constexpr int V = v.value;
-      const unsigned grid = (unsigned)(P.B * ((P.C + 64 * V - 1) / (64 * V)));
-      if (P.i)
-        hipLaunchKernelGGL((scan_backward_kernel<T, V, true>), dim3(grid), dim3(THREADS), 0, stream, P);
-      else
-        hipLaunchKernelGGL((scan_backward_kernel<T, V, false>), dim3(grid), dim3(THREADS), 0, stream, P);
-      return hipGetLastError();
-    });
+    constexpr int V = v.value, L = runs.value ? LANES_RUNS : LANES_ONE;
+    const unsigned grid = grid_of(P, L, V);
+    if constexpr (runs.value)
+      if (P.segments > 1) hipLaunchKernelGGL((scan_kernel<T, V, L, 8, gated.value, true>), dim3(grid), dim3(THREADS), 0, stream, P);
+    hipLaunchKernelGGL((scan_kernel<T, V, L, 8, gated.value, false>), dim3(grid), dim3(THREADS), 0, stream, P);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_scan_backward(ScanParams P, int type, hipStream_t stream) {
+  return by_cut(P, type, [&](auto t, auto v, auto runs, auto gated) {
+    typedef decltype(t) T;
+    constexpr int V = v.value, L = runs.value ? LANES_RUNS : LANES_BACK;
+    const unsigned grid = grid_of(P, L, V);
+    if constexpr (runs.value)
+      if (P.segments > 1) hipLaunchKernelGGL((scan_backward_kernel<T, V, L, 8, false, true>), dim3(grid), dim3(THREADS), 0, stream, P);
+    hipLaunchKernelGGL((scan_backward_kernel<T, V, L, 4, gated.value, false>), dim3(grid), dim3(THREADS), 0, stream, P);
+    return hipGetLastError();
   });
 }
 

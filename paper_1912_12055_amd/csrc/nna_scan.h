@@ -24,6 +24,7 @@ struct ScanParams {
   float* parts;                    // scan_workspace bytes
   long long B;
   int T, C;
+  int segments, segment_frames;    // the launch's
 };
 
 struct ScanStep {
@@ -37,8 +38,8 @@ struct ScanStep {
 
 // bytes of `parts`: none where a workgroup takes a sequence from its first frame to its last
 size_t scan_workspace(long long B, long long T, long long C);
-hipError_t launch_scan(const ScanParams& P, int type, hipStream_t stream);
-hipError_t launch_scan_backward(const ScanParams& P, int type, hipStream_t stream);
+hipError_t launch_scan(ScanParams P, int type, hipStream_t stream);
+hipError_t launch_scan_backward(ScanParams P, int type, hipStream_t stream);
 hipError_t launch_scan_step(const ScanStep& P, int type, hipStream_t stream);
 
 }  // namespace nna
