@@ -722,25 +722,20 @@ nna_status nna_gated_scan_step(const void* x_dev, long long x_stride, const void
 
 /*
  * One AdamW step over `count` tensors:  m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,  p <- (1 - lr wd) p - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps).
- *   tensors      [count] in host memory (read during the call): n values p_dev, updated, and their gradient g_dev, of `type`, contiguous; n may be 0.  Their states begin at value
- *                `at` of m and v: multiples of 128, in the tensors' order, without overlap.  No two tensors may share memory
- *   m_dev, v_dev [state_size] float32, m_scales_dev and v_scales_dev NULL; or int8 (m) and uint8 (v) codes with float32 scales [state_size / 128].  Zeros before the first step
+ *   p_dev, g_dev, n, types  [count] in host memory (read during the call): of each tensor its n values, updated, and their gradient (NULL: this tensor and its states are left alone), both
+ *                contiguous and of the nna_dtype types[i]; n may be 0.  A tensor's states are n values of m and v; the first tensor's begin at 0, the next one's at the multiple of 128
+ *                behind them, and so on.  No two tensors may share memory
+ *   m_dev, v_dev [state_size] float32 (state_size: where the tensor behind the last one's would begin), m_scales_dev and v_scales_dev NULL; or int8 (m) and uint8 (v) codes with float32 scales [state_size / 128].  Zeros before the first step
  *   master_dev   [state_size] float32 or NULL: the float32 copies that tensors of 16 bits are updated in and rounded from (float32 tensors have none)
  *   step_dev, lr_dev  NULL, or the step's number (from 1) and lr in device memory in the place of step and lr: for steps recorded into a graph
  * 8 bits: 128 neighbours share a scale s, their largest magnitude.  A code c of m stands for s (c / 127) |c / 127|, rounded to the nearest code; one of v for s (c / 255)^4, rounded
- * down from (255 (v / s)^(1/4) + d), at least 1 where v > 0, d in [0, 1) the fraction (first 24 bits) of (at + index) 0x9E3779B9 + t 0xB504F333 over 2^32.  The update itself
+ * down from (255 (v / s)^(1/4) + d), at least 1 where v > 0, d in [0, 1) the fraction (first 24 bits) of (place in v) 0x9E3779B9 + t 0xB504F333 over 2^32.  The update itself
  * uses the moments before they are rounded; they are float64 until then, each product and sum rounded by itself.  A block with a value that is not finite stands for NaN throughout; one below 2^-126 for zero.
  * nna_adamw_moment: out_dev [size] float32 = what the codes of m, or (second != 0) of v, stand for; size a multiple of 128.
  * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_SHAPE, NNA_ERR_ALLOC.  A value that is not finite reaches its own weight (8 bits: its block's).
  */
-typedef struct {
-  void* p_dev;
-  const void* g_dev;
-  long long n, at;
-  int type; /* nna_dtype */
-  int reserved;
-} nna_adamw_tensor;
-nna_status nna_adamw(const nna_adamw_tensor* tensors, long long count, void* m_dev, void* v_dev, float* m_scales_dev, float* v_scales_dev, float* master_dev,
+nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long long* n, const int* types, long long count, void* m_dev, void* v_dev, float* m_scales_dev,
+                     float* v_scales_dev, float* master_dev,
                      long long state_size, long long step, const long long* step_dev, double lr, const float* lr_dev, double beta1, double beta2, double eps,
                      double weight_decay, int device, void* hip_stream);
 nna_status nna_adamw_moment(const void* codes_dev, int second, const float* scales_dev, long long size, float* out_dev, int device, void* hip_stream);

@@ -197,6 +197,7 @@ __device__ __forceinline__ void update(const AdamwParams& P, const AdamwTensor& 
     for (int i = 0; i < EACH; ++i) {
       const float old = NARROW && P.master ? copy.v[i] : (float)vp.v[i];
       weight[i] = old * F.keep - F.rate * (m[i] / (sqrtf(v[i]) * F.root + P.eps));
+      asm("" : "+v"(weight[i]));  // a float32 from here on: the 16-bit weight is its float32 copy rounded, not the sum behind it
     }
     if (n) {
       store_some(p + at, n, weight);

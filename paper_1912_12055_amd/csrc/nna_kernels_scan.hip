@@ -475,7 +475,7 @@ Cut cut_of(long long B, long long T, long long C, int channels /* of a lane */) 
   Cut c;
   c.runs = T > 128;
   const int lanes = c.runs ? LANES_RUNS : LANES_ONE, round = c.runs ? 256 : 64;
-  const long long groups = B * ((C + lanes * channels - 1) / (lanes * channels)), rounds = (T + round - 1) / round;
+  const long long groups = std::max(1LL, B * ((C + lanes * channels - 1) / (lanes * channels))), rounds = (T + round - 1) / round;
   const long long want = !c.runs || groups >= 192 ? 1 : std::min((512 + groups - 1) / groups, rounds);
   const long long each = want > 1 ? (rounds + want - 1) / want : std::max(rounds, 1LL);
   c.segments = (int)std::max(1LL, (rounds + each - 1) / each);

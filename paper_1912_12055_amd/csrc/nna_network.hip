@@ -277,26 +277,24 @@ nna_status nna_gated_scan_step(const void* x_dev, long long x_stride, const void
   return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_gated_scan_step");
 }
 
-nna_status nna_adamw(const nna_adamw_tensor* tensors, long long count, void* m_dev, void* v_dev, float* m_scales_dev, float* v_scales_dev, float* master_dev,
-                     long long state_size, long long step, const long long* step_dev, double lr, const float* lr_dev, double beta1, double beta2, double eps,
-                     double weight_decay, int device, void* hip_stream) {
-  if (count < 0 || state_size < 0 || (count && !tensors)) return fail(NNA_ERR_INVALID_ARG, "count or state_size is negative, or tensors is NULL");
+nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long long* n, const int* types, long long count, void* m_dev, void* v_dev, float* m_scales_dev,
+                     float* v_scales_dev, float* master_dev, long long state_size, long long step, const long long* step_dev, double lr, const float* lr_dev, double beta1,
+                     double beta2, double eps, double weight_decay, int device, void* hip_stream) {
+  if (count < 0 || state_size < 0 || (count && (!p_dev || !g_dev || !n || !types))) return fail(NNA_ERR_INVALID_ARG, "count or state_size is negative, or an array is NULL");
   if (!m_scales_dev != !v_scales_dev) return fail(NNA_ERR_INVALID_ARG, "m_scales_dev and v_scales_dev come together");
   if (!step_dev && step < 1) return fail(NNA_ERR_INVALID_ARG, "step counts from 1");
   if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return fail(NNA_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
   if (!(eps >= 0.0) || eps > 3.0e38) return fail(NNA_ERR_INVALID_ARG, "eps must be finite and not negative");
   if ((!lr_dev && !(std::fabs(lr) < 1e30)) || !(std::fabs(weight_decay) < 1e30)) return fail(NNA_ERR_INVALID_ARG, "lr and weight_decay must be finite");
-  long long free_from = 0, values = 0;
+  long long size = 0, values = 0;
   for (long long i = 0; i < count; ++i) {
-    const nna_adamw_tensor& t = tensors[i];
-    if (!known_type(t.type)) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
-    if (t.n < 0 || t.n > (1LL << 36)) return fail(NNA_ERR_SHAPE, "a tensor's number of values is negative or too large");
-    if (!t.n) continue;
-    if (!t.p_dev || !t.g_dev || t.p_dev == t.g_dev) return fail(NNA_ERR_INVALID_ARG, "p_dev or g_dev is NULL, or they are the same");
-    if (t.at < free_from || t.at % ADAMW_BLOCK) return fail(NNA_ERR_INVALID_ARG, "states must begin at multiples of 128, one behind the other");
-    free_from = t.at + (t.n + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
-    if (free_from > state_size) return fail(NNA_ERR_INVALID_ARG, "a tensor's state ends behind state_size");
-    values += t.n;
+    if (!known_type(types[i])) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
+    if (n[i] < 0 || n[i] > (1LL << 36)) return fail(NNA_ERR_SHAPE, "a tensor's number of values is negative or too large");
+    size += (n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
+    if (size > state_size) return fail(NNA_ERR_INVALID_ARG, "a tensor's state ends behind state_size");
+    if (!n[i] || !g_dev[i]) continue;
+    if (!p_dev[i] || p_dev[i] == g_dev[i]) return fail(NNA_ERR_INVALID_ARG, "a tensor is NULL, or its own gradient");
+    values += n[i];
   }
   if (values && (!m_dev || !v_dev || m_dev == v_dev)) return fail(NNA_ERR_INVALID_ARG, "m_dev or v_dev is NULL, or they are the same");
   try {
@@ -304,8 +302,8 @@ nna_status nna_adamw(const nna_adamw_tensor* tensors, long long count, void* m_d
     std::vector<std::pair<uintptr_t, uintptr_t>> spans;
     spans.reserve((size_t)count);
     for (long long i = 0; i < count; ++i) {
-      const uintptr_t p = reinterpret_cast<uintptr_t>(tensors[i].p_dev);
-      if (tensors[i].n) spans.emplace_back(p, p + (uintptr_t)tensors[i].n * (tensors[i].type == NNA_F32 ? 4 : 2));
+      const uintptr_t p = reinterpret_cast<uintptr_t>(p_dev[i]);
+      if (n[i] && g_dev[i]) spans.emplace_back(p, p + (uintptr_t)n[i] * (types[i] == NNA_F32 ? 4 : 2));
     }
     if (!std::is_sorted(spans.begin(), spans.end())) std::sort(spans.begin(), spans.end());
     for (size_t i = 1; i < spans.size(); ++i)
@@ -332,20 +330,23 @@ nna_status nna_adamw(const nna_adamw_tensor* tensors, long long count, void* m_d
   P.eps = (float)eps;
   P.piece = adamw_piece(values);
   P.count = P.pieces = 0;
+  long long at = 0;
   for (long long i = 0; i < count; ++i) {
-    const nna_adamw_tensor& t = tensors[i];
-    if (t.n) {
-      P.tensors[P.count++] = {t.p_dev, t.g_dev, t.n, t.at, P.pieces, t.type};
-      P.pieces += (int)((t.n + P.piece - 1) / P.piece);
-    }
+    const long long pieces = g_dev[i] ? (n[i] + P.piece - 1) / P.piece : 0;
     // (threads of a launch are counted in 32 bits)
-    if (P.count && (P.count == ADAMW_TENSORS || i + 1 == count || P.pieces + (tensors[i + 1].n + P.piece - 1) / P.piece >= 1LL << 24)) {
+    if (P.count == ADAMW_TENSORS || (P.count && P.pieces + pieces >= 1LL << 24)) {
       const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));
       if (e != hipSuccess) return fail_hip(e, "nna_adamw");
       P.count = P.pieces = 0;
     }
+    if (pieces) {
+      P.tensors[P.count++] = {p_dev[i], g_dev[i], n[i], at, P.pieces, types[i]};
+      P.pieces += (int)pieces;
+    }
+    at += (n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
   }
-  return NNA_OK;
+  const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));  // (there is a tensor: some launch has been left to do)
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_adamw");
 }
 
 nna_status nna_adamw_moment(const void* codes_dev, int second, const float* scales_dev, long long size, float* out_dev, int device, void* hip_stream) {

@@ -2,7 +2,8 @@
 
 Tolerances, U = 2^-24.  A moment in 32 bits is two products and a sum of terms: 5 U of the sum of their magnitudes (the factor 1 - b is rounded too).  An update divides one by the
 root of the other: the quotient is off by 5 + 3 + 6 U of itself (first moment, half of the second's, root, product, sum, quotient, rate, its product); the weight, kept and
-summed, by 3 U more.  With g and m of either sign the first moment's own error counts by its terms, not by itself.  8-bit codes are equal: their borders are met in 64 bits here and there.
+summed, by 3 U more.  With g and m of either sign the first moment's own error counts by its terms, not by itself.  8-bit codes are equal: their borders are met in 64 bits here and there,
+and the moments before them are sums of the same products (g^2 first): b s + (1 - b) g is often halfway between two scales.
 """
 import math
 import sys
@@ -71,7 +72,7 @@ def near(name, got, value, tolerance):
 def expect(p, g, m, v, t, lr, betas, eps, weight_decay):
     """(p, m, v and the tolerances of a float32 form) in 64 bits; p, g, m, v of 64 bits"""
     b1, b2 = betas
-    m1, v1 = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    m1, v1 = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * (g * g)
     size = b1 * m.abs() + (1 - b1) * g.abs()
     root = (v1 / (1 - b2**t)).sqrt() + eps
     rate = lr / (1 - b1**t)
@@ -147,6 +148,7 @@ def packed(x, levels, power, shift):
 @pytest.mark.parametrize("dtypes", [(torch.float32,), (torch.bfloat16, torch.float32, torch.float16)])
 def test_8_bits(nb, dtypes):
     params, grads = tensors(dtypes, seed=1)
+    torch.manual_seed(1)
     s = states(nb, params, 8, master=True)
     places, _ = nb.nna_adamw_places([p.numel() for p in params])
     for t in (1, 2, 3, 4, 500):

@@ -34,10 +34,10 @@ def step(x=P, f=Q, state=S, out=R, type=F32, B=1, C=64):
     return nb.lib().nna_gated_scan_step(x, 64, f, 64, None, 0, type, B, C, state, out, -1, None)
 
 
-def adamw(rows=((P, Q, 100, 0, F32),), m=R, v=S, ms=None, vs=None, size=1 << 20, t=1, lr=1e-3, b1=0.9, b2=0.999, eps=1e-8, wd=0.0, count=None):
-    table = np.array([(*r, 0) for r in rows], nb._ADAMW_TABLE)
-    return nb.lib().nna_adamw(table.ctypes.data if len(rows) else None, len(rows) if count is None else count, m, v, ms, vs, None, size, t, None, lr, None, b1, b2, eps, wd, -1,
-                              None)
+def adamw(rows=((P, Q, 100, F32),), m=R, v=S, ms=None, vs=None, size=1 << 20, t=1, lr=1e-3, b1=0.9, b2=0.999, eps=1e-8, wd=0.0, count=None):
+    p, g, n, types = (np.array([r[k] for r in rows], dtype) for k, dtype in enumerate((np.uint64, np.uint64, np.int64, np.int32)))
+    return nb.lib().nna_adamw(*(a.ctypes.data if len(rows) else None for a in (p, g, n, types)), len(rows) if count is None else count, m, v, ms, vs, None, size, t, None, lr, None, b1,
+                              b2, eps, wd, -1, None)
 
 
 def moment(c=P, s=Q, n=256, out=R):
@@ -65,11 +65,11 @@ NAN, INF = float("nan"), float("inf")
     (lambda: step(x=None), ARG), (lambda: step(state=None), ARG), (lambda: step(out=None), ARG), (lambda: step(C=0), SHAPE), (lambda: step(type=4), ARG),
     (lambda: adamw(t=0), ARG), (lambda: adamw(b1=1.0), ARG), (lambda: adamw(b2=-0.1), ARG), (lambda: adamw(eps=NAN), ARG), (lambda: adamw(eps=INF), ARG), (lambda: adamw(lr=NAN), ARG),
     (lambda: adamw(wd=INF), ARG), (lambda: adamw(m=None), ARG), (lambda: adamw(v=None), ARG), (lambda: adamw(m=S), ARG), (lambda: adamw(ms=P), ARG), (lambda: adamw(vs=P), ARG),
-    (lambda: adamw(rows=()), ARG), (lambda: adamw(rows=(), count=1), ARG), (lambda: adamw(count=-1), ARG), (lambda: adamw(size=100), ARG), (lambda: adamw(size=-1), ARG),
-    (lambda: adamw(rows=[(0, Q, 100, 0, F32)]), ARG), (lambda: adamw(rows=[(P, 0, 100, 0, F32)]), ARG), (lambda: adamw(rows=[(P, P, 100, 0, F32)]), ARG),
-    (lambda: adamw(rows=[(P, Q, 100, 64, F32)]), ARG), (lambda: adamw(rows=[(P, Q, -1, 0, F32)]), SHAPE), (lambda: adamw(rows=[(P, Q, 1 << 40, 0, F32)]), SHAPE),
-    (lambda: adamw(rows=[(P, Q, 100, 0, 9)]), ARG), (lambda: adamw(rows=[(P, Q, 129, 0, F32), (R, S, 5, 128, F32)]), ARG),
-    (lambda: adamw(rows=[(P, Q, 100, 0, F32), (P + 396, S, 5, 128, F32)]), ARG), (lambda: adamw(rows=[(P + 200, Q, 100, 0, F32), (P, S, 101, 128, BF16)]), ARG),
+    (lambda: adamw(rows=(), count=1), ARG), (lambda: adamw(count=-1), ARG), (lambda: adamw(size=100), ARG), (lambda: adamw(size=-1), ARG),
+    (lambda: adamw(rows=[(0, Q, 100, F32)]), ARG), (lambda: adamw(rows=[(P, P, 100, F32)]), ARG), (lambda: adamw(rows=[(P, Q, -1, F32)]), SHAPE),
+    (lambda: adamw(rows=[(P, Q, 1 << 40, F32)]), SHAPE), (lambda: adamw(rows=[(P, Q, 100, 9)]), ARG), (lambda: adamw(rows=[(P, Q, 129, F32), (R, S, 5, F32)], size=256), ARG),
+    (lambda: adamw(rows=[(P, 0, 129, F32), (R, S, 5, F32)], size=256), ARG),
+    (lambda: adamw(rows=[(P, Q, 100, F32), (P + 396, S, 5, F32)]), ARG), (lambda: adamw(rows=[(P + 200, Q, 100, F32), (P, S, 101, BF16)]), ARG),
     (lambda: moment(c=None), ARG), (lambda: moment(s=None), ARG), (lambda: moment(out=None), ARG), (lambda: moment(n=100), SHAPE), (lambda: moment(n=-128), SHAPE),
 ])
 def test_refusals(call, status):
@@ -78,7 +78,8 @@ def test_refusals(call, status):
 
 
 @pytest.mark.parametrize("call", [rotate, rotate_back, scan, scan_back, step, adamw, moment, lambda: rotate(k=None, ks=None, kheads=0, yk=None), lambda: rotate(B=0, q=None),
-                                  lambda: adamw(rows=[(P, Q, 100, 0, F32), (P + 400, S, 5, 128, F32)]), lambda: adamw(rows=[(P + 202, Q, 100, 0, F32), (P, S, 101, 128, BF16)])])
+                                  lambda: adamw(rows=[(P, Q, 100, F32), (P + 400, S, 5, F32)]), lambda: adamw(rows=[(P + 202, Q, 100, F32), (P, S, 101, BF16)]),
+                                  lambda: adamw(rows=()), lambda: adamw(rows=[(0, 0, 100, F32), (P, S, 5, F32)], size=256), lambda: adamw(rows=[(P, 0, 100, F32), (P, S, 5, F32)])])
 def test_no_device(call):
     """Arguments that would do get as far as the device."""
     assert call() == ARG and "device" in nb.nna_last_error()
@@ -93,8 +94,9 @@ def test_memory():
     assert nb.lib().nna_rotate_heads_backward_workspace(1, 1, 64, None) == ARG
     assert nb.lib().nna_gated_scan_workspace(1, 1, 0, byref(n)) == SHAPE
     assert nb.lib().nna_gated_scan_workspace(1, 1, 8, None) == ARG
-    for B, T, C in ((0, 5000, 64), (1, 0, 64), (1, 1, 1), (1, 64, 512)):
+    for B, T, C in ((0, 5000, 64), (1, 0, 64), (1, 1, 1), (1, 64, 512), (64, 5000, 512)):
         assert nb.nna_gated_scan_workspace(B, T, C) == 0
+    assert nb.nna_gated_scan_workspace(2, 5000, 64) >= 2 * 2 * 2 * 64 * 4
 
 
 def test_where_states_begin():
