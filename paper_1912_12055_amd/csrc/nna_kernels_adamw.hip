@@ -8,8 +8,8 @@
 // moment, which ends at 2^-14 of its largest, is zero before it; and none that is not zero becomes zero.  A second moment changes by 1 - b2 of itself a step, far less than the
 // distance of its codes (1.6 % at the largest): rounded to the nearest it would stay where it is for good.  So it is rounded up or down by a number in [0, 1) that
 // goes with the value's place and the step, the fractions of an additive sequence, whose mean over the steps is 1/2: no state of a random generator, and the same inputs give the same bits.
-// The moments are made and their codes' borders met in 64 bits (additions and products there run at float32's rate): a code is then what the definition says, not
-// what an order of roundings makes of it.  (The largest code's value is the scale itself, and no product is fused into a sum: b1 s + (1 - b1) g is often halfway between two float32, and
+// The moments' codes and scales are what 64 bits make of them: a code is then what the definition says, not what an order of roundings makes of it.  Made in 64 bits throughout that
+// took 170 instructions a value, and 1,015 us for 201 million weights, half as long again as their bytes; now float32 does what it can tell, and 64 bits the few values near a border or a block's largest.  (The largest code's value is the scale itself, and no product is fused into a sum: b1 s + (1 - b1) g is often halfway between two float32, and
 // which of them is the next scale has to be one answer.)  The weights and the divisions are float32.
 #include "nna_adamw.h"
 #include "nna_vector.h"
@@ -54,44 +54,113 @@ __device__ __forceinline__ void store_some(T* p, int n, const S (&v)[EACH]) {
   }
 }
 
-// the largest of 16 neighbouring lanes' magnitudes; a NaN beats all
+// the largest of 16 neighbouring lanes' magnitudes, in all of them; a NaN beats all
 __device__ __forceinline__ float larger(float m, float o) { return o <= m || m != m ? m : o; }
+template <int N>
+__device__ __forceinline__ float rotated(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float most16(float m) {
-  for (int d = 1; d < 16; d <<= 1) m = larger(m, __shfl_xor(m, d));
-  return m;
+  m = larger(m, rotated<8>(m));
+  m = larger(m, rotated<4>(m));
+  m = larger(m, rotated<2>(m));
+  return larger(m, rotated<1>(m));
 }
 
 constexpr double FIRST = 127. * 127., SECOND = 255. * 255. * 255. * 255.;
 static_assert(FIRST * (1. / FIRST) == 1. && SECOND * (1. / SECOND) == 1., "the largest codes' values");
 __device__ __forceinline__ double first_value(int code, double scale) { return (double)(code * (code < 0 ? -code : code)) * (1. / FIRST) * scale; }
 __device__ __forceinline__ double second_value(unsigned code, double scale) { return (double)(code * code * code * code) * (1. / SECOND) * scale; }
-__device__ __forceinline__ double blend(double old, double b, double fresh, double n) {
+__device__ __forceinline__ double blend(double old, double b, double fresh) {
 #pragma clang fp contract(off)
-  return old * b + fresh * n;
+  return old * b + fresh * (1. - b);
 }
 
-// the code whose square is nearest to a = |m| (by its root) in units of the scale: a first guess in float32, its borders in 64 bits
-__device__ __forceinline__ int first_code(double m, double unit, float per_scale) {
-  const double a = __builtin_fabs(m);
-  float c = __builtin_rintf(127.f * __builtin_amdgcn_sqrtf((float)a * per_scale));
-  c = c < 127.f ? c : 127.f;
-  const double lower = (double)c - 0.5, upper = (double)c + 0.5;
-  if (c > 0.f && a < lower * lower * unit)
-    c -= 1.f;
-  else if (c < 127.f && a >= upper * upper * unit)
-    c += 1.f;
-  return m < 0. ? -(int)c : (int)c;
+// One moment of a lane's eight values in 8 bits: what was, and what is now, in float32 and in 64 bits, as the definition has it.
+constexpr float TINY = 0x1p-100f;  // below it products of float32 may have lost their last bits: everything is made in 64 then
+struct First {
+  Values<signed char> was;
+  float scale;
+  double beta;
+  __device__ __forceinline__ float now(int i, float g) const {
+    const float c = (float)was.v[i];
+    return c * __builtin_fabsf(c) * (scale * (float)(1. / FIRST)) * (float)beta + g * (float)(1. - beta);
+  }
+  __device__ __forceinline__ double exact(int i, float g) const { return blend(first_value(was.v[i], (double)scale), beta, (double)g); }
+  // what now() may be off by: five roundings of its terms.  The sum may be far smaller than they are; with the new scale s no term is larger than s + the old one's
+  __device__ __forceinline__ float off(float s) const { return s < TINY ? __builtin_inff() : 0x1p-21f * (s + 2.f * scale); }
+};
+struct Second {
+  Values<unsigned char> was;
+  float scale;
+  double beta;
+  __device__ __forceinline__ float now(int i, float g) const {
+    const float c = (float)was.v[i], s = c * c * (float)(1. / 65025.);
+    return s * s * scale * (float)beta + g * (g * (float)(1. - beta));
+  }
+  __device__ __forceinline__ double exact(int i, float g) const { return blend(second_value(was.v[i], (double)scale), beta, (double)g * (double)g); }
+  __device__ __forceinline__ float off(float s) const { return s < TINY ? __builtin_inff() : 0x1p-20f * s; }  // (a sum of positive terms)
+};
+
+// The scale of 16 lanes' block, the largest of the 64-bit moments rounded: only those that float32 can't tell from the largest are made in 64 bits.
+template <typename M>
+__device__ __forceinline__ float scale_of(const M& moment, const float (&now)[EACH], const Values<float>& g, int n) {
+  float most = 0.f, spoilt = 0.f;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const float a = i < n ? __builtin_fabsf(now[i]) : 0.f;
+    most = __builtin_fmaxf(most, a);
+    spoilt = __builtin_fmaf(a, 0.f, spoilt);  // NaN if one is not finite
+  }
+  most = most16(spoilt != spoilt ? spoilt : most);
+  const float near = most - 2.f * moment.off(most);
+  float exact = most != most ? most : 0.f;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i)
+    if (i < n && __builtin_fabsf(now[i]) >= near) exact = larger(exact, (float)__builtin_fabs(moment.exact(i, g.v[i])));
+  return most16(exact);
 }
-// the largest code that, `shift` (in [0, 1)) less, is no larger than v's fourth root in units of the scale
-__device__ __forceinline__ unsigned second_code(double v, double unit, float per_scale, float shift) {
-  float c = __builtin_floorf(255.f * __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf((float)v * per_scale)) + shift);
+
+// The code whose square is nearest to |m| (by its root) in units of the scale s.  float32's guess y is off by 127^2 / (2 y) of what m is (`per`: 127^2 off / s) and by five roundings of
+// itself; where a border is as near, or y so small that this does not say it, 64 bits decide.
+__device__ __forceinline__ int first_code(const First& moment, int i, float g, float now, float s, float per_scale, float per) {
+  float y = 127.f * __builtin_amdgcn_sqrtf(__builtin_fabsf(now) * per_scale), c = __builtin_rintf(y);
+  if (__builtin_expect(!((0.5f - __builtin_fabsf(y - c)) * y > per + y * 0x1p-13f || (y < 0.25f && per < 0.125f)), 0)) {
+    const double m = moment.exact(i, g), a = __builtin_fabs(m), unit = (double)s * (1. / FIRST);
+    c = __builtin_rintf(127.f * __builtin_amdgcn_sqrtf((float)a * per_scale));
+    const double lower = (double)c - 0.5, upper = (double)c + 0.5;
+    if (c > 0.f && a < lower * lower * unit)
+      c -= 1.f;
+    else if (a >= upper * upper * unit)
+      c += 1.f;
+    now = (float)m;
+  }
+  c = c < 127.f ? c : 127.f;
+  return (int)__builtin_copysignf(c, now);
+}
+// The largest code that, `shift` (in [0, 1)) less, is no larger than v's fourth root in units of the scale.  The root leaves a quarter of v's five roundings, and of the quotient's: y is off by 2^-14.
+__device__ __forceinline__ unsigned second_code(const Second& moment, int i, float g, float now, float s, float per_scale, float shift) {
+  const float y = 255.f * __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(now * per_scale)) + shift;
+  float c = __builtin_floorf(y);
+  const bool tiny = now < TINY && (g != 0.f || moment.was.v[i] != 0);
+  if (__builtin_expect(__builtin_fabsf(y - c - 0.5f) > 0.5f - 0x1p-12f || tiny, 0)) {
+    const double unit = (double)s * (1. / SECOND), v = moment.exact(i, g);
+    c = __builtin_floorf(255.f * __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf((float)v * per_scale)) + shift);
+    const double here = (double)c - (double)shift, next = here + 1.;
+    if (here > 0. && here * here * (here * here) * unit > v)
+      c -= 1.f;
+    else if (next * next * (next * next) * unit <= v)
+      c += 1.f;
+    now = v > 0. ? 1.f : 0.f;
+  }
   c = c < 255.f ? c : 255.f;
-  const double here = (double)c - (double)shift, next = here + 1.;
-  if (here > 0. && here * here * (here * here) * unit > v)
-    c -= 1.f;
-  else if (c < 255.f && next * next * (next * next) * unit <= v)
-    c += 1.f;
-  return v > 0. && c < 1.f ? 1u : (unsigned)c;
+  return now > 0.f && c < 1.f ? 1u : (unsigned)c;
+}
+
+// the root to one unit, of values that have no normal float32, too
+__device__ __forceinline__ float root_of(float v) {
+  const bool small = v < 0x1p-60f;
+  return __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? 0x1p-32f : 1.f);
 }
 
 struct Factors {
@@ -141,36 +210,27 @@ __device__ __forceinline__ void update(const AdamwParams& P, const AdamwTensor& 
     } else {
       signed char* const mc = static_cast<signed char*>(P.m) + state;
       unsigned char* const vc = static_cast<unsigned char*>(P.v) + state;
-      Values<signed char> om = {};
-      Values<unsigned char> ov = {};
-      double um = 0., uv = 0.;
       // (n is none for whole groups of 16 lanes, too, behind the tensor's last block: those have no scales)
       const long long block = state / ADAMW_BLOCK;
       const bool there = at - (threadIdx.x & 15) * EACH < end;
+      First first = {{}, 0.f, P.beta1};
+      Second second = {{}, 0.f, P.beta2};
+      Values<float> d;
       if (n) {
-        om = load_some(mc, n);
-        ov = load_some(vc, n);
+        first.was = load_some(mc, n);
+        second.was = load_some(vc, n);
       }
       if (there) {
-        um = (double)P.m_scales[block];
-        uv = (double)P.v_scales[block];
+        first.scale = P.m_scales[block];
+        second.scale = P.v_scales[block];
       }
-      double dm[EACH], dv[EACH];
-      float most_m = 0.f, most_v = 0.f;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
-        const double d = (double)(float)vg.v[i];
-        dm[i] = blend(first_value(om.v[i], um), P.beta1, d, 1. - P.beta1);
-        dv[i] = blend(second_value(ov.v[i], uv), P.beta2, d * d, 1. - P.beta2);
-        m[i] = (float)dm[i];
-        v[i] = (float)dv[i];
-        if (i < n) {
-          most_m = larger(most_m, __builtin_fabsf(m[i]));
-          most_v = larger(most_v, v[i]);
-        }
+        d.v[i] = (float)vg.v[i];
+        m[i] = first.now(i, d.v[i]);
+        v[i] = second.now(i, d.v[i]);
       }
-      most_m = most16(most_m);
-      most_v = most16(most_v);
+      const float most_m = scale_of(first, m, d, n), most_v = scale_of(second, v, d, n);
       // a block with a value that is not finite stands for NaN throughout, so that none is lost; one without a normal float32 is zero
       const bool some_m = most_m >= 0x1p-126f && most_m < __builtin_inff(), some_v = most_v >= 0x1p-126f && most_v < __builtin_inff();
       if (there && (threadIdx.x & 15) == 0) {
@@ -179,14 +239,12 @@ __device__ __forceinline__ void update(const AdamwParams& P, const AdamwTensor& 
       }
       signed char cm[EACH];
       unsigned char cv[EACH];
-      um = (double)most_m * (1. / FIRST);
-      uv = (double)most_v * (1. / SECOND);
-      const float rm = 1.f / most_m, rv = 1.f / most_v;
+      const float rm = 1.f / most_m, rv = 1.f / most_v, per = 127.f * 127.f * first.off(most_m) * rm;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
-        const unsigned place = (unsigned)(state + i) * 0x9E3779B9u + F.shift;
-        cm[i] = (signed char)(some_m ? first_code(dm[i], um, rm) : 0);
-        cv[i] = (unsigned char)(some_v ? second_code(dv[i], uv, rv, (float)(place >> 8) * 0x1p-24f) : 0);
+        const float shift = (float)(((unsigned)(state + i) * 0x9E3779B9u + F.shift) >> 8) * 0x1p-24f;
+        cm[i] = (signed char)(some_m ? first_code(first, i, d.v[i], m[i], most_m, rm, per) : 0);
+        cv[i] = (unsigned char)(some_v ? second_code(second, i, d.v[i], v[i], most_v, rv, shift) : 0);
       }
       if (n) {
         store_some(mc, n, cm);
@@ -196,7 +254,7 @@ __device__ __forceinline__ void update(const AdamwParams& P, const AdamwTensor& 
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const float old = NARROW && P.master ? copy.v[i] : (float)vp.v[i];
-      weight[i] = old * F.keep - F.rate * (m[i] / (sqrtf(v[i]) * F.root + P.eps));
+      weight[i] = old * F.keep - F.rate * (m[i] * __builtin_amdgcn_rcpf(root_of(v[i]) * F.root + P.eps));
       asm("" : "+v"(weight[i]));  // a float32 from here on: the 16-bit weight is its float32 copy rounded, not the sum behind it
     }
     if (n) {
@@ -240,7 +298,7 @@ __global__ __launch_bounds__(THREADS) void moment_kernel(const void* codes, cons
     const double scale = scales[at / (ADAMW_BLOCK / EACH)];
     float v[EACH];
     if constexpr (SECOND_ONE) {
-      const auto c = load_some(static_cast<const unsigned char*>(codes) + at * EACH, EACH);
+      const Values<unsigned char> c = load_some(static_cast<const unsigned char*>(codes) + at * EACH, EACH);
 #pragma unroll
       for (int i = 0; i < EACH; ++i) v[i] = (float)second_value(c.v[i], scale);
     } else {
@@ -266,7 +324,7 @@ hipError_t launch_adamw(const AdamwParams& P, hipStream_t stream) {
 }
 
 hipError_t launch_adamw_moment(const void* codes, bool second, const float* scales, long long blocks, float* out, hipStream_t stream) {
-  const unsigned grid = (unsigned)std::max(1LL, std::min((blocks * (ADAMW_BLOCK / EACH) + THREADS - 1) / THREADS, 8192LL));
+  const unsigned grid = (unsigned)std::max(1LL, std::min((blocks * (ADAMW_BLOCK / EACH) + THREADS - 1) / THREADS, 1LL << 22));
   if (second)
     hipLaunchKernelGGL(moment_kernel<true>, dim3(grid), dim3(THREADS), 0, stream, codes, scales, blocks, out);
   else

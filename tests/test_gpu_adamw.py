@@ -179,6 +179,33 @@ def test_8_bits(nb, dtypes):
         assert bool(((got - want).abs() <= 2 * U * want.abs() + 1e-45).all())
 
 
+@pytest.mark.parametrize("kind", ["cancel", "tiny", "same", "steep"])
+def test_8_bits_where_float32_says_little(nb, kind):
+    """Moments that cancel to 10^-4 of their terms (64 bits' own roundings are 10^-12 of what is left), gradients whose squares are below float32, blocks of one value, and values 2^-40 apart: the codes are those of 64 bits."""
+    torch.manual_seed(7)
+    p = torch.zeros(128 * 40, device=DEV)
+    s = states(nb, [p], 8)
+    g = torch.randn_like(p)
+    if kind == "same":
+        g = torch.randn(40, 1, device=DEV).expand(40, 128).flatten().contiguous()
+    if kind == "tiny":
+        g *= 10.0 ** -torch.linspace(10, 25, g.numel(), device=DEV).view(128, 40).t().flatten()
+    if kind == "steep":
+        g *= 2.0 ** -torch.randint(0, 40, g.shape, device=DEV)
+    for t in (1, 2, 3):
+        before = {k: x.clone() for k, x in s.items()}
+        om, ov = first_values(before["m"], before["m_scales"]), second_values(before["v"], before["v_scales"])
+        if kind == "cancel" and t > 1:
+            g = (-9 * om * (1 + 1e-4 * torch.randn_like(om))).float()
+        nb.nna_adamw([p], [g], step=t, **s, **HOW)
+        _, m1, v1, *_ = expect(p.double(), g.double(), om, ov, t, **HOW)
+        codes, scales = packed(m1.abs(), 127, 2, 0.5)
+        assert torch.equal(s["m_scales"], scales) and torch.equal(s["m"].double(), codes * m1.sign())
+        shift = (((torch.arange(p.numel(), device=DEV) * 0x9E3779B9 + t * 0xB504F333) & 0xFFFFFFFF) >> 8).double() * 2.0**-24
+        codes, scales = packed(v1, 255, 4, shift)
+        assert torch.equal(s["v_scales"], scales) and torch.equal(s["v"].double(), codes)
+
+
 def test_second_moments_in_8_bits_follow_their_decay(nb):
     """Rounded to the nearest, codes whose distance is wider than 1 - b2 would stay for good where the block's largest is fed anew.  After 200 steps without a gradient (0.82 of where it began) a
     value's code is still above 56: a rounding there is off by less than one code, 4 / 56 of the value.  Every step adds one, most of one sign cancelled by the sequence's next: five left over
