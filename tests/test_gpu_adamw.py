@@ -179,7 +179,7 @@ def test_8_bits(nb, dtypes):
         assert bool(((got - want).abs() <= 2 * U * want.abs() + 1e-45).all())
 
 
-@pytest.mark.parametrize("kind", ["cancel", "tiny", "same", "steep"])
+@pytest.mark.parametrize("kind", ["cancel", "tiny", "faint", "same", "steep"])
 def test_8_bits_where_float32_says_little(nb, kind):
     """Moments that cancel to 10^-4 of their terms (64 bits' own roundings are 10^-12 of what is left), gradients whose squares are below float32, blocks of one value, and values 2^-40 apart: the codes are those of 64 bits."""
     torch.manual_seed(7)
@@ -190,6 +190,8 @@ def test_8_bits_where_float32_says_little(nb, kind):
         g = torch.randn(40, 1, device=DEV).expand(40, 128).flatten().contiguous()
     if kind == "tiny":
         g *= 10.0 ** -torch.linspace(10, 25, g.numel(), device=DEV).view(128, 40).t().flatten()
+    if kind == "faint":
+        g *= 10.0 ** -torch.linspace(8, 22, 40, device=DEV).repeat_interleave(128)
     if kind == "steep":
         g *= 2.0 ** -torch.randint(0, 40, g.shape, device=DEV)
     for t in (1, 2, 3):
