@@ -17,21 +17,24 @@ namespace {
 
 constexpr int WAVES = 8, THREADS = WAVES * 64;
 
-// e^-|v|: the argument of the machine's 2^y rounded in two parts, since y's rounding alone is y 2^-24 of the result
-__device__ __forceinline__ float exp_down(float v) {
-  const float x = -__builtin_fabsf(v), y = x * 1.44269502f;
-  const float rest = __builtin_fmaf(x, 1.44269502f, -y) + x * 1.92596303e-8f;
-  const float e = __builtin_amdgcn_exp2f(y);
-  // (x is -inf: the rest is NaN and e zero)
-  return e > 0.f ? __builtin_fmaf(e * 0.693147182f, rest, e) : e;
-}
-// sigmoid(v) and sigmoid(-v), both to float32's own precision
+// sigmoid(v) and sigmoid(-v), each to float32's own precision of itself.  Of a float32 v the argument of the machine's 2^y is made in two parts, since y's rounding alone is y 2^-24 of the
+// result; a 16-bit v is itself off by far more.  (minimum and maximum let a NaN through.)
 struct Gate {
   float on, off;
 };
-__device__ __forceinline__ Gate gate(float v) {
-  const float e = exp_down(v), r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;
-  return v >= 0.f ? Gate{r, s} : Gate{s, r};
+template <typename T>
+__device__ __forceinline__ Gate gate(T v) {
+  float e;
+  if constexpr (sizeof(T) == 4) {
+    const float x = __builtin_elementwise_maximum(__builtin_elementwise_minimum(-v, 87.f), -104.f), y = x * 1.44269502f;
+    const float rest = __builtin_fmaf(x, 1.92596303e-8f, __builtin_fmaf(x, 1.44269502f, -y));
+    e = __builtin_amdgcn_exp2f(y);
+    e = __builtin_fmaf(e * 0.693147182f, rest, e);
+  } else {
+    e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum((float)v * -1.44269502f, 126.f));
+  }
+  const float r = __builtin_amdgcn_rcpf(1.f + e);
+  return {r, e * r};
 }
 
 // a as a float32 and what it leaves of it
@@ -64,7 +67,7 @@ struct Rows {
 #pragma unroll
     for (int k = 0; k < FRAMES; ++k) v[k] = vec_load<V>(FULL ? p + k * step : base + (t + k < last ? t + k : last) * step);
   }
-  __device__ __forceinline__ float at(int k, int c) const { return (float)vec_at<V>(v[k], c); }
+  __device__ __forceinline__ T at(int k, int c) const { return vec_at<V>(v[k], c); }
 };
 
 __device__ __forceinline__ int length_of(const int* lengths, long long b, int T) {
@@ -95,36 +98,87 @@ __device__ __forceinline__ Part part_of(const ScanParams& P) {
   return p;
 }
 
-// In a wave: of (a, h) that make h = a h' + h of a run, those of all runs before this lane's (BEFORE) or behind it, and `all` of them together
-template <int CL, bool BEFORE>
-__device__ __forceinline__ void join_runs(float a, float h, float& a_to, float& h_to, float& a_all, float& h_all) {
-  if constexpr (CL == 64) {
-    a_to = 1.f, h_to = 0.f, a_all = a, h_all = h;
-  } else {
-    const int run = (threadIdx.x & 63) / CL;
-    constexpr int RUNS = 64 / CL;
-#pragma unroll
-    for (int d = 1; d < RUNS; d <<= 1) {
-      const float ao = BEFORE ? __shfl_up(a, d * CL) : __shfl_down(a, d * CL), ho = BEFORE ? __shfl_up(h, d * CL) : __shfl_down(h, d * CL);
-      if (BEFORE ? run >= d : run + d < RUNS) {
-        h = __builtin_fmaf(a, ho, h);
-        a *= ao;
-      }
-    }
-    const float ao = BEFORE ? __shfl_up(a, CL) : __shfl_down(a, CL), ho = BEFORE ? __shfl_up(h, CL) : __shfl_down(h, CL);
-    const bool none = BEFORE ? run == 0 : run == RUNS - 1;
-    a_to = none ? 1.f : ao;
-    h_to = none ? 0.f : ho;
-    a_all = a;  // (in the last run's lanes, or the first's)
-    h_all = h;
-  }
+// A value of the lower and of the upper of two neighbouring runs, in all lanes of both: rows of 16 lanes, halves of the wave.
+struct Two {
+  float low, high;
+};
+__device__ __forceinline__ Two rows_of(float v) {
+  const auto p = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+  const unsigned a = p[0], b = p[1];
+  return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
 }
+__device__ __forceinline__ Two halves_of(float v) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+  const unsigned a = p[0], b = p[1];
+  return {__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+// A run makes h = a h' + h of the state before it, and c = a c' + e of the carry behind it.  In a wave: what the runs before this lane's make together (before_a, before_h), those behind
+// it (behind_a, behind_e), and all of them (all).
+template <int CL>
+struct Joined {
+  float before_a, before_h, behind_a, behind_e, all_a, all_h, all_e;
+  template <bool FORWARD, bool BACKWARD>
+  __device__ __forceinline__ void join(float a, float h, float e) {
+    before_a = behind_a = 1.f;
+    before_h = behind_e = 0.f;
+    all_a = a, all_h = h, all_e = e;
+    if constexpr (CL == 16) {
+      const bool odd = threadIdx.x & 16;
+      const Two A = rows_of(a);
+      if (FORWARD) {
+        const Two H = rows_of(h);
+        before_a = odd ? A.low : 1.f;
+        before_h = odd ? H.low : 0.f;
+        all_h = __builtin_fmaf(A.high, H.low, H.high);
+      }
+      if (BACKWARD) {
+        const Two E = rows_of(e);
+        behind_a = odd ? 1.f : A.high;
+        behind_e = odd ? 0.f : E.high;
+        all_e = __builtin_fmaf(A.low, E.high, E.low);
+      }
+      all_a = A.low * A.high;
+    }
+    if constexpr (CL <= 32) {
+      const bool upper = threadIdx.x & 32;
+      const Two A = halves_of(all_a);
+      if (FORWARD) {
+        const Two H = halves_of(all_h);
+        before_h = upper ? __builtin_fmaf(before_a, H.low, before_h) : before_h;
+        before_a = upper ? before_a * A.low : before_a;
+        all_h = __builtin_fmaf(A.high, H.low, H.high);
+      }
+      if (BACKWARD) {
+        const Two E = halves_of(all_e);
+        behind_e = upper ? behind_e : __builtin_fmaf(behind_a, E.high, behind_e);
+        behind_a = upper ? behind_a : behind_a * A.high;
+        all_e = __builtin_fmaf(A.low, E.high, E.low);
+      }
+      all_a = A.low * A.high;
+    }
+  }
+};
+
+// What the waves of a workgroup tell each other, a column's side by side: two buffers in turn, so that the next round's writes never meet a wave that still reads this one.
+template <int V, int CL>
+struct alignas(16) Told {
+  float at[2][V][CL][WAVES];
+  __device__ __forceinline__ void get(int turn, int c, int column, float (&to)[WAVES]) const {
+    typedef float quad __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int w = 0; w < WAVES; w += 4) {
+      const quad q = *reinterpret_cast<const quad*>(&at[turn][c][column][w]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) to[w + k] = q[k];
+    }
+  }
+};
 
 // Forward.  ENDS: no outputs, but what each segment makes of the state before it, P.parts[b][segment][a, h][C]; the mix composes those of the segments before its own.
 template <typename T, int V, int CL, int FRAMES, bool INPUT, bool ENDS>
 __global__ __launch_bounds__(THREADS) void scan_kernel(ScanParams P) {
   typedef Shape<CL, FRAMES> S;
-  __shared__ float2 sums[2][WAVES][V][CL];
+  __shared__ Told<V, CL> told_a, told_h;
   const Part part = part_of<CL, V>(P);
   const long long b = part.b;
   const int channel = part.channel, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = threadIdx.x % CL, run = (threadIdx.x & 63) / CL;
@@ -177,29 +231,35 @@ __global__ __launch_bounds__(THREADS) void scan_kernel(ScanParams P) {
         const float u = INPUT ? gate(ri.at(k, c)).on : a.off;
         const Stay stay(a, here);
         A[c] = stay.of(A[c]);
-        H[c] = stay.of(H[c], here ? u * rx.at(k, c) : 0.f);
+        H[c] = stay.of(H[c], here ? u * (float)rx.at(k, c) : 0.f);
         if (!ENDS) As[k][c] = A[c], Hs[k][c] = H[c];
       }
     if (first + S::ROUND < used) load(first + S::ROUND);
-    // two buffers in turn: the next round's writes never meet a wave that still reads this one
-    float a_to[V], h_to[V];
+    Joined<CL> joined[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      float a_all, h_all;
-      join_runs<CL, true>(A[c], H[c], a_to[c], h_to[c], a_all, h_all);
-      if (run == S::RUNS - 1) sums[turn][wave][c][column] = make_float2(a_all, h_all);
+      joined[c].template join<true, false>(A[c], H[c], 0.f);
+      if (run == 0) {
+        told_a.at[turn][c][column][wave] = joined[c].all_a;
+        told_h.at[turn][c][column][wave] = joined[c].all_h;
+      }
     }
     __syncthreads();
     float h[V];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w)
+    for (int c = 0; c < V; ++c) {
+      float as[WAVES], hs[WAVES];
+      told_a.get(turn, c, column, as);
+      told_h.get(turn, c, column, hs);
+      h[c] = state[c];
 #pragma unroll
-      for (int c = 0; c < V; ++c) {
-        if (w == wave) h[c] = __builtin_fmaf(a_to[c], state[c], h_to[c]);
-        const float2 s = sums[turn][w][c][column];
-        state[c] = __builtin_fmaf(s.x, state[c], s.y);
-        if (ENDS) factor[c] *= s.x;
+      for (int w = 0; w < WAVES; ++w) {
+        state[c] = __builtin_fmaf(as[w], state[c], hs[w]);
+        if (ENDS) factor[c] *= as[w];
+        if (w + 1 == wave) h[c] = state[c];
       }
+      h[c] = __builtin_fmaf(joined[c].before_a, h[c], joined[c].before_h);
+    }
     if (ENDS) return;
     if (P.kept && t % SCAN_KEPT == 0 && t < used && part.live)
 #pragma unroll
@@ -244,8 +304,7 @@ __global__ __launch_bounds__(THREADS) void scan_kernel(ScanParams P) {
 template <typename T, int V, int CL, int FRAMES, bool INPUT, bool ENDS>
 __global__ __launch_bounds__(THREADS) void scan_backward_kernel(ScanParams P) {
   typedef Shape<CL, FRAMES> S;
-  __shared__ float2 sums[2][WAVES][V][CL];
-  __shared__ float carries[2][WAVES][V][CL];
+  __shared__ Told<V, CL> told_a, told_h, told_e;
   const Part part = part_of<CL, V>(P);
   const long long b = part.b;
   const int channel = part.channel, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = threadIdx.x % CL, run = (threadIdx.x & 63) / CL;
@@ -318,14 +377,14 @@ __global__ __launch_bounds__(THREADS) void scan_backward_kernel(ScanParams P) {
         const bool here = FULL || t + k < used;
         const Gate a = gate(rf.at(k, c));
         stay[k][c] = Stay(a, here);
-        go[k][c] = here ? rg.at(k, c) : 0.f;
+        go[k][c] = here ? (float)rg.at(k, c) : 0.f;
         if (ENDS) {
           A[c] = stay[k][c].of(A[c]);
           continue;
         }
         // (the slope a (1 - a) is made of these two where it is used)
         off[k][c] = here ? a.off : 0.f;
-        in[k][c] = here ? rx.at(k, c) : 0.f;
+        in[k][c] = here ? (float)rx.at(k, c) : 0.f;
         if (INPUT) {
           const Gate u = gate(ri.at(k, c));
           take[k][c] = here ? u.on : 0.f;
@@ -341,43 +400,42 @@ __global__ __launch_bounds__(THREADS) void scan_backward_kernel(ScanParams P) {
 #pragma unroll
       for (int c = 0; c < V; ++c) E[c] = stay[k][c].of(E[c] + go[k][c]);
     if (first > begin) load(first - S::ROUND);
-    float a_to[V], h_to[V], a_from[V], e_from[V];
+    Joined<CL> joined[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      float a_all, h_all, e_all;
-      if (!ENDS) {
-        join_runs<CL, true>(A[c], H[c], a_to[c], h_to[c], a_all, h_all);
-        if (run == S::RUNS - 1) sums[turn][wave][c][column] = make_float2(a_all, h_all);
-      }
-      join_runs<CL, false>(A[c], E[c], a_from[c], e_from[c], a_all, e_all);
+      joined[c].template join<!ENDS, true>(A[c], H[c], E[c]);
       if (run == 0) {
-        carries[turn][wave][c][column] = e_all;
-        if (ENDS) sums[turn][wave][c][column] = make_float2(a_all, 0.f);
+        told_a.at[turn][c][column][wave] = joined[c].all_a;
+        if (!ENDS) told_h.at[turn][c][column][wave] = joined[c].all_h;
+        told_e.at[turn][c][column][wave] = joined[c].all_e;
       }
     }
     __syncthreads();
     float e[V];
-    if (!ENDS)
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w)
-        if (w < wave && w >= wave - wave % S::KEPT_WAVES)
+    for (int c = 0; c < V; ++c) {
+      float as[WAVES], es[WAVES];
+      told_a.get(turn, c, column, as);
+      told_e.get(turn, c, column, es);
+      if (!ENDS) {
+        float hs[WAVES];
+        told_h.get(turn, c, column, hs);
+        const int from = wave - wave % S::KEPT_WAVES;
 #pragma unroll
-          for (int c = 0; c < V; ++c) {
-            const float2 s = sums[turn][w][c][column];
-            h[c] = __builtin_fmaf(s.x, h[c], s.y);
-          }
-#pragma unroll
-    for (int w = WAVES - 1; w >= 0; --w)
-#pragma unroll
-      for (int c = 0; c < V; ++c) {
-        if (w == wave) e[c] = __builtin_fmaf(a_from[c], carry[c], e_from[c]);
-        const float a = sums[turn][w][c][column].x;
-        carry[c] = __builtin_fmaf(a, carry[c], carries[turn][w][c][column]);
-        if (ENDS) factor[c] *= a;
+        for (int w = 0; w + 1 < WAVES; ++w)
+          if (w >= from && w < wave) h[c] = __builtin_fmaf(as[w], h[c], hs[w]);
+        h[c] = __builtin_fmaf(joined[c].before_a, h[c], joined[c].before_h);
       }
-    if (ENDS) return;
+      e[c] = carry[c];
 #pragma unroll
-    for (int c = 0; c < V; ++c) h[c] = __builtin_fmaf(a_to[c], h[c], h_to[c]);
+      for (int w = WAVES - 1; w >= 0; --w) {
+        carry[c] = __builtin_fmaf(as[w], carry[c], es[w]);
+        if (ENDS) factor[c] *= as[w];
+        if (w == wave + 1) e[c] = carry[c];
+      }
+      e[c] = __builtin_fmaf(joined[c].behind_a, e[c], joined[c].behind_e);
+    }
+    if (ENDS) return;
 #pragma unroll
     for (int k = 0; k < FRAMES; ++k)
 #pragma unroll
@@ -440,9 +498,9 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStep P) {
     const T* i = INPUT ? static_cast<const T*>(P.i) + b * P.i_b + channel : nullptr;
     float* state = P.state + b * P.C + channel;
     T* out = static_cast<T*>(P.out) + b * P.C + channel;
-    const auto next = [](float h, float x, float f, float i) {
+    const auto next = [](float h, T x, T f, T i) {
       const Gate a = gate(f);
-      return Stay(a, true).of(h, (INPUT ? gate(i).on : a.off) * x);
+      return Stay(a, true).of(h, (INPUT ? gate(i).on : a.off) * (float)x);
     };
     if (channel + STEP <= P.C) {
       const auto vx = vec_load<STEP>(x), vf = vec_load<STEP>(f), vi = INPUT ? vec_load<STEP>(i) : vf;
@@ -450,14 +508,14 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStep P) {
       typename Vec<T, STEP>::plain o;
 #pragma unroll
       for (int c = 0; c < STEP; ++c) {
-        h[c] = next(h[c], (float)vx[c], (float)vf[c], (float)vi[c]);
+        h[c] = next(h[c], vx[c], vf[c], vi[c]);
         o[c] = (T)h[c];
       }
       vec_store<STEP>(state, h);
       vec_store<STEP>(out, o);
     } else {
       for (int c = 0; c < P.C - channel; ++c) {
-        const float h = next(state[c], (float)x[c], (float)f[c], INPUT ? (float)i[c] : 0.f);
+        const float h = next(state[c], x[c], f[c], INPUT ? i[c] : f[c]);
         state[c] = h;
         out[c] = (T)h;
       }
