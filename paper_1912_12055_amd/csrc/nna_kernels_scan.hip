@@ -15,7 +15,7 @@ namespace nna {
 
 namespace {
 
-constexpr int WAVES = 8, THREADS = WAVES * 64;
+
 
 // sigmoid(v) and sigmoid(-v), each to float32's own precision of itself.  Of a float32 v the argument of the machine's 2^y is made in two parts, since y's rounding alone is y 2^-24 of the
 // result; a 16-bit v is itself off by far more.  (minimum and maximum let a NaN through.)
@@ -50,7 +50,7 @@ struct Stay {
 };
 
 // A workgroup's lanes: CL neighbours along the channels, V channels each, 64 / CL runs of FRAMES frames in a wave, WAVES waves behind one another.
-template <int CL, int FRAMES>
+template <int CL, int FRAMES, int WAVES>
 struct Shape {
   static constexpr int RUNS = 64 / CL, WAVE = RUNS * FRAMES, ROUND = WAVES * WAVE;  // runs of a wave; frames of a wave, of a round
   static constexpr int KEPT_WAVES = SCAN_KEPT / WAVE;                               // waves from one kept state to the next
@@ -122,45 +122,30 @@ struct Joined {
     before_a = behind_a = 1.f;
     before_h = behind_e = 0.f;
     all_a = a, all_h = h, all_e = e;
-    if constexpr (CL == 16) {
-      const bool odd = threadIdx.x & 16;
-      const Two A = rows_of(a);
-      if (FORWARD) {
-        const Two H = rows_of(h);
-        before_a = odd ? A.low : 1.f;
-        before_h = odd ? H.low : 0.f;
-        all_h = __builtin_fmaf(A.high, H.low, H.high);
-      }
-      if (BACKWARD) {
-        const Two E = rows_of(e);
-        behind_a = odd ? 1.f : A.high;
-        behind_e = odd ? 0.f : E.high;
-        all_e = __builtin_fmaf(A.low, E.high, E.low);
-      }
-      all_a = A.low * A.high;
+    if constexpr (CL <= 16) step<FORWARD, BACKWARD>(threadIdx.x & 16, rows_of);
+    if constexpr (CL <= 32) step<FORWARD, BACKWARD>(threadIdx.x & 32, halves_of);
+  }
+  template <bool FORWARD, bool BACKWARD, typename F>
+  __device__ __forceinline__ void step(bool upper, F two) {
+    const Two A = two(all_a);
+    if (FORWARD) {
+      const Two H = two(all_h);
+      before_h = upper ? __builtin_fmaf(before_a, H.low, before_h) : before_h;
+      before_a = upper ? before_a * A.low : before_a;
+      all_h = __builtin_fmaf(A.high, H.low, H.high);
     }
-    if constexpr (CL <= 32) {
-      const bool upper = threadIdx.x & 32;
-      const Two A = halves_of(all_a);
-      if (FORWARD) {
-        const Two H = halves_of(all_h);
-        before_h = upper ? __builtin_fmaf(before_a, H.low, before_h) : before_h;
-        before_a = upper ? before_a * A.low : before_a;
-        all_h = __builtin_fmaf(A.high, H.low, H.high);
-      }
-      if (BACKWARD) {
-        const Two E = halves_of(all_e);
-        behind_e = upper ? behind_e : __builtin_fmaf(behind_a, E.high, behind_e);
-        behind_a = upper ? behind_a : behind_a * A.high;
-        all_e = __builtin_fmaf(A.low, E.high, E.low);
-      }
-      all_a = A.low * A.high;
+    if (BACKWARD) {
+      const Two E = two(all_e);
+      behind_e = upper ? behind_e : __builtin_fmaf(behind_a, E.high, behind_e);
+      behind_a = upper ? behind_a : behind_a * A.high;
+      all_e = __builtin_fmaf(A.low, E.high, E.low);
     }
+    all_a = A.low * A.high;
   }
 };
 
 // What the waves of a workgroup tell each other, a column's side by side: two buffers in turn, so that the next round's writes never meet a wave that still reads this one.
-template <int V, int CL>
+template <int V, int CL, int WAVES>
 struct alignas(16) Told {
   float at[2][V][CL][WAVES];
   __device__ __forceinline__ void get(int turn, int c, int column, float (&to)[WAVES]) const {
@@ -175,13 +160,14 @@ struct alignas(16) Told {
 };
 
 // Forward.  ENDS: no outputs, but what each segment makes of the state before it, P.parts[b][segment][a, h][C]; the mix composes those of the segments before its own.
-template <typename T, int V, int CL, int FRAMES, bool INPUT, bool ENDS>
-__global__ __launch_bounds__(THREADS) void scan_kernel(ScanParams P) {
-  typedef Shape<CL, FRAMES> S;
-  __shared__ Told<V, CL> told_a, told_h;
+template <typename T, int V, int CL, int FRAMES, int WAVES, bool INPUT, bool ENDS>
+__global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
+  typedef Shape<CL, FRAMES, WAVES> S;
+  __shared__ Told<V, CL, WAVES> told_a, told_h;
   const Part part = part_of<CL, V>(P);
   const long long b = part.b;
   const int channel = part.channel, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = threadIdx.x % CL, run = (threadIdx.x & 63) / CL;
+  if (ENDS && part.segment == P.segments - 1) return;  // (there is none behind the last)
   const int n = length_of(P.lengths, b, P.T);
   const T* x = static_cast<const T*>(P.x) + b * P.x_b + channel;
   const T* f = static_cast<const T*>(P.f) + b * P.f_b + channel;
@@ -196,12 +182,39 @@ __global__ __launch_bounds__(THREADS) void scan_kernel(ScanParams P) {
     factor[c] = 1.f;
     state[c] = !ENDS && P.first ? P.first[b * P.C + channel + c] : 0.f;
   }
-  if (!ENDS)
-    for (int s = 0; s < part.segment; ++s) {
+  if (!ENDS && part.segment) {
+    // the segments before this one, shared out among the runs
+    const int each = (part.segment + S::RUNS * WAVES - 1) / (S::RUNS * WAVES), from = (wave * S::RUNS + run) * each, to = from + each < part.segment ? from + each : part.segment;
+    float A[V], H[V];
+#pragma unroll
+    for (int c = 0; c < V; ++c) A[c] = 1.f, H[c] = 0.f;
+    for (int s = from; s < to; ++s) {
       const float* p = P.parts + (b * P.segments + s) * 2 * P.C + channel;
 #pragma unroll
-      for (int c = 0; c < V; ++c) state[c] = __builtin_fmaf(p[c], state[c], p[P.C + c]);
+      for (int c = 0; c < V; ++c) {
+        H[c] = __builtin_fmaf(p[c], H[c], p[P.C + c]);
+        A[c] *= p[c];
+      }
     }
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      Joined<CL> joined;
+      joined.template join<true, false>(A[c], H[c], 0.f);
+      if (run == 0) {
+        told_a.at[1][c][column][wave] = joined.all_a;
+        told_h.at[1][c][column][wave] = joined.all_h;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      float as[WAVES], hs[WAVES];
+      told_a.get(1, c, column, as);
+      told_h.get(1, c, column, hs);
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) state[c] = __builtin_fmaf(as[w], state[c], hs[w]);
+    }
+  }
   Rows<T, V, FRAMES> rx, rf, ri;
   const auto load = [&](int t) {
     if (t + S::ROUND <= P.T) {
@@ -297,17 +310,18 @@ __global__ __launch_bounds__(THREADS) void scan_kernel(ScanParams P) {
   typename Vec<T, V>::plain zero;
 #pragma unroll
   for (int c = 0; c < V; ++c) vec_set<V>(zero, c, (T)0.f);
-  for (t += threadIdx.x / CL; t < end; t += THREADS / CL) vec_store<V>(out + (long long)t * P.C, zero);
+  for (t += threadIdx.x / CL; t < end; t += WAVES * 64 / CL) vec_store<V>(out + (long long)t * P.C, zero);
 }
 
 // Backward, from the last frame to the first.  ENDS: what each segment makes of the carry behind it, P.parts[b][segment][a, e][C].
-template <typename T, int V, int CL, int FRAMES, bool INPUT, bool ENDS>
-__global__ __launch_bounds__(THREADS) void scan_backward_kernel(ScanParams P) {
-  typedef Shape<CL, FRAMES> S;
-  __shared__ Told<V, CL> told_a, told_h, told_e;
+template <typename T, int V, int CL, int FRAMES, int WAVES, bool INPUT, bool ENDS>
+__global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P) {
+  typedef Shape<CL, FRAMES, WAVES> S;
+  __shared__ Told<V, CL, WAVES> told_a, told_h, told_e;
   const Part part = part_of<CL, V>(P);
   const long long b = part.b;
   const int channel = part.channel, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = threadIdx.x % CL, run = (threadIdx.x & 63) / CL;
+  if (ENDS && part.segment == 0) return;  // (there is none before the first)
   const int n = length_of(P.lengths, b, P.T);
   const T* x = static_cast<const T*>(P.x) + b * P.x_b + channel;
   const T* f = static_cast<const T*>(P.f) + b * P.f_b + channel;
@@ -324,18 +338,47 @@ __global__ __launch_bounds__(THREADS) void scan_backward_kernel(ScanParams P) {
     factor[c] = 1.f;
     carry[c] = !ENDS && P.glast ? P.glast[b * P.C + channel + c] : 0.f;
   }
-  if (!ENDS)
-    for (int s = P.segments - 1; s > part.segment; --s) {
+  const int behind = P.segments - 1 - part.segment;
+  if (!ENDS && behind) {
+    // the segments behind this one, shared out among the runs
+    const int each = (behind + S::RUNS * WAVES - 1) / (S::RUNS * WAVES), from = part.segment + 1 + (wave * S::RUNS + run) * each;
+    const int to = from + each < P.segments ? from + each : P.segments;
+    float A[V], E[V];
+#pragma unroll
+    for (int c = 0; c < V; ++c) A[c] = 1.f, E[c] = 0.f;
+    for (int s = to - 1; s >= from; --s) {
       const float* p = P.parts + (b * P.segments + s) * 2 * P.C + channel;
 #pragma unroll
-      for (int c = 0; c < V; ++c) carry[c] = __builtin_fmaf(p[c], carry[c], p[P.C + c]);
+      for (int c = 0; c < V; ++c) {
+        E[c] = __builtin_fmaf(p[c], E[c], p[P.C + c]);
+        A[c] *= p[c];
+      }
     }
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      Joined<CL> joined;
+      joined.template join<false, true>(A[c], 0.f, E[c]);
+      if (run == 0) {
+        told_a.at[1][c][column][wave] = joined.all_a;
+        told_e.at[1][c][column][wave] = joined.all_e;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      float as[WAVES], es[WAVES];
+      told_a.get(1, c, column, as);
+      told_e.get(1, c, column, es);
+#pragma unroll
+      for (int w = WAVES - 1; w >= 0; --w) carry[c] = __builtin_fmaf(as[w], carry[c], es[w]);
+    }
+  }
   const int rounds = used > begin ? (used - begin + S::ROUND - 1) / S::ROUND : 0;
   if (!ENDS && part.live) {
     typename Vec<T, V>::plain zero;
 #pragma unroll
     for (int c = 0; c < V; ++c) vec_set<V>(zero, c, (T)0.f);
-    for (int t = begin + rounds * S::ROUND + threadIdx.x / CL; t < end; t += THREADS / CL) {
+    for (int t = begin + rounds * S::ROUND + threadIdx.x / CL; t < end; t += WAVES * 64 / CL) {
       vec_store<V>(gx + (long long)t * P.C, zero);
       vec_store<V>(gf + (long long)t * P.C, zero);
       if (INPUT) vec_store<V>(gi + (long long)t * P.C, zero);
@@ -523,21 +566,29 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStep P) {
   }
 }
 
-// How a call is cut up: whether a wave's lanes are 16 neighbouring channels' and four runs of frames, and segments.
+// How a call is cut up: neighbouring channels' lanes in a wave, waves, segments.  16 sequences of 4,096 frames of 2,048 channels in bfloat16, forward and backward: 32 lanes (rows of 128 bytes, a
+// line) 170 and 316 us, 16 lanes 217 and 385, 8 lanes (4 sequences of 16,384) 270 and 413: lines shared by workgroups cost more than waves that wait.  So 32 lanes wherever their workgroups
+// fill the card: 256 of them, the same values, 162 and 308.  128 of them leave half of it idle, 265 and 527; 16 lanes' 256 take 193 and 365, eight segments of 32 lanes 134 + 156 and
+// 141 + 302 (two readings).  With 64 workgroups of 32 lanes (half the values) 16 lanes take 159 and 308, segments 69 + 75 and 75 + 153.
 struct Cut {
-  bool runs;
+  int lanes, waves;
   int segments, frames;
 };
-constexpr int LANES_RUNS = 16, LANES_ONE = 64, LANES_BACK = 32;
 Cut cut_of(long long B, long long T, long long C, int channels /* of a lane */) {
-  Cut c;
-  c.runs = T > 128;
-  const int lanes = c.runs ? LANES_RUNS : LANES_ONE, round = c.runs ? 256 : 64;
-  const long long groups = std::max(1LL, B * ((C + lanes * channels - 1) / (lanes * channels))), rounds = (T + round - 1) / round;
-  const long long want = !c.runs || groups >= 192 ? 1 : std::min((512 + groups - 1) / groups, rounds);
-  const long long each = want > 1 ? (rounds + want - 1) / want : std::max(rounds, 1LL);
-  c.segments = (int)std::max(1LL, (rounds + each - 1) / each);
-  c.frames = (int)(each * round);
+  const long long wide = std::max(1LL, B * ((C + 32 * channels - 1) / (32 * channels))), narrow = std::max(1LL, B * ((C + 16 * channels - 1) / (16 * channels)));
+  Cut c = {32, 8, 1, (int)std::max(1LL, T)};
+  if (T <= 64) {
+    c.waves = 4;
+  } else if (T > 256 && wide < 180) {
+    if (narrow >= 200) {
+      c.lanes = 16;
+    } else {
+      // 512 workgroups: one sequence of 15,504 frames of 512 channels 10 + 13 us, with 1,024 of them 10 + 17
+      const long long rounds = (T + 127) / 128, want = std::min((512 + wide - 1) / wide, rounds), each = (rounds + want - 1) / want;
+      c.segments = (int)((rounds + each - 1) / each);
+      c.frames = (int)(each * 128);
+    }
+  }
   return c;
 }
 unsigned grid_of(const ScanParams& P, int lanes, int channels) { return (unsigned)(P.B * P.segments * ((P.C + lanes * channels - 1) / (lanes * channels))); }
@@ -550,7 +601,7 @@ hipError_t by_lane(int C, F fn) {
   return fn(std::integral_constant<int, 1>());
 }
 
-// fn(the type, channels of a lane, whether a wave has runs, whether there is a gate of the input's own)
+// fn(the type, channels of a lane, lanes along the channels, waves, whether there is a gate of the input's own)
 template <typename F>
 hipError_t by_cut(ScanParams& P, int type, F fn) {
   return by_element(type, [&](auto t) {
@@ -558,8 +609,10 @@ hipError_t by_cut(ScanParams& P, int type, F fn) {
       const Cut c = cut_of(P.B, P.T, P.C, v.value);
       P.segments = c.segments;
       P.segment_frames = c.frames;
-      const auto gated = [&](auto runs) { return P.i ? fn(t, v, runs, std::true_type()) : fn(t, v, runs, std::false_type()); };
-      return c.runs ? gated(std::true_type()) : gated(std::false_type());
+      const auto gated = [&](auto lanes, auto waves) { return P.i ? fn(t, v, lanes, waves, std::true_type()) : fn(t, v, lanes, waves, std::false_type()); };
+      if (c.waves == 4) return gated(std::integral_constant<int, 32>(), std::integral_constant<int, 4>());
+      if (c.lanes == 16) return gated(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
+      return gated(std::integral_constant<int, 32>(), std::integral_constant<int, 8>());
     });
   });
 }
@@ -576,25 +629,25 @@ size_t scan_workspace(long long B, long long T, long long C) {
 }
 
 hipError_t launch_scan(ScanParams P, int type, hipStream_t stream) {
-  return by_cut(P, type, [&](auto t, auto v, auto runs, auto gated) {
+  return by_cut(P, type, [&](auto t, auto v, auto lanes, auto waves, auto gated) {
     typedef decltype(t) T;
-    constexpr int V = v.value, L = runs.value ? LANES_RUNS : LANES_ONE;
+    constexpr int V = v.value, L = lanes.value, W = waves.value;
     const unsigned grid = grid_of(P, L, V);
-    if constexpr (runs.value)
-      if (P.segments > 1) hipLaunchKernelGGL((scan_kernel<T, V, L, 8, gated.value, true>), dim3(grid), dim3(THREADS), 0, stream, P);
-    hipLaunchKernelGGL((scan_kernel<T, V, L, 8, gated.value, false>), dim3(grid), dim3(THREADS), 0, stream, P);
+    if constexpr (L == 32 && W == 8)
+      if (P.segments > 1) hipLaunchKernelGGL((scan_kernel<T, V, L, 8, W, gated.value, true>), dim3(grid), dim3(W * 64), 0, stream, P);
+    hipLaunchKernelGGL((scan_kernel<T, V, L, 8, W, gated.value, false>), dim3(grid), dim3(W * 64), 0, stream, P);
     return hipGetLastError();
   });
 }
 
 hipError_t launch_scan_backward(ScanParams P, int type, hipStream_t stream) {
-  return by_cut(P, type, [&](auto t, auto v, auto runs, auto gated) {
+  return by_cut(P, type, [&](auto t, auto v, auto lanes, auto, auto gated) {
     typedef decltype(t) T;
-    constexpr int V = v.value, L = runs.value ? LANES_RUNS : LANES_BACK;
+    constexpr int V = v.value, L = lanes.value, W = 8;  // (rounds of half as many frames: more is held of each)
     const unsigned grid = grid_of(P, L, V);
-    if constexpr (runs.value)
-      if (P.segments > 1) hipLaunchKernelGGL((scan_backward_kernel<T, V, L, 8, false, true>), dim3(grid), dim3(THREADS), 0, stream, P);
-    hipLaunchKernelGGL((scan_backward_kernel<T, V, L, 4, gated.value, false>), dim3(grid), dim3(THREADS), 0, stream, P);
+    if constexpr (L == 32)
+      if (P.segments > 1) hipLaunchKernelGGL((scan_backward_kernel<T, V, L, 8, W, false, true>), dim3(grid), dim3(W * 64), 0, stream, P);
+    hipLaunchKernelGGL((scan_backward_kernel<T, V, L, 4, W, gated.value, false>), dim3(grid), dim3(W * 64), 0, stream, P);
     return hipGetLastError();
   });
 }
