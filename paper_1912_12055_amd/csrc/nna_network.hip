@@ -32,7 +32,7 @@ nna_status check_rotate(int type, long long B, long long T, long long q_heads, l
   if (B < 0 || T < 0 || q_heads < 1 || k_heads < 0 || width < 1) return fail(NNA_ERR_SHAPE, "B, T and k_heads must not be negative, q_heads and width at least 1");
   if (width > ROTATE_HEAD_MAX) return fail(NNA_ERR_UNSUPPORTED, "heads of more than " + std::to_string(ROTATE_HEAD_MAX) + " values");
   if (pairs < 0 || 2 * pairs > width) return fail(NNA_ERR_SHAPE, "pairs must not be negative, nor more than a head holds");
-  if (q_heads > 65536 || k_heads > 65536 || (T && B > (1LL << 40) / T)) return fail(NNA_ERR_SHAPE, "too many heads or frames");
+  if (q_heads > 65536 || k_heads > 65536 || T > INT_MAX - 65536 || (T && B > (1LL << 40) / T)) return fail(NNA_ERR_SHAPE, "too many heads or frames");
   return NNA_OK;
 }
 
@@ -70,6 +70,7 @@ RotateHeads rotate_heads(const void* x, const long long* strides, long long head
   RotateHeads H = {};
   H.heads = (int)heads;
   if (!heads) return H;
+  H.inverse = ((1ULL << 32) + heads - 1) / heads;
   H.x = x;
   if (strides) {
     H.x_b = strides[0];
@@ -82,7 +83,7 @@ RotateHeads rotate_heads(const void* x, const long long* strides, long long head
   return H;
 }
 
-size_t rotate_workspace(long long B, long long T, long long width) { return (size_t)std::max(1LL, std::min(B * T, 1024LL)) * 2 * width * sizeof(float); }
+size_t rotate_workspace(long long B, long long T, long long width) { return (size_t)std::max(1LL, std::min(B * T, (long long)ROTATE_GROUPS)) * 2 * width * sizeof(float); }
 
 // ---- the gated recurrence ----
 

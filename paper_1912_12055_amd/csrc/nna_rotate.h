@@ -6,6 +6,7 @@
 namespace nna {
 
 constexpr int ROTATE_HEAD_MAX = 256;  // values of a head
+constexpr int ROTATE_GROUPS = 512;    // backward: workgroups, at most, that leave a partial sum of each weight's gradient
 
 struct RotateHeads {
   const void* x;                 // [B, T, heads, width], a head's values next to each other
@@ -14,6 +15,7 @@ struct RotateHeads {
   void* y;                       // [B, T, heads, width]; backward: the gradient of x
   const void* g;                 // backward: [B, T, heads, width]
   int heads;                     // 0: none
+  unsigned long long inverse;    // 2^32 / heads, rounded up
 };
 
 struct RotateParams {

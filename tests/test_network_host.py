@@ -88,7 +88,7 @@ def test_no_device(call):
 def test_memory():
     n = c_size_t()
     assert nb.nna_rotate_heads_backward_workspace(2, 50, 64) == 100 * 2 * 64 * 4
-    assert nb.nna_rotate_heads_backward_workspace(20, 5000, 64) == 1024 * 2 * 64 * 4
+    assert nb.nna_rotate_heads_backward_workspace(20, 5000, 64) == 512 * 2 * 64 * 4
     assert nb.nna_rotate_heads_backward_workspace(0, 0, 64) == 2 * 64 * 4
     assert nb.lib().nna_rotate_heads_backward_workspace(1, 1, 300, byref(n)) == UNSUPPORTED
     assert nb.lib().nna_rotate_heads_backward_workspace(1, 1, 64, None) == ARG
