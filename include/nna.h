@@ -706,7 +706,7 @@ nna_status nna_rotate_heads_backward(const void* gq_out_dev, const void* gk_out_
  * nna_gated_scan_backward: from gout_dev [B, T, C] (contiguous), glast_dev [B, C] (or NULL: 0) and kept_dev the gradients gx_dev, gforget_dev, ginput_dev (with input_dev)
  * [B, T, C] (contiguous, of `type`) and gfirst_dev [B, C] (float32, or NULL).  Outputs are none of the inputs.  The same inputs give the same bits.
  * nna_gated_scan_step: x_dev, forget_dev, input_dev [B, C] with their stride between batches; state_dev [B, C] updated in place; out_dev [B, C], contiguous.
- * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_SHAPE (B times C, in 64s, above 2^22).  T = 0 or B = 0 is no error.
+ * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_SHAPE (B times C, in 64s, above 2^21).  T = 0 or B = 0 is no error.
  */
 #define NNA_SCAN_KEPT 64
 nna_status nna_gated_scan_workspace(long long B, long long T, long long C, size_t* bytes);

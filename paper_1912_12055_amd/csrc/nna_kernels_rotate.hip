@@ -330,7 +330,7 @@ __global__ __launch_bounds__(THREADS, 4) void rotate_backward_kernel(RotateParam
 int tokens_of(int heads, int pairs, const Split& s) {
   int n = std::max(1, (2 * THREADS >> s.shift) / heads);
   if (pairs) n = std::max(n, 96 / pairs);
-  n = std::min(n, TOKENS_MAX);
+  n = std::min(n, std::max(1, std::min(TOKENS_MAX, 4096 / heads)));  // (what Where's quotient is good for)
   return pairs ? std::min(n, TABLE / pairs) : n;
 }
 

@@ -90,7 +90,8 @@ size_t rotate_workspace(long long B, long long T, long long width) { return (siz
 nna_status check_scan(int type, long long B, long long T, long long C) {
   if (!known_type(type)) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
   if (B < 0 || T < 0 || C < 1) return fail(NNA_ERR_SHAPE, "B and T must not be negative, C at least 1");
-  if (C > (1 << 28) || B > (1LL << 22) / ((C + 63) / 64)) return fail(NNA_ERR_SHAPE, "B C is too large");
+  // (groups of 32 channels times the 512 lanes of their workgroups are less than 2^32 in a launch)
+  if (C > (1 << 27) || B > (1LL << 21) / ((C + 63) / 64)) return fail(NNA_ERR_SHAPE, "B C is too large");
   if (T > INT_MAX - 65536) return fail(NNA_ERR_SHAPE, "T is too large");
   return NNA_OK;
 }

@@ -14,7 +14,8 @@ rounded up to 128 times frames times 4 bytes, at most 1 GiB a call.  Larger batc
 of the values the codes stand for, off by up to 1/254 of the largest of 128 neighbouring frames of a clip and kernel.  A product that is not finite makes those of
 its 128 NaN, of no other clip or kernel.
 
-``LayerNorm`` and ``DecayAttention`` are what a network on the transforms' frames is built of.
+``LayerNorm``, ``RotaryHeads``, ``DecayAttention`` and ``GatedRecurrence`` are what a network on the transforms' frames is built of; ``AdamW`` trains it, the transforms' kernels among its
+parameters.
 """
 from __future__ import annotations
 
@@ -554,3 +555,181 @@ class DecayAttention(torch.nn.Module):
         if _differentiates(q, k, v, state):
             raise RuntimeError("step has no derivative: call forward on sequences, or step under torch.no_grad()")
         return nb.nna_decay_attention_step(q, k, v, self.decay, state, scale=self.scale)
+
+
+class _RotateFn(torch.autograd.Function):
+    """nna_rotate_heads with nna_rotate_heads_backward as its derivative."""
+
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, freqs, positions, offset, eps, interleaved):
+        ctx.save_for_backward(*((q, k) if eps is not None else (None, None)), q_weight, k_weight, freqs, positions)
+        ctx.how = dict(offset=offset, eps=eps, interleaved=interleaved)
+        ctx.like = [None if x is None else (x.shape, x.dtype, x.device) for x in (q, k)]
+        ctx.set_materialize_grads(False)
+        yq, yk = nb.nna_rotate_heads(q, k, freqs, positions=positions, q_weight=q_weight, k_weight=k_weight, **ctx.how)
+        return yq if k is None else (yq, yk)
+
+    @staticmethod
+    @_one_derivative(lambda ctx: ((0, 2), (1, 3), (0,), (1,)) + 5 * ((),) if ctx.how["eps"] is not None else 9 * ((),))
+    def backward(ctx, gq, gk=None):
+        q, k, q_weight, k_weight, freqs, positions = ctx.saved_tensors
+        gq, gk = (None if like is None else torch.zeros(like[0], dtype=like[1], device=like[2]) if g is None else g.contiguous() for g, like in zip((gq, gk), ctx.like))
+        need = ctx.needs_input_grad
+        # (without a norm the gradients know nothing of q and k: theirs stand for their shapes)
+        hq, hk, gqw, gkw = nb.nna_rotate_heads_backward(gq, gk, gq if q is None else q, gk if k is None else k, freqs, positions=positions, q_weight=q_weight, k_weight=k_weight,
+                                                        want_weights=need[2] or need[3], **ctx.how)
+        return (hq if need[0] else None, hk if need[1] else None, gqw if need[2] else None, gkw if need[3] else None) + 5 * (None,)
+
+
+class RotaryHeads(torch.nn.Module):
+    """Queries and keys of heads of `width` values, each head normalised by its root mean square (``eps=None``: not) and the pairs of its first `rotary` values (all of them if None)
+    rotated by its frame's position, in one pass: what ``DecayAttention`` takes.
+
+    ``q_weight`` and ``k_weight`` are float32 parameters of the norms.  ``freqs``: float64 radians a position, or by ``base`` and ``scale`` (``nna_rotary_freqs``).  Pair j is
+    (j, j + rotary / 2), or ``interleaved`` (2 j, 2 j + 1)."""
+
+    def __init__(self, width, rotary=None, eps=1e-6, affine=True, base=10000.0, scale=1.0, freqs=None, interleaved=False, device="cuda:0"):
+        super().__init__()
+        dev = torch.device("cuda", _device_index(device))
+        self.width, self.eps, self.interleaved = int(width), None if eps is None else float(eps), bool(interleaved)
+        rotary = self.width // 2 * 2 if rotary is None else int(rotary)
+        # no buffer: a module's .bfloat16() would take the angles' precision with the weights'
+        self._freqs = nb.nna_rotary_freqs(rotary, base, scale, device=dev) if freqs is None else torch.as_tensor(freqs, dtype=torch.float64).to(dev).contiguous()
+        if self._freqs.dim() != 1 or not 2 * self._freqs.numel() <= self.width:
+            raise ValueError(f"freqs: one axis, of at most {self.width // 2}")
+        norm = affine and eps is not None
+        self.q_weight, self.k_weight = (torch.nn.Parameter(torch.ones(self.width, device=dev)) if norm else None for _ in range(2))
+
+    def forward(self, q, k=None, positions=None, offset=0):
+        """(q, k), or q where there is no k: ``[B, T, heads, width]``, or ``[B, heads, width]`` of one frame.  positions: int32 ``[B, T]`` (``[B]``) on the GPU; if None, frame t is at
+        offset + t."""
+        if q.shape[-1] != self.width:
+            raise ValueError(f"heads must have {self.width} values")
+        if self._freqs.device != q.device:
+            self._freqs = self._freqs.to(q.device)
+        wk = None if k is None else self.k_weight
+        if _differentiates(q, k, self.q_weight, wk):
+            return _RotateFn.apply(q, k, self.q_weight, wk, self._freqs, positions, offset, self.eps, self.interleaved)
+        out = nb.nna_rotate_heads(q, k, self._freqs, positions=positions, offset=offset, q_weight=self.q_weight, k_weight=wk, eps=self.eps, interleaved=self.interleaved)
+        return out[0] if k is None else out
+
+
+class _ScanFn(torch.autograd.Function):
+    """nna_gated_scan with nna_gated_scan_backward as its derivative."""
+
+    @staticmethod
+    def forward(ctx, x, forget, input, state, lengths, want_state):
+        *out, kept = nb.nna_gated_scan(x, forget, input, state=state, lengths=lengths, want_state=want_state, keep=True)
+        ctx.save_for_backward(x, forget, input, lengths, kept)
+        ctx.set_materialize_grads(False)
+        return tuple(out) if want_state else out[0]
+
+    @staticmethod
+    @_one_derivative(lambda ctx: ((1, 2), (0, 1, 2, 3), (0, 1, 2), (1,), (), ()))
+    def backward(ctx, gout, gstate=None):
+        x, forget, input, lengths, kept = ctx.saved_tensors
+        gout = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if gout is None else gout.contiguous()
+        need = ctx.needs_input_grad
+        gx, gf, gi, gfirst = nb.nna_gated_scan_backward(gout, kept, x, forget, input, lengths=lengths, gstate=None if gstate is None else gstate.contiguous(), want_gstate=need[3])
+        return gx if need[0] else None, gf if need[1] else None, gi if need[2] else None, gfirst, None, None
+
+
+class GatedRecurrence(torch.nn.Module):
+    """A linear recurrence of channels over frames, h_t = a_t h_{t-1} + u_t x_t, a = sigmoid(forget), u = sigmoid(input), or 1 - a where there is no gate of the input's own.
+
+    ``forward`` takes whole sequences ``[B, T, C]`` (float32, bfloat16 or float16) of `lengths` frames (int32 on the GPU), going on from `state`; ``step`` one new frame of each."""
+
+    def forward(self, x, forget, input=None, state=None, lengths=None, return_state=False):
+        """h ``[B, T, C]``, or (h, state after the last frame ``[B, C]`` float32)."""
+        if _differentiates(x, forget, input, state):
+            return _ScanFn.apply(x, forget, input, state, lengths, return_state)
+        return nb.nna_gated_scan(x, forget, input, state=state, lengths=lengths, want_state=return_state)
+
+    def step(self, x, forget, state, input=None):
+        """h ``[B, C]`` of one frame; ``state`` is updated in place (not differentiable)."""
+        if _differentiates(x, forget, state, input):
+            raise RuntimeError("step has no derivative: call forward on sequences, or step under torch.no_grad()")
+        return nb.nna_gated_scan_step(x, forget, state, input=input)
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW over all of a group's tensors in one pass (``nna_adamw``): contiguous float32, bfloat16 and float16 parameters of one device, a group's together.
+
+    ``bits=8`` holds the moments in 8 bits, 128 neighbours to a scale: 2.1 bytes a parameter in place of 8.  ``master=True``: 16-bit parameters are updated in float32 copies of
+    themselves and rounded from them, so that steps smaller than their own are not lost; where such a parameter is written by something else between two steps (its version
+    counter tells), its copy is taken again.  ``capturable=True`` holds the number of steps in device memory, so that a graph can record ``step`` (after a first step that is not recorded); ``lr`` may
+    then be a float32 CUDA tensor, too.  The states of a group are flat tensors in it (``m``, ``v``, ...), and part of ``state_dict``."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, bits=32, master=True, capturable=False):
+        if bits not in (8, 32):
+            raise ValueError("bits: 8 or 32")
+        self._versions = {}
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, bits=bits, master=bool(master), capturable=bool(capturable), step=0))
+
+    def add_param_group(self, group):
+        super().add_param_group(group)
+        params = self.param_groups[-1]["params"]
+        for p in params:
+            if not p.is_cuda or p.device != params[0].device or p.dtype not in (torch.float32, torch.bfloat16, torch.float16) or not p.is_contiguous():
+                self.param_groups.pop()
+                raise ValueError("parameters must be contiguous tensors of float32, bfloat16 or float16, a group's on one CUDA device")
+
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        self.__dict__.setdefault("_versions", {})
+
+    def _begin(self, group):
+        """The states of a group, zero, and the float32 copies of its 16-bit parameters."""
+        params = group["params"]
+        device, size = params[0].device, nb.nna_adamw_places([p.numel() for p in params])[1]
+        codes = group["bits"] == 8
+        group["m"] = torch.zeros(size, dtype=torch.int8 if codes else torch.float32, device=device)
+        group["v"] = torch.zeros(size, dtype=torch.uint8 if codes else torch.float32, device=device)
+        group["m_scales"], group["v_scales"] = (torch.zeros(size // nb.NNA_BLOCK8, device=device) if codes else None for _ in range(2))
+        narrow = group["master"] and any(p.dtype != torch.float32 for p in params)
+        group["copies"] = torch.zeros(size, device=device) if narrow else None
+        if group["capturable"]:
+            group["step"] = torch.full((1,), int(group["step"]), dtype=torch.int64, device=device)
+        if narrow:
+            self._copy(group, range(len(params)))
+
+    @staticmethod
+    def _copy(group, which):
+        params = group["params"]
+        at, _ = nb.nna_adamw_places([p.numel() for p in params])
+        for i in which:
+            if params[i].dtype != torch.float32:
+                group["copies"][at[i] : at[i] + params[i].numel()].copy_(params[i].detach().flatten())
+
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)
+        for group in self.param_groups:
+            for name in ("m", "v", "m_scales", "v_scales", "copies", "step"):
+                if isinstance(group.get(name), torch.Tensor):
+                    group[name] = group[name].to(group["params"][0].device)
+        self._versions = {}
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for n, group in enumerate(self.param_groups):
+            params = group["params"]
+            grads = [p.grad for p in params]
+            if not params or all(g is None for g in grads):
+                continue
+            if "m" not in group:
+                self._begin(group)
+            elif group["copies"] is not None and n in self._versions:
+                written = [i for i, (p, v) in enumerate(zip(params, self._versions[n])) if p._version != v]
+                if written:
+                    self._copy(group, written)
+            group["step"] += 1
+            grads = [g if g is None or g.is_sparse or g.is_contiguous() else g.contiguous() for g in grads]
+            nb.nna_adamw(params, grads, group["m"], group["v"], group["step"], lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
+                         m_scales=group["m_scales"], v_scales=group["v_scales"], master=group["copies"])
+            if group["copies"] is not None:
+                self._versions[n] = [p._version for p in params]
+        return loss

@@ -117,9 +117,9 @@ def test_heads(nb, width, pairs, interleaved, dtype):
         check(nb, *inputs(2, 5, H, K, width, pairs, dtype, seed=width, weights=weights), eps, interleaved)
 
 
-@pytest.mark.parametrize("B,T,H,K", [(1, 1, 1, 1), (1, 1, 16, 16), (7, 1, 8, 2), (1, 300, 5, 1), (3, 101, 8, 8), (2, 64, 1, 0), (2, 40, 70, 3), (1, 9, 300, 1)])
+@pytest.mark.parametrize("B,T,H,K", [(1, 1, 1, 1), (1, 1, 16, 16), (7, 1, 8, 2), (1, 300, 5, 1), (3, 101, 8, 8), (2, 64, 1, 0), (2, 40, 70, 3), (1, 9, 300, 1), (2, 3, 4100, 1), (1, 50, 1, 130)])
 def test_shapes(nb, B, T, H, K):
-    for dtype, width in ((torch.bfloat16, 64), (torch.float32, 48)):
+    for dtype, width in ((torch.bfloat16, 64), (torch.float32, 48), (torch.float32, 6)):
         check(nb, *inputs(B, T, H, K, width, width // 2, dtype, seed=T), 1e-6, False)
 
 

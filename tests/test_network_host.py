@@ -59,7 +59,7 @@ NAN, INF = float("nan"), float("inf")
     (lambda: rotate_back(width=300), UNSUPPORTED), (lambda: rotate_back(type=-1), ARG),
     (lambda: scan(x=None), ARG), (lambda: scan(f=None), ARG), (lambda: scan(out=None), ARG), (lambda: scan(xs=None), ARG), (lambda: scan(fs=None), ARG),
     (lambda: scan(i=P, is_=None), ARG), (lambda: scan(type=3), ARG), (lambda: scan(C=0), SHAPE), (lambda: scan(T=-1), SHAPE), (lambda: scan(B=-1), SHAPE),
-    (lambda: scan(B=1 << 40), SHAPE), (lambda: scan(C=1 << 29), SHAPE), (lambda: scan(T=1 << 31), SHAPE),
+    (lambda: scan(B=1 << 40), SHAPE), (lambda: scan(C=1 << 29), SHAPE), (lambda: scan(B=(1 << 21) + 1), SHAPE), (lambda: scan(B=1 << 20, C=192), SHAPE), (lambda: scan(T=1 << 31), SHAPE),
     (lambda: scan_back(g=None), ARG), (lambda: scan_back(kept=None), ARG), (lambda: scan_back(x=None), ARG), (lambda: scan_back(gx=None), ARG), (lambda: scan_back(gf=None), ARG),
     (lambda: scan_back(gi=P), ARG), (lambda: scan_back(i=P), ARG), (lambda: scan_back(C=0), SHAPE),
     (lambda: step(x=None), ARG), (lambda: step(state=None), ARG), (lambda: step(out=None), ARG), (lambda: step(C=0), SHAPE), (lambda: step(type=4), ARG),
