@@ -1270,38 +1270,46 @@ def nna_rotary_freqs(width, base=10000.0, scale=1.0, device=0):
 
 
 def _turns(q, k, freqs, positions, offset, q_weight, k_weight, eps):
-    """(nna_dtype, (B, T, heads, key heads, width), [q, strides, heads, k, strides, heads], the arguments from freqs to the weights) of q, k [B, (T,) heads, width]."""
+    """(nna_dtype, (B, T, width), [q, strides, heads, k, strides, heads], the arguments from freqs to the weights) of q, k [B, (T,) heads, width]."""
     import torch
 
-    t, tensor, device = _type_of(q, "q"), torch.Tensor, q.device
-    shape, axes = q.shape, q.dim()
-    if axes not in (3, 4):
+    t, tensor, device, dtype, shape = _type_of(q, "q"), torch.Tensor, q.device, q.dtype, q.shape
+    one = len(shape) == 3
+    if one:
+        (B, H, width), T, (sb, sh, last) = shape, 1, q.stride()
+        args = [q.data_ptr(), _strides3(sb, 0, sh), H]
+    elif len(shape) == 4:
+        (B, T, H, width), (sb, st, sh, last) = shape, q.stride()
+        args = [q.data_ptr(), _strides3(sb, st, sh), H]
+    else:
         raise TypeError("q must be [B, T, heads, width], or [B, heads, width] of one frame")
-    if k is not None and not (isinstance(k, tensor) and k.dtype == q.dtype and k.device == device and k.dim() == axes and k.shape[:-2] == shape[:-2] and k.shape[-1] == shape[-1]):
-        raise TypeError("k must be of q's type, on its device and of its shape but for the number of heads")
-    B, T, H, width = shape if axes == 4 else (shape[0], 1, *shape[1:])
-    args = []
-    for x in (q, k):
-        if x is None:
-            args += [None, None, 0]
-            continue
-        *s, last = x.stride()
-        if width != 1 and last != 1:
-            raise TypeError("a head's values must lie next to each other")
-        args += [x.data_ptr(), _strides3(*s) if axes == 4 else _strides3(s[0], 0, s[1]), x.shape[-2]]
+    if k is None:
+        args += (None, None, 0)
+    else:
+        if not (isinstance(k, tensor) and k.dtype == dtype and k.device == device and len(k.shape) == len(shape)):
+            raise TypeError("k must be of q's type, on its device and of its shape but for the number of heads")
+        heads = k.shape[-2]
+        if k.shape != ((B, heads, width) if one else (B, T, heads, width)):
+            raise TypeError("k must be of q's type, on its device and of its shape but for the number of heads")
+        sb, *st, sh, last_k = k.stride()
+        last = last if last != 1 else last_k
+        args += (k.data_ptr(), _strides3(sb, 0 if one else st[0], sh), heads)
+    if last != 1 and width != 1:
+        raise TypeError("a head's values must lie next to each other")
     if not (isinstance(freqs, tensor) and freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous() and freqs.device == device):
         raise TypeError(f"freqs must be a contiguous float64 tensor of one axis on {device}")
     at, steps = None, None
     if positions is not None:
-        if not (isinstance(positions, tensor) and positions.dtype == torch.int32 and positions.device == device and positions.shape == shape[: axes - 2]):
-            raise TypeError(f"positions must be an int32 tensor of shape {tuple(shape[: axes - 2])} on {device}")
+        if not (isinstance(positions, tensor) and positions.dtype == torch.int32 and positions.device == device and positions.shape == ((B,) if one else (B, T))):
+            raise TypeError(f"positions must be an int32 tensor of shape {(B,) if one else (B, T)} on {device}")
         if offset:
             raise ValueError("offset is where positions are not given")
-        at, steps = positions.data_ptr(), _strides2(*positions.stride()) if axes == 4 else _strides2(positions.stride(0), 0)
-    if eps is None and (q_weight is not None or k_weight is not None):
+        at, steps = positions.data_ptr(), _strides2(positions.stride(0), 0) if one else _strides2(*positions.stride())
+    norm = eps is not None
+    if not norm and (q_weight is not None or k_weight is not None):
         raise ValueError("weights are the norm's: give eps")
     weights = (_vector(q_weight, "q_weight", (width,), device, none=True), _vector(k_weight, "k_weight", (width,), device, none=True))
-    return t, (B, T, H, args[5], width), args, (freqs.data_ptr(), freqs.shape[0], at, steps, int(offset), eps is not None, 0.0 if eps is None else eps, *weights)
+    return t, (B, T, width), args, (freqs.data_ptr(), freqs.numel(), at, steps, int(offset), norm, eps if norm else 0.0, *weights)
 
 
 def nna_rotate_heads(q, k, freqs, positions=None, offset=0, q_weight=None, k_weight=None, eps=None, interleaved=False, out=None, stream=None):
@@ -1311,7 +1319,7 @@ def nna_rotate_heads(q, k, freqs, positions=None, offset=0, q_weight=None, k_wei
     `interleaved` (2 j, 2 j + 1).  out: (q, k) to write to, not over inputs."""
     import torch
 
-    t, (B, T, _, heads, width), args, (freqs_p, pairs, *rest) = _turns(q, k, freqs, positions, offset, q_weight, k_weight, eps)
+    t, (B, T, width), args, (freqs_p, pairs, *rest) = _turns(q, k, freqs, positions, offset, q_weight, k_weight, eps)
     device = q.device
     if stream is not None and (done := _under(stream, device, lambda: nna_rotate_heads(q, k, freqs, positions, offset, q_weight, k_weight, eps, interleaved, out))) is not None:
         return done
@@ -1345,7 +1353,7 @@ def nna_rotate_heads_backward(gq, gk, q, k, freqs, positions=None, offset=0, q_w
     The weights' are those of ones where they are not given.  `workspace`: nna_rotate_heads_backward_workspace bytes (taken here if None)."""
     import torch
 
-    t, (B, T, _, heads, width), args, (freqs_p, pairs, *rest) = _turns(q, k, freqs, positions, offset, q_weight, k_weight, eps)
+    t, (B, T, width), args, (freqs_p, pairs, *rest) = _turns(q, k, freqs, positions, offset, q_weight, k_weight, eps)
     device = q.device
     if stream is not None and (done := _under(stream, device, lambda: nna_rotate_heads_backward(gq, gk, q, k, freqs, positions, offset, q_weight, k_weight, eps, interleaved,
                                                                                                 want_weights, workspace))) is not None:
@@ -1379,21 +1387,21 @@ def _gates(x, forget, input, axes):
     """(nna_dtype, x's shape, [x, strides, forget, strides, input, strides]) of [B, (T,) C] tensors."""
     import torch
 
-    t = _type_of(x, "x")
-    if x.dim() != axes:
+    t, dtype, device, shape = _type_of(x, "x"), x.dtype, x.device, x.shape
+    if len(shape) != axes:
         raise TypeError("x must be " + ("[B, T, C]" if axes == 3 else "[B, C]"))
     args = []
-    for name, g in (("x", x), ("forget", forget), ("input", input)):
-        if g is None and name == "input":
-            args += [None, None if axes == 3 else 0]
+    for n, g in enumerate((x, forget, input)):
+        if g is None and n == 2:
+            args += (None, None if axes == 3 else 0)
             continue
-        if not (isinstance(g, torch.Tensor) and g.dtype == x.dtype and g.device == x.device and g.shape == x.shape):
-            raise TypeError(f"{name} must be of x's type and shape, on its device")
+        if g is not x and not (isinstance(g, torch.Tensor) and g.dtype == dtype and g.device == device and g.shape == shape):
+            raise TypeError("forget and input must be of x's type and shape, on its device")
         *s, last = g.stride()
-        if last != 1 and x.shape[-1] != 1:
-            raise TypeError(f"{name}: a frame's channels must lie next to each other")
-        args += [g.data_ptr(), _strides2(*s) if axes == 3 else s[0]]
-    return t, x.shape, args
+        if last != 1 and shape[-1] != 1:
+            raise TypeError("a frame's channels must lie next to each other")
+        args += (g.data_ptr(), _strides2(*s) if axes == 3 else s[0])
+    return t, shape, args
 
 
 def nna_gated_scan_workspace(B: int, T: int, C: int) -> int:
@@ -1477,9 +1485,8 @@ def nna_gated_scan_step(x, forget, state, input=None, out=None, stream=None):
         raise TypeError(f"out must be a contiguous {x.dtype} tensor of shape {(B, C)}")
     else:
         _refuse_overlap(out, x, forget, input, state)
-    for g in (x, forget, input):
-        if g is not None and g.dtype == torch.float32 and _overlap(state, g):
-            raise ValueError("state must not share memory with an input")
+    if t == NNA_F32 and any(g is not None and _overlap(state, g) for g in (x, forget, input)):
+        raise ValueError("state must not share memory with an input")
     _check(lib().nna_gated_scan_step(*args, t, B, C, sp, out.data_ptr(), device.index, _stream_on(device, stream)))
     _written(state, given)
     return out
