@@ -169,6 +169,21 @@ def test_gates_at_their_ends(nb):
         check(nb, x, f, i, go, first, first)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gates_that_forget_in_long_sequences(nb, dtype):
+    """Segments' ends where products of 1 / a pass float32's range: gates of -8 to -200 frame after frame, one frame in eight, or by turns with open ones."""
+    T, C = 1100, 48
+    t = torch.arange(T, device=DEV)[:, None]
+    low = -torch.logspace(0.9, 2.3, C, device=DEV)
+    f = torch.where(torch.arange(C, device=DEV) % 3 == 0, low.expand(T, C), torch.where(torch.arange(C, device=DEV) % 3 == 1, torch.where(t % 8 == 3, low, 3.0), torch.where(t % 2 == 0, low, 9.0)))
+    f[700, ::5] = -float("inf")
+    f = f[None].to(dtype).contiguous()
+    x, go = (torch.randn(1, T, C, device=DEV, generator=torch.Generator(device=DEV).manual_seed(k)).to(dtype) for k in (1, 2))
+    first = torch.randn(1, C, device=DEV)
+    for i in (None, f.flip(-1).contiguous()):
+        check(nb, x, f, i, go, first, first)
+
+
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
 def test_what_is_not_finite_stays_in_its_channel_and_behind_its_frame(nb, value):
     x, f, _, go, first, _ = inputs(2, 300, 70, torch.float32, False, seed=5)
