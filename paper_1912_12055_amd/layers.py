@@ -728,7 +728,10 @@ class AdamW(torch.optim.Optimizer):
                     self._copy(group, written)
             group["step"] += 1
             grads = [g if g is None or g.is_sparse or g.is_contiguous() else g.contiguous() for g in grads]
-            nb.nna_adamw(params, grads, group["m"], group["v"], group["step"], lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
+            lr = group["lr"]
+            if isinstance(lr, torch.Tensor) and not lr.is_cuda:
+                lr = float(lr)
+            nb.nna_adamw(params, grads, group["m"], group["v"], group["step"], lr=lr, betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
                          m_scales=group["m_scales"], v_scales=group["v_scales"], master=group["copies"])
             if group["copies"] is not None:
                 self._versions[n] = [p._version for p in params]

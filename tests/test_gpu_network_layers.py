@@ -265,6 +265,7 @@ def test_adamw_goes_on_from_its_state(layers, bits):
     twins = [torch.nn.Parameter(p) for p in at]
     b = make(twins)
     b.load_state_dict(saved)
+    b.param_groups[0]["lr"] = torch.tensor(b.param_groups[0]["lr"], dtype=torch.float64)  # (in host memory: read as a number)
     for n in range(3, 6):
         step(b, twins, n)
     for p, q in zip(params, twins):
