@@ -335,19 +335,19 @@ nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long lo
   long long at = 0;
   for (long long i = 0; i < count; ++i) {
     const long long pieces = g_dev[i] ? (n[i] + P.piece - 1) / P.piece : 0;
-    // (threads of a launch are counted in 32 bits)
-    if (P.count == ADAMW_TENSORS || (P.count && P.pieces + pieces >= 1LL << 24)) {
-      const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));
-      if (e != hipSuccess) return fail_hip(e, "nna_adamw");
-      P.count = P.pieces = 0;
-    }
     if (pieces) {
+      // (threads of a launch are counted in 32 bits)
+      if (P.count == ADAMW_TENSORS || (P.count && P.pieces + pieces >= 1LL << 24)) {
+        const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));
+        if (e != hipSuccess) return fail_hip(e, "nna_adamw");
+        P.count = P.pieces = 0;
+      }
       P.tensors[P.count++] = {p_dev[i], g_dev[i], n[i], at, P.pieces, types[i]};
       P.pieces += (int)pieces;
     }
     at += (n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
   }
-  const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));  // (there is a tensor: some launch has been left to do)
+  const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));  // (there is a tensor: a launch is left to do, since one before it made room for the next)
   return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_adamw");
 }
 

@@ -292,6 +292,18 @@ def test_many_tensors(nb):
                 assert torch.equal(p, whole)
 
 
+@pytest.mark.parametrize("live,behind", [(80, 1), (80, 100), (79, 3), (160, 2), (81, 1)])
+def test_tensors_without_a_gradient_behind_a_full_launch(nb, live, behind):
+    """80 tensors go into a launch: what lies behind them without a gradient asks for none."""
+    params, grads = tensors((torch.float32, torch.bfloat16), shapes=[(1 + 37 * n % 300,) for n in range(live + behind)])
+    mine, s = [p.clone() for p in params], states(nb, params, 32)
+    nb.nna_adamw(mine, [*grads[:live], *[None] * behind], step=3, **s, **HOW)
+    twin = [p.clone() for p in params[:live]]
+    nb.nna_adamw(twin, grads[:live], step=3, **states(nb, twin, 32), **HOW)
+    for n, p in enumerate(mine):
+        assert torch.equal(p, twin[n] if n < live else params[n]), n
+
+
 def test_views_at_any_place(nb):
     for bits in (32, 8):
         for dtype in (torch.float32, torch.bfloat16):
