@@ -657,8 +657,9 @@ class AdamW(torch.optim.Optimizer):
 
     ``bits=8`` holds the moments in 8 bits, 128 neighbours to a scale: 2.1 bytes a parameter in place of 8.  ``master=True``: 16-bit parameters are updated in float32 copies of
     themselves and rounded from them, so that steps smaller than their own are not lost; where such a parameter is written by something else between two steps (its version
-    counter tells), its copy is taken again.  ``capturable=True`` holds the number of steps in device memory, so that a graph can record ``step`` (after a first step that is not recorded); ``lr`` may
-    then be a float32 CUDA tensor, too.  The states of a group are flat tensors in it (``m``, ``v``, ...), and part of ``state_dict``."""
+    counter tells: not what goes through ``.data``, nor between a graph's replays), its copy is taken again.  ``capturable=True`` holds the number of steps in device memory, so that a
+    graph can record ``step`` (after a first step that is not recorded); ``lr`` may then be a float32 CUDA tensor, too.  The states of a group are flat tensors in it (``m``, ``v``, ...),
+    and part of ``state_dict``."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, bits=32, master=True, capturable=False):
         if bits not in (8, 32):
@@ -720,12 +721,19 @@ class AdamW(torch.optim.Optimizer):
             grads = [p.grad for p in params]
             if not params or all(g is None for g in grads):
                 continue
+            written = ()
+            if "m" in group and group["copies"] is not None and n in self._versions:
+                written = [i for i, (p, v) in enumerate(zip(params, self._versions[n])) if p._version != v]
+            if torch.cuda.is_current_stream_capturing():
+                # what a graph records it does again in each replay: zero the states, take the copies from the rounded parameters, make the same step
+                if "m" not in group or not isinstance(group["step"], torch.Tensor):
+                    raise RuntimeError("a recorded step needs capturable=True, and a step before it that is not recorded")
+                if written:
+                    raise RuntimeError("16-bit parameters were written since the last step: take a step that is not recorded first")
             if "m" not in group:
                 self._begin(group)
-            elif group["copies"] is not None and n in self._versions:
-                written = [i for i, (p, v) in enumerate(zip(params, self._versions[n])) if p._version != v]
-                if written:
-                    self._copy(group, written)
+            elif written:
+                self._copy(group, written)
             group["step"] += 1
             grads = [g if g is None or g.is_sparse or g.is_contiguous() else g.contiguous() for g in grads]
             lr = group["lr"]

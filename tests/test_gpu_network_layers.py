@@ -291,6 +291,44 @@ def test_small_steps_of_16_bit_weights_are_not_lost(layers):
         assert float(p.detach()[0]) == 0.5
 
 
+@pytest.mark.parametrize("case", ["first", "counted", "written", "fine"])
+def test_what_may_not_be_recorded(layers, case):
+    """A first step would zero its states in each replay, one counted in host memory repeat its number, and one behind a write take the float32 copies from rounded weights."""
+    p = torch.nn.Parameter(torch.ones(5, device=DEV, dtype=torch.bfloat16))
+    p.grad = torch.ones_like(p)
+    optimiser = layers.AdamW([p], lr=1e-5, weight_decay=0.0, capturable=case != "counted")
+    if case != "first":
+        optimiser.step()
+    if case == "written":
+        with torch.no_grad():
+            p.fill_(1.0)
+    tick = torch.zeros(1, device=DEV)
+    torch.cuda.synchronize()
+    graph, refused = torch.cuda.CUDAGraph(), False
+    with torch.cuda.graph(graph):
+        tick.add_(1)
+        try:
+            optimiser.step()
+        except RuntimeError as e:
+            refused = "not recorded" in str(e)
+    assert refused == (case != "fine")
+    if case == "first":
+        assert "m" not in optimiser.param_groups[0]
+        return
+    if case == "written":
+        optimiser.step()
+        with torch.cuda.graph(graph := torch.cuda.CUDAGraph()):
+            optimiser.step()
+    if case in ("written", "fine"):
+        before = optimiser.param_groups[0]["copies"][:5].clone()
+        for n in range(3):  # steps of 1e-5, which a bfloat16 one would lose
+            graph.replay()
+            torch.cuda.synchronize()
+            moved = (before - optimiser.param_groups[0]["copies"][:5]).double()
+            # (a float32 below one holds its value to 2^-25 and a step is off by 2^-20 of itself: each of them)
+            assert float((moved - (n + 1) * 1e-5).abs().max()) <= (n + 1) * (2.0**-25 + 2.0**-20 * 1e-5) + 2.0**-25
+
+
 def test_the_kernels_of_a_transform_are_trained(layers):
     """The library's own copy of a layer's weights follows the steps."""
     layer = layers.STFT(n_fft=256, hop_length=64, trainable=True, output_format="Power")
