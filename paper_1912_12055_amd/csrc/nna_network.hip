@@ -298,7 +298,11 @@ nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long lo
     if (!p_dev[i] || p_dev[i] == g_dev[i]) return fail(NNA_ERR_INVALID_ARG, "a tensor is NULL, or its own gradient");
     values += n[i];
   }
-  if (values && (!m_dev || !v_dev || m_dev == v_dev)) return fail(NNA_ERR_INVALID_ARG, "m_dev or v_dev is NULL, or they are the same");
+  if (values && (!m_dev || !v_dev)) return fail(NNA_ERR_INVALID_ARG, "m_dev or v_dev is NULL");
+  const void* states[] = {m_dev, v_dev, m_scales_dev, v_scales_dev, master_dev};
+  for (const void*& a : states)
+    for (const void*& b : states)
+      if (values && a && &a != &b && a == b) return fail(NNA_ERR_INVALID_ARG, "two of the states are the same");
   try {
     // weights that two tensors share would be updated twice at once
     std::vector<std::pair<uintptr_t, uintptr_t>> spans;
