@@ -729,6 +729,8 @@ nna_status nna_gated_scan_step(const void* x_dev, long long x_stride, const void
  *                no two of the states one array
  *   master_dev   [state_size] float32 or NULL: the float32 copies that tensors of 16 bits are updated in and rounded from (float32 tensors have none)
  *   step_dev, lr_dev  NULL, or the step's number (from 1) and lr in device memory in the place of step and lr: for steps recorded into a graph
+ * nna_adamw_steps: the same, with t of each tensor: steps[count] in host memory, or steps_dev[count] in device memory in its place (apart = 1); or one for all, steps[1] or steps_dev[1]
+ * (apart = 0).  A tensor whose gradient comes and goes has taken fewer steps than others: with the others' t its moments would be taken for whole ones.
  * 8 bits: 128 neighbours share a scale s, their largest magnitude.  A code c of m stands for s (c / 127) |c / 127|, rounded to the nearest code; one of v for s (c / 255)^4, rounded
  * down from (255 (v / s)^(1/4) + d), at least 1 where v > 0, d in [0, 1) the fraction (first 24 bits) of (place in v) 0x9E3779B9 + t 0xB504F333 over 2^32.  The update itself
  * uses the moments before they are rounded; they are float64 until then, each product and sum rounded by itself.  A block with a value that is not finite stands for NaN throughout; one below 2^-126 for zero.
@@ -739,6 +741,9 @@ nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long lo
                      float* v_scales_dev, float* master_dev,
                      long long state_size, long long step, const long long* step_dev, double lr, const float* lr_dev, double beta1, double beta2, double eps,
                      double weight_decay, int device, void* hip_stream);
+nna_status nna_adamw_steps(void* const* p_dev, const void* const* g_dev, const long long* n, const int* types, long long count, void* m_dev, void* v_dev, float* m_scales_dev,
+                           float* v_scales_dev, float* master_dev, long long state_size, const long long* steps, const long long* steps_dev, int apart, double lr,
+                           const float* lr_dev, double beta1, double beta2, double eps, double weight_decay, int device, void* hip_stream);
 nna_status nna_adamw_moment(const void* codes_dev, int second, const float* scales_dev, long long size, float* out_dev, int device, void* hip_stream);
 
 void nna_plan_destroy(nna_plan* plan); /* NULL is allowed */

@@ -45,7 +45,7 @@ EXPORTS = [
     "nna_decay_attention_workspace", "nna_decay_attention_backward_workspace", "nna_decay_attention", "nna_decay_attention_backward", "nna_decay_attention_step",
     "nna_rotate_heads", "nna_rotate_heads_backward_workspace", "nna_rotate_heads_backward",
     "nna_gated_scan_workspace", "nna_gated_scan", "nna_gated_scan_backward", "nna_gated_scan_step",
-    "nna_adamw", "nna_adamw_moment",
+    "nna_adamw", "nna_adamw_steps", "nna_adamw_moment",
 ]
 
 _c = ctypes
@@ -146,6 +146,7 @@ def lib():
         L.nna_gated_scan_backward.argtypes = [_VP, _VP, *gates, *frames, _VP, _VP, _VP, _VP, _VP, _VP, _c.c_size_t, _I, _VP]
         L.nna_gated_scan_step.argtypes = [_VP, _LL, _VP, _LL, _VP, _LL, _I, _LL, _LL, _VP, _VP, _I, _VP]
         L.nna_adamw.argtypes = [_VP, _VP, _VP, _VP, _LL, _VP, _VP, _VP, _VP, _VP, _LL, _LL, _VP, _D, _VP, _D, _D, _D, _D, _I, _VP]
+        L.nna_adamw_steps.argtypes = [_VP, _VP, _VP, _VP, _LL, _VP, _VP, _VP, _VP, _VP, _LL, _VP, _VP, _I, _D, _VP, _D, _D, _D, _D, _I, _VP]
         L.nna_adamw_moment.argtypes = [_VP, _I, _VP, _LL, _VP, _I, _VP]
         L.nna_out_shape.argtypes = [_VP, _LL, _LL, _c.POINTER(_LL), _c.POINTER(_LL)]
         for name in ("nna_stft", "nna_mel", "nna_cqt", "nna_cqt1992", "nna_cqt2010v2_static"):
@@ -1506,7 +1507,8 @@ def nna_adamw(params, grads, m, v, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, 
     """One AdamW step over all of `params`, in place: lists of contiguous float32, bfloat16 or float16 CUDA tensors and their gradients, of their types (None: that tensor and its
     states are left alone).  m, v: the moments, flat, a tensor's beginning at nna_adamw_places' multiple of 128: float32, or int8 (m) and uint8 (v) codes with float32
     m_scales, v_scales [values / 128]; zeros before the first step.  master: flat float32 copies of the 16-bit tensors, likewise, which are updated and rounded from.
-    step: the step's number, from 1; step and lr may be CUDA tensors of one value, int64 and float32, read when the step runs (so that a graph can record it)."""
+    step: the step's number, from 1, of all tensors, or a list of each one's own (tensors whose gradients come and go have taken fewer); step and lr may be CUDA tensors, int64 of one
+    value or one for each tensor, and float32 of one value, read when the step runs (so that a graph can record it)."""
     import torch
 
     tensor, f32 = torch.Tensor, torch.float32
@@ -1543,11 +1545,18 @@ def nna_adamw(params, grads, m, v, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, 
             continue
         if not (isinstance(t, tensor) and t.dtype == dtype and t.device == device and t.is_contiguous() and t.numel() == n):
             raise TypeError(f"{name} must be a contiguous {dtype} tensor of {n} values on {device}")
-    step_p = lr_p = None
+    step_p = lr_p = steps = None
+    apart = 0
     if isinstance(step, tensor):
-        if not (step.dtype == torch.int64 and step.device == device and step.numel() == 1):
-            raise TypeError(f"step must be a whole number, or one int64 value on {device}")
-        step_p, step = step.data_ptr(), 0
+        if not (step.dtype == torch.int64 and step.device == device and step.is_contiguous() and step.numel() in (1, count)):
+            raise TypeError(f"step must be a whole number or one for each tensor, or as many int64 values on {device}")
+        step_p, apart = step.data_ptr(), int(step.numel() != 1)
+    elif isinstance(step, (list, tuple)):
+        if len(step) != count:
+            raise ValueError("step must be one number, or one for each tensor")
+        steps, apart = array.array("q", step), 1
+    else:
+        steps = array.array("q", (int(step),))
     if isinstance(lr, tensor):
         if not (lr.dtype == f32 and lr.device == device and lr.numel() == 1):
             raise TypeError(f"lr must be a number, or one float32 value on {device}")
@@ -1555,9 +1564,9 @@ def nna_adamw(params, grads, m, v, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, 
     at = array.array("Q", map(tensor.data_ptr, params))
     at_g = array.array("Q", map(tensor.data_ptr, grads) if live is params else (0 if g is None else g.data_ptr() for g in grads))
     types = array.array("i", [_types[dtypes[0]][0]]) * count if len(set(dtypes)) == 1 else array.array("i", [_types[d][0] for d in dtypes])
-    _check(lib().nna_adamw(*(a.buffer_info()[0] if count else None for a in (at, at_g, sizes, types)), count, m.data_ptr(), v.data_ptr(),
-                           *(None if t is None else t.data_ptr() for t in (m_scales, v_scales, master)), size, int(step), step_p, float(lr), lr_p, float(betas[0]), float(betas[1]),
-                           float(eps), float(weight_decay), device.index, _stream_on(device, stream)))
+    _check(lib().nna_adamw_steps(*(a.buffer_info()[0] if count else None for a in (at, at_g, sizes, types)), count, m.data_ptr(), v.data_ptr(),
+                                 *(None if t is None else t.data_ptr() for t in (m_scales, v_scales, master)), size, None if steps is None else steps.buffer_info()[0], step_p, apart,
+                                 float(lr), lr_p, float(betas[0]), float(betas[1]), float(eps), float(weight_decay), device.index, _stream_on(device, stream)))
     _all_written([*live, *(t for t in (m, v, m_scales, v_scales, master) if t is not None)])
 
 

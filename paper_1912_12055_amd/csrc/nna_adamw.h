@@ -12,6 +12,7 @@ struct AdamwTensor {
   void* p;
   const void* g;
   long long n, at;  // values, and where their states begin
+  long long step;   // its number of steps with this one; with step_dev, where that is in it
   int first, type;  // the first of its pieces in the launch
 };
 
@@ -23,9 +24,8 @@ struct AdamwParams {
   float *m_scales, *v_scales;
   float* master;                 // float32 copies of 16-bit tensors, or NULL
   double beta1, beta2;
-  const long long* step_dev;     // or NULL: step
+  const long long* step_dev;     // or NULL: the tensors' step
   const float* lr_dev;           // or NULL: lr
-  long long step;
   double lr, weight_decay;
   float eps;
 };

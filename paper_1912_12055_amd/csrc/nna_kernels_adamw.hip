@@ -329,7 +329,7 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(AdamwParams P) {
   }
   const AdamwTensor tensor = P.tensors[low];
   const long long from = (long long)((int)blockIdx.x - tensor.first) * P.piece;
-  const long long t = P.step_dev ? *P.step_dev : P.step;
+  const long long t = P.step_dev ? P.step_dev[tensor.step] : tensor.step;
   const double lr = P.lr_dev ? (double)*P.lr_dev : P.lr;
   Factors F;
   F.keep = (float)(1. - lr * P.weight_decay);

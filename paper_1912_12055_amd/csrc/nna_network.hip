@@ -282,9 +282,19 @@ nna_status nna_gated_scan_step(const void* x_dev, long long x_stride, const void
 nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long long* n, const int* types, long long count, void* m_dev, void* v_dev, float* m_scales_dev,
                      float* v_scales_dev, float* master_dev, long long state_size, long long step, const long long* step_dev, double lr, const float* lr_dev, double beta1,
                      double beta2, double eps, double weight_decay, int device, void* hip_stream) {
+  return nna_adamw_steps(p_dev, g_dev, n, types, count, m_dev, v_dev, m_scales_dev, v_scales_dev, master_dev, state_size, &step, step_dev, 0, lr, lr_dev, beta1, beta2, eps,
+                         weight_decay, device, hip_stream);
+}
+
+nna_status nna_adamw_steps(void* const* p_dev, const void* const* g_dev, const long long* n, const int* types, long long count, void* m_dev, void* v_dev, float* m_scales_dev,
+                           float* v_scales_dev, float* master_dev, long long state_size, const long long* steps, const long long* steps_dev, int apart, double lr,
+                           const float* lr_dev, double beta1, double beta2, double eps, double weight_decay, int device, void* hip_stream) {
   if (count < 0 || state_size < 0 || (count && (!p_dev || !g_dev || !n || !types))) return fail(NNA_ERR_INVALID_ARG, "count or state_size is negative, or an array is NULL");
   if (!m_scales_dev != !v_scales_dev) return fail(NNA_ERR_INVALID_ARG, "m_scales_dev and v_scales_dev come together");
-  if (!step_dev && step < 1) return fail(NNA_ERR_INVALID_ARG, "step counts from 1");
+  if (apart != 0 && apart != 1) return fail(NNA_ERR_INVALID_ARG, "apart is 0 (one number of steps for all tensors) or 1 (each its own)");
+  if (!steps && !steps_dev && (count || !apart)) return fail(NNA_ERR_INVALID_ARG, "steps is NULL");
+  const auto step_of = [&](long long i) { return steps_dev ? i * apart : steps[i * apart]; };  // ... or where it is
+  if (!steps_dev && !apart && steps[0] < 1) return fail(NNA_ERR_INVALID_ARG, "steps count from 1");
   if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return fail(NNA_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
   if (!(eps >= 0.0) || eps > 3.0e38) return fail(NNA_ERR_INVALID_ARG, "eps must be finite and not negative");
   if ((!lr_dev && !(std::fabs(lr) < 1e30)) || !(std::fabs(weight_decay) < 1e30)) return fail(NNA_ERR_INVALID_ARG, "lr and weight_decay must be finite");
@@ -295,6 +305,7 @@ nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long lo
     size += (n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
     if (size > state_size) return fail(NNA_ERR_INVALID_ARG, "a tensor's state ends behind state_size");
     if (!n[i] || !g_dev[i]) continue;
+    if (!steps_dev && step_of(i) < 1) return fail(NNA_ERR_INVALID_ARG, "steps count from 1");
     if (!p_dev[i] || p_dev[i] == g_dev[i]) return fail(NNA_ERR_INVALID_ARG, "a tensor is NULL, or its own gradient");
     values += n[i];
   }
@@ -328,9 +339,8 @@ nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long lo
   P.master = master_dev;
   P.beta1 = beta1;
   P.beta2 = beta2;
-  P.step_dev = step_dev;
+  P.step_dev = steps_dev;
   P.lr_dev = lr_dev;
-  P.step = step;
   P.lr = lr;
   P.weight_decay = weight_decay;
   P.eps = (float)eps;
@@ -346,7 +356,7 @@ nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long lo
         if (e != hipSuccess) return fail_hip(e, "nna_adamw");
         P.count = P.pieces = 0;
       }
-      P.tensors[P.count++] = {p_dev[i], g_dev[i], n[i], at, P.pieces, types[i]};
+      P.tensors[P.count++] = {p_dev[i], g_dev[i], n[i], at, step_of(i), P.pieces, types[i]};
       P.pieces += (int)pieces;
     }
     at += (n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;

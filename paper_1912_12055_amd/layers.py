@@ -657,7 +657,8 @@ class AdamW(torch.optim.Optimizer):
 
     ``bits=8`` holds the moments in 8 bits, 128 neighbours to a scale: 2.1 bytes a parameter in place of 8.  ``master=True``: 16-bit parameters are updated in float32 copies of
     themselves and rounded from them, so that steps smaller than their own are not lost; where such a parameter is written by something else between two steps (its version
-    counter tells: not what goes through ``.data``, nor between a graph's replays), its copy is taken again.  ``capturable=True`` holds the number of steps in device memory, so that a
+    counter tells: not what goes through ``.data``, nor between a graph's replays), its copy is taken again.  Each tensor counts the steps that it has had a gradient for (``steps`` of
+    its group), which its moments are corrected by.  ``capturable=True`` holds the numbers of steps in device memory, so that a
     graph can record ``step`` (after a first step that is not recorded); ``lr`` may then be a float32 CUDA tensor, too.  The states of a group are flat tensors in it (``m``, ``v``, ...),
     and part of ``state_dict``."""
 
@@ -689,10 +690,17 @@ class AdamW(torch.optim.Optimizer):
         group["m_scales"], group["v_scales"] = (torch.zeros(size // nb.NNA_BLOCK8, device=device) if codes else None for _ in range(2))
         narrow = group["master"] and any(p.dtype != torch.float32 for p in params)
         group["copies"] = torch.zeros(size, device=device) if narrow else None
+        self._count(group)
         if group["capturable"]:
             group["step"] = torch.full((1,), int(group["step"]), dtype=torch.int64, device=device)
         if narrow:
             self._copy(group, range(len(params)))
+
+    @staticmethod
+    def _count(group):
+        """The tensors' own numbers of steps, where there are none yet: the group's."""
+        params, step = group["params"], int(group["step"])
+        group["steps"] = torch.full((len(params),), step, dtype=torch.int64, device=params[0].device) if group["capturable"] else [step] * len(params)
 
     @staticmethod
     def _copy(group, which):
@@ -705,7 +713,9 @@ class AdamW(torch.optim.Optimizer):
     def load_state_dict(self, state_dict):
         super().load_state_dict(state_dict)
         for group in self.param_groups:
-            for name in ("m", "v", "m_scales", "v_scales", "copies", "step"):
+            if "m" in group and "steps" not in group:
+                self._count(group)
+            for name in ("m", "v", "m_scales", "v_scales", "copies", "step", "steps"):
                 if isinstance(group.get(name), torch.Tensor):
                     group[name] = group[name].to(group["params"][0].device)
         self._versions = {}
@@ -735,11 +745,17 @@ class AdamW(torch.optim.Optimizer):
             elif written:
                 self._copy(group, written)
             group["step"] += 1
+            if not isinstance(group["steps"], torch.Tensor):
+                group["steps"] = [n + (g is not None) for n, g in zip(group["steps"], grads)]
+            elif all(g is not None for g in grads):
+                group["steps"] += 1
+            else:
+                torch._foreach_add_([one for one, g in zip(group["steps"].unbind(), grads) if g is not None], 1)
             grads = [g if g is None or g.is_sparse or g.is_contiguous() else g.contiguous() for g in grads]
             lr = group["lr"]
             if isinstance(lr, torch.Tensor) and not lr.is_cuda:
                 lr = float(lr)
-            nb.nna_adamw(params, grads, group["m"], group["v"], group["step"], lr=lr, betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
+            nb.nna_adamw(params, grads, group["m"], group["v"], group["steps"], lr=lr, betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
                          m_scales=group["m_scales"], v_scales=group["v_scales"], master=group["copies"])
             if group["copies"] is not None:
                 self._versions[n] = [p._version for p in params]
