@@ -657,7 +657,8 @@ class AdamW(torch.optim.Optimizer):
 
     ``bits=8`` holds the moments in 8 bits, 128 neighbours to a scale: 2.1 bytes a parameter in place of 8.  ``master=True``: 16-bit parameters are updated in float32 copies of
     themselves and rounded from them, so that steps smaller than their own are not lost; where such a parameter is written by something else between two steps (its version
-    counter tells: not what goes through ``.data``, nor between a graph's replays), its copy is taken again.  Each tensor counts the steps that it has had a gradient for (``steps`` of
+    counter tells: not what goes through ``.data``, nor between a graph's replays), its copy is taken again.  So it is where the first step behind a load, or of a copy of the optimiser, finds a
+    parameter that its copy does not round to.  Each tensor counts the steps that it has had a gradient for (``steps`` of
     its group), which its moments are corrected by.  ``capturable=True`` holds the numbers of steps in device memory, so that a
     graph can record ``step`` (after a first step that is not recorded); ``lr`` may then be a float32 CUDA tensor, too.  The states of a group are flat tensors in it (``m``, ``v``, ...),
     and part of ``state_dict``."""
@@ -710,6 +711,16 @@ class AdamW(torch.optim.Optimizer):
             if params[i].dtype != torch.float32:
                 group["copies"][at[i] : at[i] + params[i].numel()].copy_(params[i].detach().flatten())
 
+    @staticmethod
+    def _compare(group):
+        """Copies of parameters whose versions nobody has followed are taken again where the parameter is not the copy rounded.  (Those that are keep what a load brought.)"""
+        params = group["params"]
+        at, _ = nb.nna_adamw_places([p.numel() for p in params])
+        for i, p in enumerate(params):
+            if p.dtype != torch.float32:
+                copy, now = group["copies"][at[i] : at[i] + p.numel()], p.detach().flatten()
+                copy.copy_(torch.where((copy.to(p.dtype) == now).all(), copy, now.float()))
+
     def load_state_dict(self, state_dict):
         super().load_state_dict(state_dict)
         for group in self.param_groups:
@@ -731,17 +742,19 @@ class AdamW(torch.optim.Optimizer):
             grads = [p.grad for p in params]
             if not params or all(g is None for g in grads):
                 continue
-            written = ()
-            if "m" in group and group["copies"] is not None and n in self._versions:
+            written, unknown = (), "m" in group and group["copies"] is not None and n not in self._versions
+            if "m" in group and group["copies"] is not None and not unknown:
                 written = [i for i, (p, v) in enumerate(zip(params, self._versions[n])) if p._version != v]
             if torch.cuda.is_current_stream_capturing():
                 # what a graph records it does again in each replay: zero the states, take the copies from the rounded parameters, make the same step
                 if "m" not in group or not isinstance(group["step"], torch.Tensor):
                     raise RuntimeError("a recorded step needs capturable=True, and a step before it that is not recorded")
-                if written:
-                    raise RuntimeError("16-bit parameters were written since the last step: take a step that is not recorded first")
+                if written or unknown:
+                    raise RuntimeError("16-bit parameters were written, or states loaded, since the last step: take a step that is not recorded first")
             if "m" not in group:
                 self._begin(group)
+            elif unknown:
+                self._compare(group)
             elif written:
                 self._copy(group, written)
             group["step"] += 1

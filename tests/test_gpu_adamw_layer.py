@@ -4,6 +4,7 @@ Tolerances against a loop in 64 bits are those of a step in 32 bits: a step of o
 steps take both over.
 """
 import copy
+import pickle
 
 import pytest
 import torch
@@ -107,3 +108,63 @@ def test_counts_are_part_of_the_state(layers, bits):
         step(b, twins, t)
     for p, q in zip(params, twins):
         assert torch.equal(p, q)
+
+
+def _stepped(layers, value=1.0, steps=3):
+    """A bfloat16 parameter and its optimiser, whose float32 copy is between two bfloat16 values"""
+    p = torch.nn.Parameter(torch.full((300,), value, device=DEV, dtype=torch.bfloat16))
+    optimiser = layers.AdamW([p], lr=1e-4, weight_decay=0.0)
+    for _ in range(steps):
+        p.grad = torch.ones_like(p)
+        optimiser.step()
+    return p, optimiser
+
+
+@pytest.mark.parametrize("way", ["loaded", "copied", "pickled"])
+@pytest.mark.parametrize("write", [None, "all", "some", "same"])
+def test_weights_written_behind_a_load(layers, way, write):
+    """A 16-bit weight that is not what its float32 copy rounds to has been written by something else: the step goes on from it.  One that is keeps its copy."""
+    p, optimiser = _stepped(layers)
+    if way == "loaded":
+        q = torch.nn.Parameter(p.detach().clone())
+        other = layers.AdamW([q], lr=1e-4, weight_decay=0.0)
+        other.load_state_dict(copy.deepcopy(optimiser.state_dict()))
+    else:
+        q, other = copy.deepcopy((p, optimiser)) if way == "copied" else pickle.loads(pickle.dumps((p, optimiser)))
+        q = other.param_groups[0]["params"][0]
+    was = other.param_groups[0]["copies"][:300].clone()
+    assert float(was[0]) == float(optimiser.param_groups[0]["copies"][0]) and float(was[0]) != float(q.detach()[0])
+    start = was.double()
+    with torch.no_grad():
+        if write == "all":
+            q.fill_(0.5)
+            start = q.double()
+        elif write == "some":
+            q[7:9] = 0.25
+            start = q.double()
+        elif write == "same":
+            q.copy_(q.clone())  # (its own values again: other weights' loading, as a checkpoint does it)
+    q.grad = torch.ones_like(q)
+    other.step()
+    got = other.param_groups[0]["copies"][:300].double()
+    # a steady gradient's step is lr: 1e-4 off by 2^-20 of itself, the copy by half a step of a value below 1
+    assert float((got - (start - 1e-4)).abs().max()) <= 2.0**-25 + 1e-4 * 2.0**-20
+    assert torch.equal(q.detach(), got.bfloat16())
+
+
+def test_a_load_is_not_recorded(layers):
+    """Behind a load the copies are compared with the weights first: not in a graph, whose replays would do it again."""
+    p = torch.nn.Parameter(torch.ones(5, device=DEV, dtype=torch.bfloat16))
+    optimiser = layers.AdamW([p], lr=1e-4, capturable=True)
+    p.grad = torch.ones_like(p)
+    optimiser.step()
+    optimiser.load_state_dict(copy.deepcopy(optimiser.state_dict()))
+    torch.cuda.synchronize()
+    tick, refused = torch.zeros(1, device=DEV), False
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        tick.add_(1)
+        try:
+            optimiser.step()
+        except RuntimeError as e:
+            refused = "not recorded" in str(e)
+    assert refused
