@@ -737,6 +737,7 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        capturing, todo = torch.cuda.is_current_stream_capturing(), []
         for n, group in enumerate(self.param_groups):
             params = group["params"]
             grads = [p.grad for p in params]
@@ -745,31 +746,43 @@ class AdamW(torch.optim.Optimizer):
             written, unknown = (), "m" in group and group["copies"] is not None and n not in self._versions
             if "m" in group and group["copies"] is not None and not unknown:
                 written = [i for i, (p, v) in enumerate(zip(params, self._versions[n])) if p._version != v]
-            if torch.cuda.is_current_stream_capturing():
+            if capturing:
                 # what a graph records it does again in each replay: zero the states, take the copies from the rounded parameters, make the same step
                 if "m" not in group or not isinstance(group["step"], torch.Tensor):
                     raise RuntimeError("a recorded step needs capturable=True, and a step before it that is not recorded")
                 if written or unknown:
                     raise RuntimeError("16-bit parameters were written, or states loaded, since the last step: take a step that is not recorded first")
+            todo.append((n, group, grads, written, unknown))
+        for n, group, grads, written, unknown in todo:
             if "m" not in group:
                 self._begin(group)
             elif unknown:
                 self._compare(group)
             elif written:
                 self._copy(group, written)
-            group["step"] += 1
-            if not isinstance(group["steps"], torch.Tensor):
-                group["steps"] = [n + (g is not None) for n, g in zip(group["steps"], grads)]
-            elif all(g is not None for g in grads):
-                group["steps"] += 1
-            else:
-                torch._foreach_add_([one for one, g in zip(group["steps"].unbind(), grads) if g is not None], 1)
-            grads = [g if g is None or g.is_sparse or g.is_contiguous() else g.contiguous() for g in grads]
-            lr = group["lr"]
-            if isinstance(lr, torch.Tensor) and not lr.is_cuda:
-                lr = float(lr)
-            nb.nna_adamw(params, grads, group["m"], group["v"], group["steps"], lr=lr, betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
-                         m_scales=group["m_scales"], v_scales=group["v_scales"], master=group["copies"])
+            self._step_group(group, grads)
             if group["copies"] is not None:
-                self._versions[n] = [p._version for p in params]
+                self._versions[n] = [p._version for p in group["params"]]
         return loss
+
+    @staticmethod
+    def _step_group(group, grads):
+        """One step of a group's tensors; one that is refused leaves the numbers of steps as they were."""
+        lr, steps = group["lr"], group["steps"]
+        if isinstance(lr, torch.Tensor) and not lr.is_cuda:
+            lr = float(lr)
+        if isinstance(steps, torch.Tensor):
+            counts = [group["step"], steps] if all(g is not None for g in grads) else [group["step"], *(one for one, g in zip(steps.unbind(), grads) if g is not None)]
+            torch._foreach_add_(counts, 1)
+        else:
+            steps = [n + (g is not None) for n, g in zip(steps, grads)]
+        try:
+            grads = [g if g is None or g.is_sparse or g.is_contiguous() else g.contiguous() for g in grads]
+            nb.nna_adamw(group["params"], grads, group["m"], group["v"], steps, lr=lr, betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
+                         m_scales=group["m_scales"], v_scales=group["v_scales"], master=group["copies"])
+        except BaseException:
+            if isinstance(steps, torch.Tensor):
+                torch._foreach_add_(counts, -1)
+            raise
+        if not isinstance(steps, torch.Tensor):
+            group["steps"], group["step"] = steps, group["step"] + 1

@@ -168,3 +168,50 @@ def test_a_load_is_not_recorded(layers):
         except RuntimeError as e:
             refused = "not recorded" in str(e)
     assert refused
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+def test_a_refused_step_does_not_count(layers, capturable):
+    p, q = (torch.nn.Parameter(torch.ones(300, device=DEV)) for _ in range(2))
+    a, b = (layers.AdamW([x], lr=1e-2, bits=8, capturable=capturable) for x in (p, q))
+    for t in range(4):
+        grad = torch.randn(300, device=DEV, generator=_gen(t))
+        for x in (p, q):
+            x.grad = grad.clone()
+        # (a rate that is no number, and a decay that is none)
+        for name in ("lr", "weight_decay") if t != 1 else ():
+            was = a.param_groups[0][name]
+            a.param_groups[0][name] = float("nan")
+            with pytest.raises(Exception):
+                a.step()
+            a.param_groups[0][name] = was
+        p.grad = torch.ones(300, device=DEV).to_sparse()
+        with pytest.raises(TypeError):
+            a.step()
+        p.grad = grad.clone()
+        a.step()
+        b.step()
+        assert torch.equal(p, q) and int(a.param_groups[0]["step"]) == t + 1, t
+    for name in ("m", "v", "m_scales", "v_scales"):
+        assert torch.equal(a.param_groups[0][name], b.param_groups[0][name])
+
+
+def test_a_step_is_recorded_whole_or_not_at_all(layers):
+    """Groups of which one may not be recorded: nothing of the others is."""
+    p, q = (torch.nn.Parameter(torch.ones(300, device=DEV)) for _ in range(2))
+    optimiser = layers.AdamW([dict(params=[p]), dict(params=[q], capturable=False)], lr=1e-2, capturable=True)
+    for x in (p, q):
+        x.grad = torch.ones_like(x)
+    optimiser.step()
+    was, tick, refused = p.detach().clone(), torch.zeros(1, device=DEV), False
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tick.add_(1)
+        try:
+            optimiser.step()
+        except RuntimeError as e:
+            refused = "not recorded" in str(e)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert refused and torch.equal(p.detach(), was) and int(optimiser.param_groups[0]["step"]) == 1
