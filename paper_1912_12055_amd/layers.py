@@ -671,7 +671,10 @@ class AdamW(torch.optim.Optimizer):
 
     def add_param_group(self, group):
         super().add_param_group(group)
-        params = self.param_groups[-1]["params"]
+        params, bits = self.param_groups[-1]["params"], self.param_groups[-1]["bits"]
+        if bits not in (8, 32):
+            self.param_groups.pop()
+            raise ValueError("bits: 8 or 32, of each group")
         for p in params:
             if not p.is_cuda or p.device != params[0].device or p.dtype not in (torch.float32, torch.bfloat16, torch.float16) or not p.is_contiguous():
                 self.param_groups.pop()

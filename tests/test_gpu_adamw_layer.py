@@ -215,3 +215,15 @@ def test_a_step_is_recorded_whole_or_not_at_all(layers):
     graph.replay()
     torch.cuda.synchronize()
     assert refused and torch.equal(p.detach(), was) and int(optimiser.param_groups[0]["step"]) == 1
+
+
+@pytest.mark.parametrize("bits", [16, 4, 0, None, "8"])
+def test_bits_of_a_group(layers, bits):
+    p, q = (torch.nn.Parameter(torch.ones(3, device=DEV)) for _ in range(2))
+    with pytest.raises(ValueError, match="bits"):
+        layers.AdamW([dict(params=[p], bits=bits)])
+    optimiser = layers.AdamW([dict(params=[p], bits=8)])
+    with pytest.raises(ValueError, match="bits"):
+        optimiser.add_param_group(dict(params=[q], bits=bits))
+    assert len(optimiser.param_groups) == 1
+    optimiser.add_param_group(dict(params=[q], bits=32))
