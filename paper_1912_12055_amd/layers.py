@@ -593,6 +593,8 @@ class RotaryHeads(torch.nn.Module):
         dev = torch.device("cuda", _device_index(device))
         self.width, self.eps, self.interleaved = int(width), None if eps is None else float(eps), bool(interleaved)
         rotary = self.width // 2 * 2 if rotary is None else int(rotary)
+        if isinstance(freqs, torch.Tensor) and freqs.requires_grad:
+            raise ValueError("freqs are constants of the layer: no gradient is taken")
         # no buffer: a module's .bfloat16() would take the angles' precision with the weights'
         self._freqs = nb.nna_rotary_freqs(rotary, base, scale, device=dev) if freqs is None else torch.as_tensor(freqs, dtype=torch.float64).to(dev).contiguous()
         if self._freqs.dim() != 1 or not 2 * self._freqs.numel() <= self.width:

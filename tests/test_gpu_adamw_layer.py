@@ -227,3 +227,14 @@ def test_bits_of_a_group(layers, bits):
         optimiser.add_param_group(dict(params=[q], bits=bits))
     assert len(optimiser.param_groups) == 1
     optimiser.add_param_group(dict(params=[q], bits=32))
+
+
+def test_frequencies_are_constants(layers):
+    """No gradient is taken of them: one that is asked for is refused."""
+    f = torch.ones(4, device=DEV, dtype=torch.float64).requires_grad_()
+    with pytest.raises(ValueError, match="constant"):
+        layers.RotaryHeads(8, freqs=f)
+    with pytest.raises(ValueError, match="constant"):
+        layers.RotaryHeads(8, freqs=torch.nn.Parameter(torch.ones(4)))
+    with torch.no_grad():
+        layers.RotaryHeads(8, freqs=f.detach())
