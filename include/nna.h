@@ -724,9 +724,9 @@ nna_status nna_gated_scan_step(const void* x_dev, long long x_stride, const void
  * One AdamW step over `count` tensors:  m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,  p <- (1 - lr wd) p - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps).
  *   p_dev, g_dev, n, types  [count] in host memory (read during the call): of each tensor its n values, updated, and their gradient (NULL: this tensor and its states are left alone), both
  *                contiguous and of the nna_dtype types[i]; n may be 0.  A tensor's states are n values of m and v; the first tensor's begin at 0, the next one's at the multiple of 128
- *                behind them, and so on.  No two tensors may share memory
- *   m_dev, v_dev [state_size] float32 (state_size: where the tensor behind the last one's would begin), m_scales_dev and v_scales_dev NULL; or int8 (m) and uint8 (v) codes with float32 scales [state_size / 128].  Zeros before the first step;
- *                no two of the states one array
+ *                behind them, and so on.  What is written (tensors, states) shares no memory with anything else of the call: refused, but gradients
+ *                over states by nna_adamw_steps alone
+ *   m_dev, v_dev [state_size] float32 (state_size: where the tensor behind the last one's would begin), m_scales_dev and v_scales_dev NULL; or int8 (m) and uint8 (v) codes with float32 scales [state_size / 128].  Zeros before the first step
  *   master_dev   [state_size] float32 or NULL: the float32 copies that tensors of 16 bits are updated in and rounded from (float32 tensors have none)
  *   step_dev, lr_dev  NULL, or the step's number (from 1) and lr in device memory in the place of step and lr: for steps recorded into a graph
  * nna_adamw_steps: the same, with t of each tensor: steps[count] in host memory, or steps_dev[count] in device memory in its place (apart = 1); or one for all, steps[1] or steps_dev[1]

@@ -108,6 +108,133 @@ nna_status check_scan_workspace(const void* workspace, size_t bytes, size_t need
   return NNA_OK;
 }
 
+// ---- the optimiser's step ----
+
+struct Span {
+  uintptr_t from, to;
+  bool operator<(const Span& o) const { return from < o.from; }
+};
+Span span_of(const void* p, long long bytes) { return {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes}; }
+// sorts them
+bool disjoint(std::vector<Span>& spans) {
+  if (!std::is_sorted(spans.begin(), spans.end())) std::sort(spans.begin(), spans.end());
+  for (size_t i = 1; i < spans.size(); ++i)
+    if (spans[i].from < spans[i - 1].to) return false;
+  return true;
+}
+// whether one shares memory with a span of `others`, which disjoint() has sorted
+bool meets(const Span& s, const std::vector<Span>& others) {
+  const auto behind = std::lower_bound(others.begin(), others.end(), Span{s.to, s.to});
+  return behind != others.begin() && (behind - 1)->to > s.from;
+}
+
+struct AdamwCall {
+  void* const* p;
+  const void* const* g;
+  const long long* n;
+  const int* types;
+  long long count;
+  void *m, *v;
+  float *m_scales, *v_scales, *master;
+  long long state_size;
+  const long long *steps, *steps_dev;
+  int apart;
+  double lr;
+  const float* lr_dev;
+  double beta1, beta2, eps, weight_decay;
+};
+
+// What a workgroup writes no other one may read or write: weights, states, and (states_too, of gradients) what is read beside them.  `size` values of states
+nna_status refuse_shared(const AdamwCall& c, long long size, bool states_too) {
+  std::vector<Span> weights, all, grads;
+  weights.reserve((size_t)c.count);
+  grads.reserve((size_t)c.count);
+  for (long long i = 0; i < c.count; ++i) {
+    if (!c.n[i] || !c.g[i]) continue;
+    const long long bytes = c.n[i] * (c.types[i] == NNA_F32 ? 4 : 2);
+    weights.push_back(span_of(c.p[i], bytes));
+    grads.push_back(span_of(c.g[i], bytes));
+  }
+  if (!disjoint(weights)) return fail(NNA_ERR_INVALID_ARG, "two tensors share memory");
+  if (weights.empty()) return NNA_OK;
+  all.reserve(weights.size() + 5);
+  all = weights;
+  const long long value = c.m_scales ? 1 : 4, blocks = size / ADAMW_BLOCK;
+  for (const Span& s : {span_of(c.m, size * value), span_of(c.v, size * value), span_of(c.m_scales, blocks * 4), span_of(c.v_scales, blocks * 4), span_of(c.master, size * 4)})
+    if (s.from) all.push_back(s);
+  if (!disjoint(all)) return fail(NNA_ERR_INVALID_ARG, "two of the states, or a state and a tensor, share memory");
+  for (const Span& g : grads)
+    if (meets(g, states_too ? all : weights)) return fail(NNA_ERR_INVALID_ARG, "a gradient shares memory with what the step writes");
+  if (c.lr_dev && meets(span_of(c.lr_dev, 4), all)) return fail(NNA_ERR_INVALID_ARG, "lr_dev is in what the step writes");
+  if (c.steps_dev && meets(span_of(c.steps_dev, (c.apart ? c.count : 1) * 8), all)) return fail(NNA_ERR_INVALID_ARG, "the numbers of steps are in what the step writes");
+  return NNA_OK;
+}
+
+nna_status adamw(const AdamwCall& c, bool states_too, int device, void* hip_stream) {
+  if (c.count < 0 || c.state_size < 0 || (c.count && (!c.p || !c.g || !c.n || !c.types))) return fail(NNA_ERR_INVALID_ARG, "count or state_size is negative, or an array is NULL");
+  if (!c.m_scales != !c.v_scales) return fail(NNA_ERR_INVALID_ARG, "m_scales_dev and v_scales_dev come together");
+  if (c.apart != 0 && c.apart != 1) return fail(NNA_ERR_INVALID_ARG, "apart is 0 (one number of steps for all tensors) or 1 (each its own)");
+  if (!c.steps && !c.steps_dev && (c.count || !c.apart)) return fail(NNA_ERR_INVALID_ARG, "steps is NULL");
+  const auto step_of = [&](long long i) { return c.steps_dev ? i * c.apart : c.steps[i * c.apart]; };  // ... or where it is
+  if (!c.steps_dev && !c.apart && c.steps[0] < 1) return fail(NNA_ERR_INVALID_ARG, "steps count from 1");
+  if (!(c.beta1 >= 0.0 && c.beta1 < 1.0 && c.beta2 >= 0.0 && c.beta2 < 1.0)) return fail(NNA_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
+  if (!(c.eps >= 0.0) || c.eps > 3.0e38) return fail(NNA_ERR_INVALID_ARG, "eps must be finite and not negative");
+  if ((!c.lr_dev && !(std::fabs(c.lr) < 1e30)) || !(std::fabs(c.weight_decay) < 1e30)) return fail(NNA_ERR_INVALID_ARG, "lr and weight_decay must be finite");
+  long long size = 0, values = 0;
+  for (long long i = 0; i < c.count; ++i) {
+    if (!known_type(c.types[i])) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
+    if (c.n[i] < 0 || c.n[i] > (1LL << 36)) return fail(NNA_ERR_SHAPE, "a tensor's number of values is negative or too large");
+    size += (c.n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
+    if (size > c.state_size) return fail(NNA_ERR_INVALID_ARG, "a tensor's state ends behind state_size");
+    if (!c.n[i] || !c.g[i]) continue;
+    if (!c.steps_dev && step_of(i) < 1) return fail(NNA_ERR_INVALID_ARG, "steps count from 1");
+    if (!c.p[i] || c.p[i] == c.g[i]) return fail(NNA_ERR_INVALID_ARG, "a tensor is NULL, or its own gradient");
+    values += c.n[i];
+  }
+  if (values && (!c.m || !c.v)) return fail(NNA_ERR_INVALID_ARG, "m_dev or v_dev is NULL");
+  try {
+    const nna_status shared = refuse_shared(c, size, states_too);
+    if (shared != NNA_OK) return shared;
+  } catch (const std::exception&) {
+    return fail(NNA_ERR_ALLOC, "out of host memory");
+  }
+  DeviceGuard guard;
+  const nna_status s = enter_device(guard, device);
+  if (s != NNA_OK || !values) return s;
+  AdamwParams P;
+  P.m = c.m;
+  P.v = c.v;
+  P.m_scales = c.m_scales;
+  P.v_scales = c.v_scales;
+  P.master = c.master;
+  P.beta1 = c.beta1;
+  P.beta2 = c.beta2;
+  P.step_dev = c.steps_dev;
+  P.lr_dev = c.lr_dev;
+  P.lr = c.lr;
+  P.weight_decay = c.weight_decay;
+  P.eps = (float)c.eps;
+  P.piece = adamw_piece(values);
+  P.count = P.pieces = 0;
+  long long at = 0;
+  for (long long i = 0; i < c.count; ++i) {
+    const long long pieces = c.g[i] ? (c.n[i] + P.piece - 1) / P.piece : 0;
+    if (pieces) {
+      // (threads of a launch are counted in 32 bits)
+      if (P.count == ADAMW_TENSORS || (P.count && P.pieces + pieces >= 1LL << 24)) {
+        const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));
+        if (e != hipSuccess) return fail_hip(e, "nna_adamw");
+        P.count = P.pieces = 0;
+      }
+      P.tensors[P.count++] = {c.p[i], c.g[i], c.n[i], at, step_of(i), P.pieces, c.types[i]};
+      P.pieces += (int)pieces;
+    }
+    at += (c.n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
+  }
+  const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));  // (there is a tensor: a launch is left to do, since one before it made room for the next)
+  return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_adamw");
+}
+
 }  // namespace
 
 extern "C" {
@@ -282,87 +409,15 @@ nna_status nna_gated_scan_step(const void* x_dev, long long x_stride, const void
 nna_status nna_adamw(void* const* p_dev, const void* const* g_dev, const long long* n, const int* types, long long count, void* m_dev, void* v_dev, float* m_scales_dev,
                      float* v_scales_dev, float* master_dev, long long state_size, long long step, const long long* step_dev, double lr, const float* lr_dev, double beta1,
                      double beta2, double eps, double weight_decay, int device, void* hip_stream) {
-  return nna_adamw_steps(p_dev, g_dev, n, types, count, m_dev, v_dev, m_scales_dev, v_scales_dev, master_dev, state_size, &step, step_dev, 0, lr, lr_dev, beta1, beta2, eps,
-                         weight_decay, device, hip_stream);
+  return adamw({p_dev, g_dev, n, types, count, m_dev, v_dev, m_scales_dev, v_scales_dev, master_dev, state_size, &step, step_dev, 0, lr, lr_dev, beta1, beta2, eps, weight_decay}, false,
+               device, hip_stream);
 }
 
 nna_status nna_adamw_steps(void* const* p_dev, const void* const* g_dev, const long long* n, const int* types, long long count, void* m_dev, void* v_dev, float* m_scales_dev,
                            float* v_scales_dev, float* master_dev, long long state_size, const long long* steps, const long long* steps_dev, int apart, double lr,
                            const float* lr_dev, double beta1, double beta2, double eps, double weight_decay, int device, void* hip_stream) {
-  if (count < 0 || state_size < 0 || (count && (!p_dev || !g_dev || !n || !types))) return fail(NNA_ERR_INVALID_ARG, "count or state_size is negative, or an array is NULL");
-  if (!m_scales_dev != !v_scales_dev) return fail(NNA_ERR_INVALID_ARG, "m_scales_dev and v_scales_dev come together");
-  if (apart != 0 && apart != 1) return fail(NNA_ERR_INVALID_ARG, "apart is 0 (one number of steps for all tensors) or 1 (each its own)");
-  if (!steps && !steps_dev && (count || !apart)) return fail(NNA_ERR_INVALID_ARG, "steps is NULL");
-  const auto step_of = [&](long long i) { return steps_dev ? i * apart : steps[i * apart]; };  // ... or where it is
-  if (!steps_dev && !apart && steps[0] < 1) return fail(NNA_ERR_INVALID_ARG, "steps count from 1");
-  if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0)) return fail(NNA_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
-  if (!(eps >= 0.0) || eps > 3.0e38) return fail(NNA_ERR_INVALID_ARG, "eps must be finite and not negative");
-  if ((!lr_dev && !(std::fabs(lr) < 1e30)) || !(std::fabs(weight_decay) < 1e30)) return fail(NNA_ERR_INVALID_ARG, "lr and weight_decay must be finite");
-  long long size = 0, values = 0;
-  for (long long i = 0; i < count; ++i) {
-    if (!known_type(types[i])) return fail(NNA_ERR_INVALID_ARG, "unknown nna_dtype");
-    if (n[i] < 0 || n[i] > (1LL << 36)) return fail(NNA_ERR_SHAPE, "a tensor's number of values is negative or too large");
-    size += (n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
-    if (size > state_size) return fail(NNA_ERR_INVALID_ARG, "a tensor's state ends behind state_size");
-    if (!n[i] || !g_dev[i]) continue;
-    if (!steps_dev && step_of(i) < 1) return fail(NNA_ERR_INVALID_ARG, "steps count from 1");
-    if (!p_dev[i] || p_dev[i] == g_dev[i]) return fail(NNA_ERR_INVALID_ARG, "a tensor is NULL, or its own gradient");
-    values += n[i];
-  }
-  if (values && (!m_dev || !v_dev)) return fail(NNA_ERR_INVALID_ARG, "m_dev or v_dev is NULL");
-  const void* states[] = {m_dev, v_dev, m_scales_dev, v_scales_dev, master_dev};
-  for (const void*& a : states)
-    for (const void*& b : states)
-      if (values && a && &a != &b && a == b) return fail(NNA_ERR_INVALID_ARG, "two of the states are the same");
-  try {
-    // weights that two tensors share would be updated twice at once
-    std::vector<std::pair<uintptr_t, uintptr_t>> spans;
-    spans.reserve((size_t)count);
-    for (long long i = 0; i < count; ++i) {
-      const uintptr_t p = reinterpret_cast<uintptr_t>(p_dev[i]);
-      if (n[i] && g_dev[i]) spans.emplace_back(p, p + (uintptr_t)n[i] * (types[i] == NNA_F32 ? 4 : 2));
-    }
-    if (!std::is_sorted(spans.begin(), spans.end())) std::sort(spans.begin(), spans.end());
-    for (size_t i = 1; i < spans.size(); ++i)
-      if (spans[i].first < spans[i - 1].second) return fail(NNA_ERR_INVALID_ARG, "two tensors share memory");
-  } catch (const std::exception&) {
-    return fail(NNA_ERR_ALLOC, "out of host memory");
-  }
-  DeviceGuard guard;
-  const nna_status s = enter_device(guard, device);
-  if (s != NNA_OK || !values) return s;
-  AdamwParams P;
-  P.m = m_dev;
-  P.v = v_dev;
-  P.m_scales = m_scales_dev;
-  P.v_scales = v_scales_dev;
-  P.master = master_dev;
-  P.beta1 = beta1;
-  P.beta2 = beta2;
-  P.step_dev = steps_dev;
-  P.lr_dev = lr_dev;
-  P.lr = lr;
-  P.weight_decay = weight_decay;
-  P.eps = (float)eps;
-  P.piece = adamw_piece(values);
-  P.count = P.pieces = 0;
-  long long at = 0;
-  for (long long i = 0; i < count; ++i) {
-    const long long pieces = g_dev[i] ? (n[i] + P.piece - 1) / P.piece : 0;
-    if (pieces) {
-      // (threads of a launch are counted in 32 bits)
-      if (P.count == ADAMW_TENSORS || (P.count && P.pieces + pieces >= 1LL << 24)) {
-        const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));
-        if (e != hipSuccess) return fail_hip(e, "nna_adamw");
-        P.count = P.pieces = 0;
-      }
-      P.tensors[P.count++] = {p_dev[i], g_dev[i], n[i], at, step_of(i), P.pieces, types[i]};
-      P.pieces += (int)pieces;
-    }
-    at += (n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
-  }
-  const hipError_t e = launch_adamw(P, static_cast<hipStream_t>(hip_stream));  // (there is a tensor: a launch is left to do, since one before it made room for the next)
-  return e == hipSuccess ? NNA_OK : fail_hip(e, "nna_adamw");
+  return adamw({p_dev, g_dev, n, types, count, m_dev, v_dev, m_scales_dev, v_scales_dev, master_dev, state_size, steps, steps_dev, apart, lr, lr_dev, beta1, beta2, eps, weight_decay}, true,
+               device, hip_stream);
 }
 
 nna_status nna_adamw_moment(const void* codes_dev, int second, const float* scales_dev, long long size, float* out_dev, int device, void* hip_stream) {
