@@ -733,7 +733,7 @@ nna_status nna_gated_scan_step(const void* x_dev, long long x_stride, const void
  * (apart = 0).  A tensor whose gradient comes and goes has taken fewer steps than others: with the others' t its moments would be taken for whole ones.
  * 8 bits: 128 neighbours share a scale s, their largest magnitude.  A code c of m stands for s (c / 127) |c / 127|, rounded to the nearest code; one of v for s (c / 255)^4, rounded
  * down from (255 (v / s)^(1/4) + d), at least 1 where v > 0, d in [0, 1) the fraction (first 24 bits) of (place in v) 0x9E3779B9 + t 0xB504F333 over 2^32.  The update itself
- * uses the moments before they are rounded; they are float64 until then, each product and sum rounded by itself.  A block with a value that is not finite stands for NaN throughout; one below 2^-126 for zero.
+ * uses the moments before they are rounded, in float32; codes and scales are those of moments in float64, each product and sum rounded by itself.  A block with a value that is not finite stands for NaN throughout; one below 2^-126 for zero.
  * nna_adamw_moment: out_dev [size] float32 = what the codes of m, or (second != 0) of v, stand for; size a multiple of 128.
  * Errors: NNA_ERR_INVALID_ARG, NNA_ERR_SHAPE, NNA_ERR_ALLOC.  A value that is not finite reaches its own weight (8 bits: its block's).
  */

@@ -110,6 +110,9 @@ __device__ __forceinline__ void store_codes(unsigned char* p, int n, const Codes
 
 // One moment of a lane's eight values in 8 bits: what was, and what is now, in float32 and in 64 bits, as the definition has it.
 constexpr float TINY = 0x1p-80f;  // below it products of float32 may have lost their last bits: everything is made in 64 then
+// Whether a factor of the codes' powers has no normal float32, though what it makes of the larger codes has one: what was is then read in 64 bits (else a block's history, scales below 2^-94
+// of second moments and 2^-112 of first ones, fades out of its weights: steps up to 1 / sqrt(1 - b2) too long where eps is as small)
+__device__ __forceinline__ bool faded(float factor, float scale, double beta) { return factor < 0x1p-126f && scale > 0.f && beta > 0.; }
 struct First {
   Codes was;  // their highest bits turned: 0..255 for -128..127
   float scale, old, fresh;
@@ -258,6 +261,12 @@ __device__ __forceinline__ void update(const AdamwParams& P, const AdamwTensor& 
       m[i] = first.now(i, d.v[i]);
       v[i] = second.now(i, d.v[i]);
     }
+    if (__builtin_expect(faded(first.old, first.scale, P.beta1), 0))
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) m[i] = (float)first.exact(i, d.v[i]);
+    if (__builtin_expect(faded(second.old, second.scale, P.beta2), 0))
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) v[i] = (float)second.exact(i, d.v[i]);
     const float most_m = scale_of<FULL>(first, m, d, n), most_v = scale_of<FULL>(second, v, d, n);
     // a block with a value that is not finite stands for NaN throughout, so that none is lost; one without a normal float32 is zero
     const bool some_m = most_m >= 0x1p-126f && most_m < __builtin_inff(), some_v = most_v >= 0x1p-126f && most_v < __builtin_inff();
