@@ -6,8 +6,10 @@
 // c = A c' + E for c_t = a_t e_t).  So a wave takes FRAMES frames of 64 lanes' channels into registers and makes their A and H, the waves of a workgroup exchange those
 // through LDS, and each walks its frames again from its own first state: every array is read or written once.
 //
-// A channel that remembers for thousands of frames has a within 2^-12 of one, where a float32 holds a itself to 2^-13 of its distance from one.  So 1 - a = sigmoid(-f) is
-// computed too, and a is held as the nearest float32 and what that leaves: products of thousands of them are off by their own roundings alone.
+// A channel that remembers for thousands of frames has a within 2^-12 of one, where a float32 holds a to 2^-13 of its distance from one; and where its gate is steady every frame's, every run's
+// and every segment's product is rounded the same way: over 16,384 frames what is left of a first state would be off by 5 10^-4 (runs' products as one float32 each), and by 10^-4 at the median.
+// So 1 - a = sigmoid(-f) is computed too, and of what is passed on, a run's A, also Q = 1 - A: Q <- Q + q (1 - Q) with q = 1 - a, and the state goes through A as the nearest float32 and what that
+// leaves: 5 10^-6, and 4 10^-7 at the median.  Inside of a run, whose products end there, a and A are one float32.
 #include "nna_scan.h"
 #include "nna_vector.h"
 
@@ -19,6 +21,7 @@ namespace {
 // result; a 16-bit v is itself off by far more.  (minimum and maximum let a NaN through.)
 struct Gate {
   float on, off;
+  __device__ __forceinline__ Gate where(bool here) const { return {here ? on : 1.f, here ? off : 0.f}; }  // a frame that takes no part leaves the state as it is
 };
 template <typename T>
 __device__ __forceinline__ float exp_of_minus(T v) {
@@ -39,17 +42,35 @@ __device__ __forceinline__ Gate gate(T v) {
   return {r, e * r};
 }
 
-// a as a float32 and what it leaves of it
-struct Stay {
-  float a, rest;
-  __device__ __forceinline__ Stay() {}
-  __device__ __forceinline__ Stay(Gate g, bool here) {
-    a = here ? g.on : 1.f;
-    rest = here && g.on >= 0.5f ? (1.f - g.on) - g.off : 0.f;  // (the first difference is exact there; below a half a float32 holds a to its own 2^-24)
+// A product A of gates and 1 - A, each to float32's own precision of itself, the second without the first's roundings: Q + q (1 - Q)
+struct Product {
+  float a = 1.f, q = 0.f;
+  __device__ __forceinline__ void by(float on, float off) {
+    q += __builtin_fmaf(-off, q, off);
+    a *= on;
   }
-  __device__ __forceinline__ float of(float h) const { return __builtin_fmaf(a, h, rest * h); }
-  __device__ __forceinline__ float of(float h, float add) const { return __builtin_fmaf(a, h, __builtin_fmaf(rest, h, add)); }
+  // what the float32 a leaves of A (the first difference is exact from a half on, and below it A is held to its own 2^-24): of a as it was rounded, so no product is fused into it
+  __device__ __forceinline__ float rest() const {
+#pragma clang fp contract(off)
+    return a >= 0.5f ? (1.f - a) - q : 0.f;
+  }
+  __device__ __forceinline__ static Product of(float a, float rest) {
+    Product p;
+    p.a = a;
+    p.q = (1.f - a) - rest;
+    return p;
+  }
+  // the one of the two that is below a half as one number: A, or -(1 - A), with its sign set also where it is zero
+  __device__ __forceinline__ float code() const { return a >= 0.5f ? -q : a; }
+  __device__ __forceinline__ static Product of_code(float code) {
+    Product p;
+    p.a = __builtin_signbit(code) ? 1.f + code : code;
+    p.q = __builtin_signbit(code) ? -code : 1.f - code;
+    return p;
+  }
 };
+// A h + add
+__device__ __forceinline__ float through(float a, float rest, float h, float add) { return __builtin_fmaf(a, h, __builtin_fmaf(rest, h, add)); }
 
 // A workgroup's lanes: CL neighbours along the channels, V channels each, 64 / CL runs of FRAMES frames in a wave, WAVES waves behind one another.
 template <int CL, int FRAMES, int WAVES>
@@ -72,61 +93,65 @@ struct Rows {
   __device__ __forceinline__ T at(int k, int c) const { return vec_at<V>(v[k], c); }
 };
 
-// A run's A and H alone, for segments' ends.  With d = 1 / a = 1 + e^-f and D the product of the d so far the sums have no quotient in their recurrences,
-//   D_t = D_{t-1} + e^-f D_{t-1},   G_t = G_{t-1} + u x D_t  (u = 1 - a: + e^-f x D_{t-1}),   A = 1 / D,   H = G / D   (backwards E = sum of g_t / D_t),
-// and D takes a small e^-f as it is: 13 instructions a value in place of 30.  Where D or G comes near float32's largest value (gates that all but forget frame after frame, and what is not
+// A run's A and H alone, for segments' ends.  With d = 1 / a = 1 + e^-f and D = 1 + M the product of the d so far the sums have no quotient in their recurrences,
+//   M_t = M_{t-1} + e^-f D_{t-1},   G_t = G_{t-1} + u x D_t  (u = 1 - a: + e^-f x D_{t-1}),   A = 1 / D,   1 - A = M / D,   H = G / D   (backwards E = sum of g_t / D_t):
+// 14 instructions a value in place of 30.  Where D or G comes near float32's largest value (gates that all but forget frame after frame, and what is not
 // finite) the run is walked by a and 1 - a.
 constexpr float ENDS_MOST = 0x1p124f;
 template <bool INPUT, typename T, int V, int FRAMES>
-__device__ __forceinline__ void run_ends(const Rows<T, V, FRAMES>& rx, const Rows<T, V, FRAMES>& rf, const Rows<T, V, FRAMES>& ri, int here /* frames taken */, float (&A)[V], float (&H)[V]) {
+__device__ __forceinline__ void run_ends(const Rows<T, V, FRAMES>& rx, const Rows<T, V, FRAMES>& rf, const Rows<T, V, FRAMES>& ri, int here /* frames taken */, Product (&A)[V], float (&H)[V]) {
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    float D = 1.f, G = 0.f;
+    float D = 1.f, M = 0.f, G = 0.f;
 #pragma unroll
     for (int k = 0; k < FRAMES; ++k) {
       const float e = k < here ? exp_of_minus(rf.at(k, c)) : 0.f;
       if (INPUT) {
-        D = __builtin_fmaf(e, D, D);
+        M = __builtin_fmaf(e, D, M);
+        D = 1.f + M;
         G = __builtin_fmaf(k < here ? gate(ri.at(k, c)).on * (float)rx.at(k, c) : 0.f, D, G);
       } else {
         G = __builtin_fmaf(k < here ? e * (float)rx.at(k, c) : 0.f, D, G);
-        D = __builtin_fmaf(e, D, D);
+        M = __builtin_fmaf(e, D, M);
+        D = 1.f + M;
       }
     }
-    A[c] = __builtin_amdgcn_rcpf(D);
-    H[c] = G * A[c];
+    A[c].a = __builtin_amdgcn_rcpf(D);
+    A[c].q = M * A[c].a;
+    H[c] = G * A[c].a;
     if (__builtin_expect(!(D + __builtin_fabsf(G) < ENDS_MOST), 0)) {
-      A[c] = 1.f, H[c] = 0.f;
+      A[c] = Product(), H[c] = 0.f;
 #pragma unroll
       for (int k = 0; k < FRAMES; ++k) {
-        const Gate a = gate(rf.at(k, c));
-        const Stay stay(a, k < here);
-        A[c] = stay.of(A[c]);
-        H[c] = stay.of(H[c], k < here ? (INPUT ? gate(ri.at(k, c)).on : a.off) * (float)rx.at(k, c) : 0.f);
+        const Gate a = gate(rf.at(k, c)).where(k < here);
+        A[c].by(a.on, a.off);
+        H[c] = __builtin_fmaf(a.on, H[c], k < here ? (INPUT ? gate(ri.at(k, c)).on : a.off) * (float)rx.at(k, c) : 0.f);
       }
     }
   }
 }
 template <typename T, int V, int FRAMES>
-__device__ __forceinline__ void run_ends_back(const Rows<T, V, FRAMES>& rf, const Rows<T, V, FRAMES>& rg, int here, float (&A)[V], float (&E)[V]) {
+__device__ __forceinline__ void run_ends_back(const Rows<T, V, FRAMES>& rf, const Rows<T, V, FRAMES>& rg, int here, Product (&A)[V], float (&E)[V]) {
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    float D = 1.f;
+    float D = 1.f, M = 0.f;
     E[c] = 0.f;
 #pragma unroll
     for (int k = 0; k < FRAMES; ++k) {
       const float e = k < here ? exp_of_minus(rf.at(k, c)) : 0.f;
-      D = __builtin_fmaf(e, D, D);
-      A[c] = __builtin_amdgcn_rcpf(D);
-      E[c] = __builtin_fmaf(k < here ? (float)rg.at(k, c) : 0.f, A[c], E[c]);
+      M = __builtin_fmaf(e, D, M);
+      D = 1.f + M;
+      A[c].a = __builtin_amdgcn_rcpf(D);
+      E[c] = __builtin_fmaf(k < here ? (float)rg.at(k, c) : 0.f, A[c].a, E[c]);
     }
+    A[c].q = M * A[c].a;
     if (__builtin_expect(!(D < ENDS_MOST), 0)) {
-      A[c] = 1.f, E[c] = 0.f;
+      A[c] = Product(), E[c] = 0.f;
 #pragma unroll
       for (int k = FRAMES - 1; k >= 0; --k) {
-        const Stay stay(gate(rf.at(k, c)), k < here);
-        A[c] = stay.of(A[c]);
-        E[c] = stay.of(E[c] + (k < here ? (float)rg.at(k, c) : 0.f));
+        const Gate a = gate(rf.at(k, c)).where(k < here);
+        A[c].by(a.on, a.off);
+        E[c] = a.on * (E[c] + (k < here ? (float)rg.at(k, c) : 0.f));
       }
     }
   }
@@ -178,18 +203,19 @@ __device__ __forceinline__ Two halves_of(float v) {
 // it (behind_a, behind_e), and all of them (all).
 template <int CL>
 struct Joined {
-  float before_a, before_h, behind_a, behind_e, all_a, all_h, all_e;
+  float before_a, before_h, behind_a, behind_e, all_h, all_e;
+  Product all;
   template <bool FORWARD, bool BACKWARD>
-  __device__ __forceinline__ void join(float a, float h, float e) {
+  __device__ __forceinline__ void join(Product a, float h, float e) {
     before_a = behind_a = 1.f;
     before_h = behind_e = 0.f;
-    all_a = a, all_h = h, all_e = e;
+    all = a, all_h = h, all_e = e;
     if constexpr (CL <= 16) step<FORWARD, BACKWARD>(threadIdx.x & 16, rows_of);
     if constexpr (CL <= 32) step<FORWARD, BACKWARD>(threadIdx.x & 32, halves_of);
   }
   template <bool FORWARD, bool BACKWARD, typename F>
   __device__ __forceinline__ void step(bool upper, F two) {
-    const Two A = two(all_a);
+    const Two A = two(all.a), Q = two(all.q);
     if (FORWARD) {
       const Two H = two(all_h);
       before_h = upper ? __builtin_fmaf(before_a, H.low, before_h) : before_h;
@@ -202,32 +228,34 @@ struct Joined {
       behind_a = upper ? behind_a : behind_a * A.high;
       all_e = __builtin_fmaf(A.low, E.high, E.low);
     }
-    all_a = A.low * A.high;
+    all.q = Q.low + __builtin_fmaf(-Q.high, Q.low, Q.high);
+    all.a = A.low * A.high;
   }
 };
 
 // What the waves of a workgroup tell each other, a column's side by side: two buffers in turn, so that the next round's writes never meet a wave that still reads this one.
+typedef float Quad __attribute__((ext_vector_type(4)));
 template <int V, int CL, int WAVES>
 struct alignas(16) Told {
   float at[2][V][CL][WAVES];
+  __device__ __forceinline__ Quad four(int turn, int c, int column, int w) const { return *reinterpret_cast<const Quad*>(&at[turn][c][column][w]); }
   __device__ __forceinline__ void get(int turn, int c, int column, float (&to)[WAVES]) const {
-    typedef float quad __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int w = 0; w < WAVES; w += 4) {
-      const quad q = *reinterpret_cast<const quad*>(&at[turn][c][column][w]);
+      const Quad q = four(turn, c, column, w);
 #pragma unroll
       for (int k = 0; k < 4; ++k) to[w + k] = q[k];
     }
   }
 };
 
-// Forward.  ENDS: no outputs, but what each segment makes of the state before it, P.parts[b][segment][a, h][C]; the mix composes those of the segments before its own.
+// Forward.  ENDS: no outputs, but what each segment makes of the state before it, P.parts[b][segment][A (coded), h][C]; the mix composes those of the segments before its own.
 // The next round's loads are asked for when this one's values have been used, half a round ahead.  16 x 4,096 frames of 2,048 channels, bfloat16: 170 us, 4.7 TB/s of the 5.1 that a copy
 // reaches; 4 x 16,384 (rows of half lines): 193 us.  With D and G of run_ends here, too, it takes a third of the instructions less, 143 registers, and is no faster.
 template <typename T, int V, int CL, int FRAMES, int WAVES, bool INPUT, bool ENDS>
 __global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
   typedef Shape<CL, FRAMES, WAVES> S;
-  __shared__ Told<V, CL, WAVES> told_a, told_h;
+  __shared__ Told<V, CL, WAVES> told_a, told_rest, told_h;
   const Part part = part_of<CL, V>(P);
   const long long b = part.b;
   const int channel = part.channel, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = threadIdx.x % CL, run = (threadIdx.x & 63) / CL;
@@ -240,24 +268,24 @@ __global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
   const int begin = part.segment * P.segment_frames, end = begin + P.segment_frames < P.T ? begin + P.segment_frames : P.T;
   const int used = n < end ? n : end;  // frames up to here are taken
   const int kept_rows = (P.T + SCAN_KEPT - 1) / SCAN_KEPT;
-  float state[V], factor[V];
+  float state[V];
+  Product factor[V];
 #pragma unroll
-  for (int c = 0; c < V; ++c) {
-    factor[c] = 1.f;
-    state[c] = !ENDS && P.first ? P.first[b * P.C + channel + c] : 0.f;
-  }
+  for (int c = 0; c < V; ++c) state[c] = !ENDS && P.first ? P.first[b * P.C + channel + c] : 0.f;
   if (!ENDS && part.segment) {
     // the segments before this one, shared out among the runs
     const int each = (part.segment + S::RUNS * WAVES - 1) / (S::RUNS * WAVES), from = (wave * S::RUNS + run) * each, to = from + each < part.segment ? from + each : part.segment;
-    float A[V], H[V];
+    Product A[V];
+    float H[V];
 #pragma unroll
-    for (int c = 0; c < V; ++c) A[c] = 1.f, H[c] = 0.f;
+    for (int c = 0; c < V; ++c) H[c] = 0.f;
     for (int s = from; s < to; ++s) {
       const float* p = P.parts + (b * P.segments + s) * 2 * P.C + channel;
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        H[c] = __builtin_fmaf(p[c], H[c], p[P.C + c]);
-        A[c] *= p[c];
+        const Product of = Product::of_code(p[c]);
+        H[c] = through(of.a, of.rest(), H[c], p[P.C + c]);
+        A[c].by(of.a, of.q);
       }
     }
 #pragma unroll
@@ -265,18 +293,20 @@ __global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
       Joined<CL> joined;
       joined.template join<true, false>(A[c], H[c], 0.f);
       if (run == 0) {
-        told_a.at[1][c][column][wave] = joined.all_a;
+        told_a.at[1][c][column][wave] = joined.all.a;
+        told_rest.at[1][c][column][wave] = joined.all.rest();
         told_h.at[1][c][column][wave] = joined.all_h;
       }
     }
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      float as[WAVES], hs[WAVES];
+      float as[WAVES], rests[WAVES], hs[WAVES];
       told_a.get(1, c, column, as);
+      told_rest.get(1, c, column, rests);
       told_h.get(1, c, column, hs);
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) state[c] = __builtin_fmaf(as[w], state[c], hs[w]);
+      for (int w = 0; w < WAVES; ++w) state[c] = through(as[w], rests[w], state[c], hs[w]);
     }
   }
   Rows<T, V, FRAMES> rx, rf, ri;
@@ -296,21 +326,21 @@ __global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
   const auto round = [&](int first, int turn, auto full) {
     constexpr bool FULL = full.value;  // all frames of the round are taken
     const int t = first + wave * S::WAVE + run * FRAMES;
-    float As[FRAMES][V], Hs[FRAMES][V], A[V], H[V];  // of the run's frames up to each
+    float As[FRAMES][V], Hs[FRAMES][V], H[V];  // of the run's frames up to each
+    Product A[V];
 #pragma unroll
-    for (int c = 0; c < V; ++c) A[c] = 1.f, H[c] = 0.f;
+    for (int c = 0; c < V; ++c) H[c] = 0.f;
     if (ENDS) run_ends<INPUT>(rx, rf, ri, FULL ? FRAMES : used - t, A, H);
 #pragma unroll
     for (int k = 0; k < (ENDS ? 0 : FRAMES); ++k)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
         const bool here = FULL || t + k < used;
-        const Gate a = gate(rf.at(k, c));
+        const Gate a = gate(rf.at(k, c)).where(here);
         const float u = INPUT ? gate(ri.at(k, c)).on : a.off;
-        const Stay stay(a, here);
-        A[c] = stay.of(A[c]);
-        H[c] = stay.of(H[c], here ? u * (float)rx.at(k, c) : 0.f);
-        As[k][c] = A[c], Hs[k][c] = H[c];
+        A[c].by(a.on, a.off);
+        H[c] = __builtin_fmaf(a.on, H[c], here ? u * (float)rx.at(k, c) : 0.f);
+        As[k][c] = A[c].a, Hs[k][c] = H[c];
       }
     if (first + S::ROUND < used) load(first + S::ROUND);
     Joined<CL> joined[V];
@@ -318,23 +348,27 @@ __global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
     for (int c = 0; c < V; ++c) {
       joined[c].template join<true, false>(A[c], H[c], 0.f);
       if (run == 0) {
-        told_a.at[turn][c][column][wave] = joined[c].all_a;
+        told_a.at[turn][c][column][wave] = joined[c].all.a;
+        told_rest.at[turn][c][column][wave] = joined[c].all.rest();
         told_h.at[turn][c][column][wave] = joined[c].all_h;
       }
     }
     __syncthreads();
+    if (ENDS && wave) return;  // (the first wave's state is the segment's)
     float h[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      float as[WAVES], hs[WAVES];
-      told_a.get(turn, c, column, as);
-      told_h.get(turn, c, column, hs);
       h[c] = state[c];
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        state[c] = __builtin_fmaf(as[w], state[c], hs[w]);
-        if (ENDS) factor[c] *= as[w];
-        if (w + 1 == wave) h[c] = state[c];
+      for (int w = 0; w < WAVES; w += 4) {
+        const Quad as = told_a.four(turn, c, column, w), rests = told_rest.four(turn, c, column, w), hs = told_h.four(turn, c, column, w);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          state[c] = through(as[k], rests[k], state[c], hs[k]);
+          if (ENDS) factor[c].by(as[k], Product::of(as[k], rests[k]).q);
+          if (w + k + 1 == wave) h[c] = state[c];
+        }
+        if (INPUT && !ENDS) __builtin_amdgcn_sched_barrier(0);  // (the next four asked for now would take the registers that a second workgroup has its place by: 132 of 128)
       }
       h[c] = __builtin_fmaf(joined[c].before_a, h[c], joined[c].before_h);
     }
@@ -366,7 +400,7 @@ __global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
     if (threadIdx.x >= CL) return;
     float* p = P.parts + (b * P.segments + part.segment) * 2 * P.C + channel;
 #pragma unroll
-    for (int c = 0; c < V; ++c) p[c] = factor[c], p[P.C + c] = state[c];
+    for (int c = 0; c < V; ++c) p[c] = factor[c].code(), p[P.C + c] = state[c];
     return;
   }
   if (P.last && part.segment == P.segments - 1 && threadIdx.x < CL)
@@ -378,12 +412,12 @@ __global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
   for (t += threadIdx.x / CL; t < end; t += WAVES * 64 / CL) vec_store<V>(out + (long long)t * P.C, zero);
 }
 
-// Backward, from the last frame to the first; the states inside a round are made again from the kept one.  ENDS: what each segment makes of the carry behind it, P.parts[b][segment][a, e][C].
+// Backward, from the last frame to the first; the states inside a round are made again from the kept one.  ENDS: what each segment makes of the carry behind it, P.parts[b][segment][A (coded), e][C].
 // 16 x 4,096 frames of 2,048 channels, bfloat16: 316 us, 4.2 TB/s; 4 x 16,384: 364 us.  Rounds of eight frames a lane need 230 registers and more, half as many 150.
 template <typename T, int V, int CL, int FRAMES, int WAVES, bool INPUT, bool ENDS>
 __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P) {
   typedef Shape<CL, FRAMES, WAVES> S;
-  __shared__ Told<V, CL, WAVES> told_a, told_h, told_e;
+  __shared__ Told<V, CL, WAVES> told_a, told_rest, told_h, told_e;
   const Part part = part_of<CL, V>(P);
   const long long b = part.b;
   const int channel = part.channel, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = threadIdx.x % CL, run = (threadIdx.x & 63) / CL;
@@ -398,26 +432,26 @@ __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P)
   const int begin = part.segment * P.segment_frames, end = begin + P.segment_frames < P.T ? begin + P.segment_frames : P.T;
   const int used = n < end ? n : end;
   const int kept_rows = (P.T + SCAN_KEPT - 1) / SCAN_KEPT;
-  float carry[V], factor[V];  // a e of the frame behind
+  float carry[V];  // a e of the frame behind
+  Product factor[V];
 #pragma unroll
-  for (int c = 0; c < V; ++c) {
-    factor[c] = 1.f;
-    carry[c] = !ENDS && P.glast ? P.glast[b * P.C + channel + c] : 0.f;
-  }
+  for (int c = 0; c < V; ++c) carry[c] = !ENDS && P.glast ? P.glast[b * P.C + channel + c] : 0.f;
   const int behind = P.segments - 1 - part.segment;
   if (!ENDS && behind) {
     // the segments behind this one, shared out among the runs
     const int each = (behind + S::RUNS * WAVES - 1) / (S::RUNS * WAVES), from = part.segment + 1 + (wave * S::RUNS + run) * each;
     const int to = from + each < P.segments ? from + each : P.segments;
-    float A[V], E[V];
+    Product A[V];
+    float E[V];
 #pragma unroll
-    for (int c = 0; c < V; ++c) A[c] = 1.f, E[c] = 0.f;
+    for (int c = 0; c < V; ++c) E[c] = 0.f;
     for (int s = to - 1; s >= from; --s) {
       const float* p = P.parts + (b * P.segments + s) * 2 * P.C + channel;
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        E[c] = __builtin_fmaf(p[c], E[c], p[P.C + c]);
-        A[c] *= p[c];
+        const Product of = Product::of_code(p[c]);
+        E[c] = through(of.a, of.rest(), E[c], p[P.C + c]);
+        A[c].by(of.a, of.q);
       }
     }
 #pragma unroll
@@ -425,18 +459,20 @@ __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P)
       Joined<CL> joined;
       joined.template join<false, true>(A[c], 0.f, E[c]);
       if (run == 0) {
-        told_a.at[1][c][column][wave] = joined.all_a;
+        told_a.at[1][c][column][wave] = joined.all.a;
+        told_rest.at[1][c][column][wave] = joined.all.rest();
         told_e.at[1][c][column][wave] = joined.all_e;
       }
     }
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      float as[WAVES], es[WAVES];
+      float as[WAVES], rests[WAVES], es[WAVES];
       told_a.get(1, c, column, as);
+      told_rest.get(1, c, column, rests);
       told_e.get(1, c, column, es);
 #pragma unroll
-      for (int w = WAVES - 1; w >= 0; --w) carry[c] = __builtin_fmaf(as[w], carry[c], es[w]);
+      for (int w = WAVES - 1; w >= 0; --w) carry[c] = through(as[w], rests[w], carry[c], es[w]);
     }
   }
   const int rounds = used > begin ? (used - begin + S::ROUND - 1) / S::ROUND : 0;
@@ -468,12 +504,12 @@ __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P)
   const auto round = [&](int first, int turn, auto full) {
     constexpr bool FULL = full.value;
     const int t = first + wave * S::WAVE + run * FRAMES;
-    Stay stay[FRAMES][V];
-    float off[FRAMES][V], take[FRAMES][V], take_slope[FRAMES][V], in[FRAMES][V], go[FRAMES][V], before[FRAMES][V];
-    float A[V], H[V], E[V], h[V];
+    float on[FRAMES][V], off[FRAMES][V], take[FRAMES][V], take_slope[FRAMES][V], in[FRAMES][V], go[FRAMES][V], before[FRAMES][V];
+    Product A[V];
+    float H[V], E[V], h[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      A[c] = 1.f, H[c] = 0.f, E[c] = 0.f;
+      H[c] = 0.f, E[c] = 0.f;
       if (!ENDS) {
         const int row = (first + (wave - wave % S::KEPT_WAVES) * S::WAVE) / SCAN_KEPT;
         h[c] = FULL || row < kept_rows ? P.kept[(b * kept_rows + row) * P.C + channel + c] : 0.f;
@@ -485,11 +521,11 @@ __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
         const bool here = FULL || t + k < used;
-        const Gate a = gate(rf.at(k, c));
-        stay[k][c] = Stay(a, here);
+        const Gate a = gate(rf.at(k, c)).where(here);
+        on[k][c] = a.on;
         go[k][c] = here ? (float)rg.at(k, c) : 0.f;
         // (the slope a (1 - a) is made of these two where it is used)
-        off[k][c] = here ? a.off : 0.f;
+        off[k][c] = a.off;
         in[k][c] = here ? (float)rx.at(k, c) : 0.f;
         if (INPUT) {
           const Gate u = gate(ri.at(k, c));
@@ -498,30 +534,33 @@ __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P)
         } else {
           take[k][c] = off[k][c];
         }
-        A[c] = stay[k][c].of(A[c]);
-        H[c] = stay[k][c].of(H[c], take[k][c] * in[k][c]);
+        A[c].by(a.on, a.off);
+        H[c] = __builtin_fmaf(a.on, H[c], take[k][c] * in[k][c]);
       }
 #pragma unroll
     for (int k = ENDS ? -1 : FRAMES - 1; k >= 0; --k)
 #pragma unroll
-      for (int c = 0; c < V; ++c) E[c] = stay[k][c].of(E[c] + go[k][c]);
+      for (int c = 0; c < V; ++c) E[c] = on[k][c] * (E[c] + go[k][c]);
     if (first > begin) load(first - S::ROUND);
     Joined<CL> joined[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
       joined[c].template join<!ENDS, true>(A[c], H[c], E[c]);
       if (run == 0) {
-        told_a.at[turn][c][column][wave] = joined[c].all_a;
+        told_a.at[turn][c][column][wave] = joined[c].all.a;
+        told_rest.at[turn][c][column][wave] = joined[c].all.rest();
         if (!ENDS) told_h.at[turn][c][column][wave] = joined[c].all_h;
         told_e.at[turn][c][column][wave] = joined[c].all_e;
       }
     }
     __syncthreads();
+    if (ENDS && wave) return;  // (the first wave's carry is the segment's)
     float e[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      float as[WAVES], es[WAVES];
+      float as[WAVES], rests[WAVES], es[WAVES];
       told_a.get(turn, c, column, as);
+      told_rest.get(turn, c, column, rests);
       told_e.get(turn, c, column, es);
       if (!ENDS) {
         float hs[WAVES];
@@ -529,14 +568,14 @@ __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P)
         const int from = wave - wave % S::KEPT_WAVES;
 #pragma unroll
         for (int w = 0; w + 1 < WAVES; ++w)
-          if (w >= from && w < wave) h[c] = __builtin_fmaf(as[w], h[c], hs[w]);
+          if (w >= from && w < wave) h[c] = through(as[w], rests[w], h[c], hs[w]);
         h[c] = __builtin_fmaf(joined[c].before_a, h[c], joined[c].before_h);
       }
       e[c] = carry[c];
 #pragma unroll
       for (int w = WAVES - 1; w >= 0; --w) {
-        carry[c] = __builtin_fmaf(as[w], carry[c], es[w]);
-        if (ENDS) factor[c] *= as[w];
+        carry[c] = through(as[w], rests[w], carry[c], es[w]);
+        if (ENDS) factor[c].by(as[w], Product::of(as[w], rests[w]).q);
         if (w == wave + 1) e[c] = carry[c];
       }
       e[c] = __builtin_fmaf(joined[c].behind_a, e[c], joined[c].behind_e);
@@ -547,7 +586,7 @@ __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
         before[k][c] = h[c];
-        h[c] = stay[k][c].of(h[c], take[k][c] * in[k][c]);
+        h[c] = __builtin_fmaf(on[k][c], h[c], take[k][c] * in[k][c]);
       }
 #pragma unroll
     for (int k = FRAMES - 1; k >= 0; --k) {
@@ -557,9 +596,9 @@ __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P)
         e[c] += go[k][c];
         const bool here = FULL || t + k < used;
         vec_set<V>(ox, c, (T)(here ? take[k][c] * e[c] : 0.f));
-        vec_set<V>(of, c, (T)(here ? stay[k][c].a * off[k][c] * e[c] * (INPUT ? before[k][c] : before[k][c] - in[k][c]) : 0.f));
+        vec_set<V>(of, c, (T)(here ? on[k][c] * off[k][c] * e[c] * (INPUT ? before[k][c] : before[k][c] - in[k][c]) : 0.f));
         if (INPUT) vec_set<V>(oi, c, (T)(here ? take_slope[k][c] * e[c] * in[k][c] : 0.f));
-        e[c] = stay[k][c].of(e[c]);
+        e[c] *= on[k][c];
       }
       if ((FULL || t + k < end) && part.live) {
         const long long at = (long long)(t + k) * P.C;
@@ -582,7 +621,7 @@ __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P)
   if (ENDS) {
     float* p = P.parts + (b * P.segments + part.segment) * 2 * P.C + channel;
 #pragma unroll
-    for (int c = 0; c < V; ++c) p[c] = factor[c], p[P.C + c] = carry[c];
+    for (int c = 0; c < V; ++c) p[c] = factor[c].code(), p[P.C + c] = carry[c];
     return;
   }
   if (P.gfirst && part.segment == 0)
@@ -605,8 +644,10 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStep P) {
     float* state = P.state + b * P.C + channel;
     T* out = static_cast<T*>(P.out) + b * P.C + channel;
     const auto next = [](float h, T x, T f, T i) {
+      // (a as the nearest float32 and what that leaves of it; the first difference is exact from a half on, and below it a float32 holds a to its own 2^-24)
       const Gate a = gate(f);
-      return Stay(a, true).of(h, (INPUT ? gate(i).on : a.off) * (float)x);
+      const float rest = a.on >= 0.5f ? (1.f - a.on) - a.off : 0.f;
+      return __builtin_fmaf(a.on, h, __builtin_fmaf(rest, h, (INPUT ? gate(i).on : a.off) * (float)x));
     };
     if (channel + STEP <= P.C) {
       const auto vx = vec_load<STEP>(x), vf = vec_load<STEP>(f), vi = INPUT ? vec_load<STEP>(i) : vf;

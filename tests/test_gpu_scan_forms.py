@@ -104,3 +104,60 @@ def test_forms(nb, B, T, C, gated, dtype):
                 near(name, got, *want[name])
                 if lengths is not None and got.dim() == 3:
                     assert not got[torch.arange(T, device=DEV) >= ragged[:, None]].any(), name
+
+
+@pytest.mark.parametrize("B,C", [(1, 64), (4, 1024), (16, 512)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_steady_gates(nb, B, C, gated):
+    """A decay for each channel, the same in every frame, over 16,384 frames: what is left of a first state, of a constant input, and the gradients that come all the way.  A run's 1 - A is off by
+    6 U for the gate (exponential 3, its sum, the reciprocal and the product 1 each), 5 for its own sum (eight additions of a sum that grows to it), 1 for what they add and 2 for each time that
+    runs are joined: 16 U at most, if all had one sign, of a sum over all frames of ten at most: 9.6e-6; a state's own steps, 1,024 roundings of up to U / 2, are a walk of less than 4e-7: below 1e-5 together.
+    In half of the channels the sum is below 0.6: the median is below 2e-6."""
+    T = 16384
+    f = torch.linspace(7.4, 13, C, device=DEV)
+    a, q = torch.sigmoid(f.double()), torch.sigmoid(-f.double())
+    left = torch.exp(T * torch.log1p(-q))
+    some = -torch.expm1(T * torch.log1p(-q))
+    f = f.expand(B, T, C)
+    one, zero = torch.ones(1, 1, C, device=DEV).expand(B, T, C), torch.zeros(1, 1, C, device=DEV).expand(B, T, C)
+    first = 0.5 + torch.rand(B, C, device=DEV, generator=torch.Generator(device=DEV).manual_seed(C))
+
+    def held(name, got, want):
+        off = ((got.double() - want) / want).abs()
+        _say(name, float(off.max()), float(off.median()))
+        assert float(off.max()) <= 1e-5 and float(off.median()) <= 2e-6, (name, float(off.max()), float(off.median()))
+
+    # (a gate of the input's own that is open as far as the other's is closed)
+    i = -f.contiguous() if gated else None
+    _, last, kept = nb.nna_gated_scan(zero, f, i, state=first, want_state=True, keep=True)
+    held("left", last, left * first.double())
+    h, last = nb.nna_gated_scan(one, f, i, want_state=True)
+    held("of ones", last, some.expand(B, C))
+    held("of ones, the last frame", h[:, -1], some.expand(B, C))
+    gx, gf, gi, gfirst = nb.nna_gated_scan_backward(torch.zeros(B, T, C, device=DEV), kept, zero, f, i, gstate=first, want_gstate=True)
+    held("first state's gradient", gfirst, left * first.double())
+    held("first frame's", gx[:, 0], q * torch.exp((T - 1) * torch.log1p(-q)) * first.double())
+    # gf: a (1 - a) e h, the state left of the first one so far times the gradient left of the last one: the same in all frames
+    held("gates'", gf[:, 5000], q * left * first.double() ** 2)
+    gx, _, _, gfirst = nb.nna_gated_scan_backward(one.contiguous(), kept, zero, f, i, want_gstate=True)
+    held("of ones, first state's", gfirst, (a * some / q).expand(B, C))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("B,C", [(1, 128), (4, 2048), (16, 1024)])
+def test_steady_gates_of_16_bits(nb, B, C, dtype):
+    """The same of 16-bit gates, whose exponential's argument (up to 11 where the sum is large) is one float32: 6 U for its rounding, 2 for its factor's, 2 for the exponential and 3 as above, and 10
+    for the sums: 23 U of a sum of ten: 1.4e-5, and the walk: 1.5e-5."""
+    T = 16384
+    f = torch.linspace(7.41, 13, C, device=DEV).to(dtype)
+    q = torch.sigmoid(-f.double())
+    left, some, f = torch.exp(T * torch.log1p(-q)), -torch.expm1(T * torch.log1p(-q)), f.expand(B, T, C)
+    first = 0.5 + torch.rand(B, C, device=DEV, generator=torch.Generator(device=DEV).manual_seed(C))
+    zero, one = torch.zeros(1, 1, C, device=DEV, dtype=dtype).expand(B, T, C), torch.ones(1, 1, C, device=DEV, dtype=dtype).expand(B, T, C)
+    _, last, kept = nb.nna_gated_scan(zero, f, state=first, want_state=True, keep=True)
+    ones = nb.nna_gated_scan(one, f, want_state=True)[1]
+    gfirst = nb.nna_gated_scan_backward(zero.contiguous(), kept, zero, f, gstate=first, want_gstate=True)[3]
+    for name, got, want in (("left", last, left * first.double()), ("of ones", ones, some.expand(B, C)), ("gradient", gfirst, left * first.double())):
+        off = ((got.double() - want) / want).abs()
+        _say(name, dtype, float(off.max()), float(off.median()))
+        assert float(off.max()) <= 1.5e-5 and float(off.median()) <= 2e-6, (name, float(off.max()), float(off.median()))
