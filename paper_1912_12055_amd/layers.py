@@ -654,6 +654,16 @@ class GatedRecurrence(torch.nn.Module):
         return nb.nna_gated_scan_step(x, forget, state, input=input)
 
 
+_NO_GRADIENT = {type(None)}
+
+
+def _contiguous(grads):
+    try:
+        return all(map(torch.Tensor.is_contiguous, grads))
+    except RuntimeError:  # (a sparse one has no such thing)
+        return False
+
+
 class AdamW(torch.optim.Optimizer):
     """AdamW over all of a group's tensors in one pass (``nna_adamw``): contiguous float32, bfloat16 and float16 parameters of one device, a group's together.
 
@@ -746,7 +756,8 @@ class AdamW(torch.optim.Optimizer):
         for n, group in enumerate(self.param_groups):
             params = group["params"]
             grads = [p.grad for p in params]
-            if not params or all(g is None for g in grads):
+            kinds = set(map(type, grads))  # (asked of all without a loop in Python)
+            if kinds <= _NO_GRADIENT:
                 continue
             written, unknown = (), "m" in group and group["copies"] is not None and n not in self._versions
             if "m" in group and group["copies"] is not None and not unknown:
@@ -757,32 +768,33 @@ class AdamW(torch.optim.Optimizer):
                     raise RuntimeError("a recorded step needs capturable=True, and a step before it that is not recorded")
                 if written or unknown:
                     raise RuntimeError("16-bit parameters were written, or states loaded, since the last step: take a step that is not recorded first")
-            todo.append((n, group, grads, written, unknown))
-        for n, group, grads, written, unknown in todo:
+            todo.append((n, group, grads, kinds.isdisjoint(_NO_GRADIENT), written, unknown))
+        for n, group, grads, whole, written, unknown in todo:
             if "m" not in group:
                 self._begin(group)
             elif unknown:
                 self._compare(group)
             elif written:
                 self._copy(group, written)
-            self._step_group(group, grads)
+            self._step_group(group, grads, whole)
             if group["copies"] is not None:
                 self._versions[n] = [p._version for p in group["params"]]
         return loss
 
     @staticmethod
-    def _step_group(group, grads):
-        """One step of a group's tensors; one that is refused leaves the numbers of steps as they were."""
+    def _step_group(group, grads, whole):
+        """One step of a group's tensors (`whole`: they all have a gradient); one that is refused leaves the numbers of steps as they were."""
         lr, steps = group["lr"], group["steps"]
         if isinstance(lr, torch.Tensor) and not lr.is_cuda:
             lr = float(lr)
         if isinstance(steps, torch.Tensor):
-            counts = [group["step"], steps] if all(g is not None for g in grads) else [group["step"], *(one for one, g in zip(steps.unbind(), grads) if g is not None)]
+            counts = [group["step"], steps] if whole else [group["step"], *(one for one, g in zip(steps.unbind(), grads) if g is not None)]
             torch._foreach_add_(counts, 1)
         else:
-            steps = [n + (g is not None) for n, g in zip(steps, grads)]
+            steps = [n + 1 for n in steps] if whole else [n + (g is not None) for n, g in zip(steps, grads)]
         try:
-            grads = [g if g is None or g.is_sparse or g.is_contiguous() else g.contiguous() for g in grads]
+            if not whole or not _contiguous(grads):
+                grads = [g if g is None or g.is_sparse or g.is_contiguous() else g.contiguous() for g in grads]
             nb.nna_adamw(group["params"], grads, group["m"], group["v"], steps, lr=lr, betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
                          m_scales=group["m_scales"], v_scales=group["v_scales"], master=group["copies"])
         except BaseException:
