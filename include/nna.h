@@ -729,6 +729,7 @@ nna_status nna_gated_scan_step(const void* x_dev, long long x_stride, const void
  *   m_dev, v_dev [state_size] float32 (state_size: where the tensor behind the last one's would begin), m_scales_dev and v_scales_dev NULL; or int8 (m) and uint8 (v) codes with float32 scales [state_size / 128].  Zeros before the first step
  *   master_dev   [state_size] float32 or NULL: the float32 copies that tensors of 16 bits are updated in and rounded from (float32 tensors have none)
  *   step_dev, lr_dev  NULL, or the step's number (from 1) and lr in device memory in the place of step and lr: for steps recorded into a graph
+ *   eps          at least 0; one above zero and below 2^-126 is taken for that
  * nna_adamw_steps: the same, with t of each tensor: steps[count] in host memory, or steps_dev[count] in device memory in its place (apart = 1); or one for all, steps[1] or steps_dev[1]
  * (apart = 0).  A tensor whose gradient comes and goes has taken fewer steps than others: with the others' t its moments would be taken for whole ones.
  * 8 bits: 128 neighbours share a scale s, their largest magnitude.  A code c of m stands for s (c / 127) |c / 127|, rounded to the nearest code; one of v for s (c / 255)^4, rounded

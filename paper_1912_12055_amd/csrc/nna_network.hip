@@ -213,7 +213,8 @@ nna_status adamw(const AdamwCall& c, bool states_too, int device, void* hip_stre
   P.lr_dev = c.lr_dev;
   P.lr = c.lr;
   P.weight_decay = c.weight_decay;
-  P.eps = (float)c.eps;
+  // (the quotient's reciprocal takes no float32 below the normal ones: beside a root that is not zero an eps as small is nothing, and beside one that is, nothing over it stays nothing)
+  P.eps = c.eps > 0.0 ? std::max((float)c.eps, 0x1p-126f) : 0.f;
   P.piece = adamw_piece(values);
   P.count = P.pieces = 0;
   long long at = 0;

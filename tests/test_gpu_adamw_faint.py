@@ -84,3 +84,17 @@ def test_many_tensors_in_8_bits(nb, dtypes):
     shift = (((torch.arange(v.numel(), device=DEV) * 0x9E3779B9 + 5 * 0xB504F333) & 0xFFFFFFFF) >> 8).double() * 2.0**-24
     codes = torch.floor(255 * (v / torch.where(most > 0, most, 1)) ** 0.25 + shift).clamp(max=255)
     assert torch.equal(s["v"].double(), torch.where(v > 0, codes.clamp(min=1), 0))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-38, 1e-40, 1e-45, 1e-60])
+def test_no_gradient_and_an_eps_below_float32(nb, bits, eps):
+    """Nothing over an eps that has no normal float32 is nothing, and not a NaN."""
+    p, s = torch.ones(300, device=DEV), states(nb, [300], bits)
+    g = torch.zeros(300, device=DEV)
+    g[7] = 1.0
+    for t in (1, 2):
+        nb.nna_adamw([p], [g], step=t, **s, lr=0.25, betas=(0.9, 0.99), eps=eps, weight_decay=0.0)
+    rest = torch.ones(300, dtype=torch.bool, device=DEV)
+    rest[7] = False
+    assert bool((p[rest] == 1).all()) and abs(float(p[7]) - 0.5) <= 40 * U
