@@ -696,6 +696,10 @@ class AdamW(torch.optim.Optimizer):
         super().__setstate__(state)
         self.__dict__.setdefault("_versions", {})
 
+    @staticmethod
+    def _narrow(group):
+        return group["master"] and any(p.dtype != torch.float32 for p in group["params"])
+
     def _begin(self, group):
         """The states of a group, zero, and the float32 copies of its 16-bit parameters."""
         params = group["params"]
@@ -704,7 +708,7 @@ class AdamW(torch.optim.Optimizer):
         group["m"] = torch.zeros(size, dtype=torch.int8 if codes else torch.float32, device=device)
         group["v"] = torch.zeros(size, dtype=torch.uint8 if codes else torch.float32, device=device)
         group["m_scales"], group["v_scales"] = (torch.zeros(size // nb.NNA_BLOCK8, device=device) if codes else None for _ in range(2))
-        narrow = group["master"] and any(p.dtype != torch.float32 for p in params)
+        narrow = self._narrow(group)
         group["copies"] = torch.zeros(size, device=device) if narrow else None
         self._count(group)
         if group["capturable"]:
@@ -744,6 +748,8 @@ class AdamW(torch.optim.Optimizer):
             for name in ("m", "v", "m_scales", "v_scales", "copies", "step", "steps"):
                 if isinstance(group.get(name), torch.Tensor):
                     group[name] = group[name].to(group["params"][0].device)
+            if "m" in group and group["copies"] is None and self._narrow(group):
+                group["copies"] = torch.zeros(group["m"].numel(), device=group["m"].device)  # (states of float32 weights: the next step takes the copies)
         self._versions = {}
 
     @torch.no_grad()

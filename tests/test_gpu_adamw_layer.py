@@ -238,3 +238,20 @@ def test_frequencies_are_constants(layers):
         layers.RotaryHeads(8, freqs=torch.nn.Parameter(torch.ones(4)))
     with torch.no_grad():
         layers.RotaryHeads(8, freqs=f.detach())
+
+
+def test_a_load_into_16_bit_weights_makes_their_copies(layers):
+    """States saved of float32 weights have no copies: a 16-bit model that loads them gets its own, and keeps small steps."""
+    p = torch.nn.Parameter(torch.ones(300, device=DEV))
+    a = layers.AdamW([p], lr=1e-4, weight_decay=0.0)
+    p.grad = torch.ones_like(p)
+    a.step()
+    q = torch.nn.Parameter(torch.ones(300, device=DEV, dtype=torch.bfloat16))
+    b = layers.AdamW([q], lr=1e-4, weight_decay=0.0)
+    b.load_state_dict(copy.deepcopy(a.state_dict()))
+    for _ in range(60):
+        q.grad = torch.ones_like(q)
+        b.step()
+    # 60 steps of lr: 1e-4 off by 2^-20 of itself each, the copy by half a step of a value below 1
+    got = b.param_groups[0]["copies"][:300].double()
+    assert float((got - (1 - 60e-4)).abs().max()) <= 60 * (2.0**-25 + 1e-4 * 2.0**-20) and torch.equal(q.detach(), got.bfloat16())
