@@ -745,6 +745,9 @@ class AdamW(torch.optim.Optimizer):
         for group in self.param_groups:
             if "m" in group and "steps" not in group:
                 self._count(group)
+            lr = group["lr"]
+            if group["capturable"] and isinstance(lr, torch.Tensor) and lr.dtype == torch.float32:
+                group["lr"] = lr.to(group["params"][0].device)  # (one in host memory would be a constant of the graphs that record it)
             for name in ("m", "v", "m_scales", "v_scales", "copies", "step", "steps"):
                 if isinstance(group.get(name), torch.Tensor):
                     group[name] = group[name].to(group["params"][0].device)

@@ -255,3 +255,16 @@ def test_a_load_into_16_bit_weights_makes_their_copies(layers):
     # 60 steps of lr: 1e-4 off by 2^-20 of itself each, the copy by half a step of a value below 1
     got = b.param_groups[0]["copies"][:300].double()
     assert float((got - (1 - 60e-4)).abs().max()) <= 60 * (2.0**-25 + 1e-4 * 2.0**-20) and torch.equal(q.detach(), got.bfloat16())
+
+
+def test_a_rate_in_device_memory_is_loaded_there(layers):
+    """A recorded step reads its rate where it is: one that a load brought in host memory would be a constant of the graph."""
+    p = torch.nn.Parameter(torch.ones(5, device=DEV))
+    a = layers.AdamW([p], lr=torch.tensor(1e-2, device=DEV), weight_decay=0.0, capturable=True)
+    p.grad = torch.ones_like(p)
+    a.step()
+    saved = copy.deepcopy(a.state_dict())
+    saved["param_groups"][0]["lr"] = saved["param_groups"][0]["lr"].cpu()
+    a.load_state_dict(saved)
+    rate = a.param_groups[0]["lr"]
+    assert rate.is_cuda and float(rate) == float(torch.tensor(1e-2))
