@@ -11,7 +11,7 @@
 // The moments' codes and scales are what 64 bits make of them, so that a code is what the definition says and not what an order of roundings makes of it.  (The largest code's value is the
 // scale itself, and no product is fused into a sum: b1 s + (1 - b1) g is often halfway between two float32, and which of them is the next scale has to be one answer.)  Float32 does what it
 // can tell, and 64 bits the few values near a border or a block's largest: in 64 bits throughout, 126 to 170 instructions a value, 201 million bfloat16 weights with their float32 copies took
-// 890 to 1,025 us; now 655, 5.0 TB/s.  With states in 32 bits 1,107 us, 5.1 TB/s.  A table of a launch's tensors goes with its arguments; 26 small tensors, 1.6 million values: 10 us.
+// 890 to 1,025 us; now 642, 5.1 TB/s.  With states in 32 bits 1,092 us, 5.2 TB/s.  A table of a launch's tensors goes with its arguments; 28 small tensors, 1.6 million values: 10 us.
 #include "nna_adamw.h"
 #include "nna_vector.h"
 

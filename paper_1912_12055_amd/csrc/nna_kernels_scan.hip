@@ -250,8 +250,8 @@ struct alignas(16) Told {
 };
 
 // Forward.  ENDS: no outputs, but what each segment makes of the state before it, P.parts[b][segment][A (coded), h][C]; the mix composes those of the segments before its own.
-// The next round's loads are asked for when this one's values have been used, half a round ahead.  16 x 4,096 frames of 2,048 channels, bfloat16: 170 us, 4.7 TB/s of the 5.1 that a copy
-// reaches; 4 x 16,384 (rows of half lines): 193 us.  With D and G of run_ends here, too, it takes a third of the instructions less, 143 registers, and is no faster.
+// The next round's loads are asked for when this one's values have been used, half a round ahead.  16 x 4,096 frames of 2,048 channels, bfloat16: 171 us, 4.7 TB/s of the 5.1 that a copy
+// reaches; 4 x 16,384 (rows of half lines): 195 us.  With D and G of run_ends here, too, it takes a third of the instructions less, 143 registers, and is no faster.
 template <typename T, int V, int CL, int FRAMES, int WAVES, bool INPUT, bool ENDS>
 __global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
   typedef Shape<CL, FRAMES, WAVES> S;
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(WAVES * 64) void scan_kernel(ScanParams P) {
 }
 
 // Backward, from the last frame to the first; the states inside a round are made again from the kept one.  ENDS: what each segment makes of the carry behind it, P.parts[b][segment][A (coded), e][C].
-// 16 x 4,096 frames of 2,048 channels, bfloat16: 316 us, 4.2 TB/s; 4 x 16,384: 364 us.  Rounds of eight frames a lane need 230 registers and more, half as many 150.
+// 16 x 4,096 frames of 2,048 channels, bfloat16: 300 us, 4.5 TB/s; 4 x 16,384: 361 us.  Rounds of eight frames a lane need 230 registers and more, half as many 156.
 template <typename T, int V, int CL, int FRAMES, int WAVES, bool INPUT, bool ENDS>
 __global__ __launch_bounds__(WAVES * 64) void scan_backward_kernel(ScanParams P) {
   typedef Shape<CL, FRAMES, WAVES> S;
@@ -671,9 +671,9 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanStep P) {
 }
 
 // How a call is cut up: neighbouring channels' lanes in a wave, waves, segments.  16 sequences of 4,096 frames of 2,048 channels in bfloat16, forward and backward: 32 lanes (rows of 128 bytes, a
-// line) 170 and 316 us, 16 lanes 217 and 385, 8 lanes (4 sequences of 16,384) 270 and 413: lines shared by workgroups cost more than waves that wait.  So 32 lanes wherever their workgroups
-// fill the card: 256 of them, the same values, 162 and 308.  128 of them leave half of it idle, 265 and 527; 16 lanes' 256 take 193 and 365, eight segments of 32 lanes 134 + 156 and
-// 141 + 302 (two readings).  With 64 workgroups of 32 lanes (half the values) 16 lanes take 159 and 308, segments 69 + 75 and 75 + 153.
+// line) 171 and 300 us, 16 lanes 220 and 391: lines shared by workgroups cost more than waves that wait.  So 32 lanes wherever their workgroups
+// fill the card: 256 of them, the same values, 167 and 304.  128 of them leave half of it idle, 272 and 527; 16 lanes' 256 take 195 and 361, segments of 32 lanes (512 workgroups) 108 + 165 and
+// 110 + 311 (two readings).  With 64 workgroups of 32 lanes (half the values) 16 lanes take 162 and 309, segments 54 + 80 and 60 + 170.
 struct Cut {
   int lanes, waves;
   int segments, frames;
@@ -687,7 +687,7 @@ Cut cut_of(long long B, long long T, long long C, int channels /* of a lane */) 
     if (narrow >= 200) {
       c.lanes = 16;
     } else {
-      // 512 workgroups: one sequence of 15,504 frames of 512 channels 10 + 13 us, with 1,024 of them 10 + 17
+      // 512 workgroups: one sequence of 15,504 frames of 512 channels 9 + 14 us, with 1,024 of them 9 + 18
       const long long rounds = (T + 127) / 128, want = std::min((512 + wide - 1) / wide, rounds), each = (rounds + want - 1) / want;
       c.segments = (int)((rounds + each - 1) / each);
       c.frames = (int)(each * 128);

@@ -583,7 +583,7 @@ class _RotateFn(torch.autograd.Function):
 
 class RotaryHeads(torch.nn.Module):
     """Queries and keys of heads of `width` values, each head normalised by its root mean square (``eps=None``: not) and the pairs of its first `rotary` values (all of them if None)
-    rotated by its frame's position, in one pass: what ``DecayAttention`` takes.
+    rotated by its frame's position, in one pass: what ``DecayAttention`` takes (float32 or bfloat16, as many keys as queries).
 
     ``q_weight`` and ``k_weight`` are float32 parameters of the norms.  ``freqs``: float64 radians a position, or by ``base`` and ``scale`` (``nna_rotary_freqs``).  Pair j is
     (j, j + rotary / 2), or ``interleaved`` (2 j, 2 j + 1)."""
