@@ -144,8 +144,9 @@ struct AdamwCall {
   double beta1, beta2, eps, weight_decay;
 };
 
-// What a workgroup writes no other one may read or write: weights, states, and (states_too, of gradients) what is read beside them.  `size` values of states
-nna_status refuse_shared(const AdamwCall& c, long long size, bool states_too) {
+// What a workgroup writes no other one may read or write: weights, states, and (states_too, of gradients) what is read beside them.  The states are taken whole first, `size` values of each,
+// and if that fails (`closely`) tensor by tensor, as they are written: those without a gradient are not, nor copies of float32 tensors, whose weights may lie there.
+nna_status refuse_shared(const AdamwCall& c, long long size, bool states_too, bool closely) {
   std::vector<Span> weights, all, grads;
   weights.reserve((size_t)c.count);
   grads.reserve((size_t)c.count);
@@ -157,11 +158,25 @@ nna_status refuse_shared(const AdamwCall& c, long long size, bool states_too) {
   }
   if (!disjoint(weights)) return fail(NNA_ERR_INVALID_ARG, "two tensors share memory");
   if (weights.empty()) return NNA_OK;
-  all.reserve(weights.size() + 5);
+  all.reserve(weights.size() * (closely ? 6 : 1) + 5);
   all = weights;
-  const long long value = c.m_scales ? 1 : 4, blocks = size / ADAMW_BLOCK;
-  for (const Span& s : {span_of(c.m, size * value), span_of(c.v, size * value), span_of(c.m_scales, blocks * 4), span_of(c.v_scales, blocks * 4), span_of(c.master, size * 4)})
-    if (s.from) all.push_back(s);
+  const long long value = c.m_scales ? 1 : 4;
+  const auto states = [&](long long at, long long n, bool copied) {
+    const long long block = at / ADAMW_BLOCK, blocks = (n + ADAMW_BLOCK - 1) / ADAMW_BLOCK;
+    for (void* p : {c.m, c.v}) all.push_back(span_of(static_cast<char*>(p) + at * value, n * value));
+    for (float* p : {c.m_scales, c.v_scales})
+      if (p) all.push_back(span_of(p + block, blocks * 4));
+    if (c.master && copied) all.push_back(span_of(c.master + at, n * 4));
+  };
+  if (closely) {
+    long long at = 0;
+    for (long long i = 0; i < c.count; ++i) {
+      if (c.n[i] && c.g[i]) states(at, c.n[i], c.types[i] != NNA_F32);
+      at += (c.n[i] + ADAMW_BLOCK - 1) / ADAMW_BLOCK * ADAMW_BLOCK;
+    }
+  } else {
+    states(0, size, true);
+  }
   if (!disjoint(all)) return fail(NNA_ERR_INVALID_ARG, "two of the states, or a state and a tensor, share memory");
   for (const Span& g : grads)
     if (meets(g, states_too ? all : weights)) return fail(NNA_ERR_INVALID_ARG, "a gradient shares memory with what the step writes");
@@ -192,9 +207,15 @@ nna_status adamw(const AdamwCall& c, bool states_too, int device, void* hip_stre
     values += c.n[i];
   }
   if (values && (!c.m || !c.v)) return fail(NNA_ERR_INVALID_ARG, "m_dev or v_dev is NULL");
+  const void* states[] = {c.m, c.v, c.m_scales, c.v_scales, c.master};
+  for (const void*& a : states)
+    for (const void*& b : states)
+      if (values && a && &a != &b && a == b) return fail(NNA_ERR_INVALID_ARG, "two of the states are the same");
   try {
-    const nna_status shared = refuse_shared(c, size, states_too);
-    if (shared != NNA_OK) return shared;
+    if (refuse_shared(c, size, states_too, false) != NNA_OK) {
+      const nna_status shared = refuse_shared(c, size, states_too, true);
+      if (shared != NNA_OK) return shared;
+    }
   } catch (const std::exception&) {
     return fail(NNA_ERR_ALLOC, "out of host memory");
   }
